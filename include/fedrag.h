@@ -4,10 +4,11 @@
  *
  * General rules for every call
  * ----------------------------
- * - Every data pointer is DEVICE memory owned by the caller, 16-byte aligned, dense row-major.
- *   The library never allocates, frees or keeps a pointer after the call returns.  Two kinds of argument are HOST
- *   memory and say so where they are declared: the fedrag_structured_key structs (which hold device pointers) and
- *   the per-shard arrays of fedrag_partial_attn_shards; they are read during the call only.
+ * - Every data pointer is DEVICE memory owned by the caller, 16-byte aligned, dense row-major (the rows of the paged
+ *   calls have strides).  The library never allocates, frees or keeps a pointer after the call returns.  Three kinds of
+ *   argument are HOST memory and say so where they are declared: the fedrag_structured_key structs, the fedrag_rows and
+ *   fedrag_paged_cache structs (all of which hold device pointers) and the per-shard arrays of
+ *   fedrag_partial_attn_shards; they are read during the call only.
  * - Tensors are laid out [batch, heads, tokens, d_head] ("[B,H,L,d]").  Query head h uses KV head
  *   h / (n_q_heads / n_kv_heads); scrambling matrices are per KV head, [n_kv_heads, d, d], row-major,
  *   and multiply ROW vectors from the right (x . Phi), the paper's convention (Section 2.1, footnote).
@@ -344,6 +345,115 @@ fedrag_status fedrag_partial_attn_varlen_quantized(const fedrag_shape* shape, in
                                                    const int32_t* kv_lens, const int32_t* q_lens,
                                                    float softmax_scale, float* O_part, float* lse,
                                                    void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The cache of a node that serves many requests: K, V rows (a Compute Node's K', V' or an Inquirer's own) in pages of
+ * page_tokens tokens, handed out from one pool, and a table per request that says which page holds which tokens.  Four
+ * calls: fedrag_paged_map plans a step from the requests' lengths, fedrag_paged_write puts the step's rows into their
+ * pages, fedrag_paged_attn attends to them, fedrag_paged_attn_workspace_bytes sizes the latter's scratch.
+ *
+ * The rows of a step are ragged: request b has rows q_start[b] .. q_start[b+1]-1 of all n_rows, and rows from
+ * q_start[batch] on are padding.  Tensors of rows are the [B,H,L,d] of the other calls with B = 1 and L = n_rows, so that
+ * fedrag_scramble_q, fedrag_unscramble, fedrag_unscramble_merge and fedrag_lse_merge take them as they are.
+ * Lengths, tables and slots are DEVICE memory: a step is planned, written and attended to without the host knowing
+ * them.  What they hold is checked where it is used: a page id outside [0, n_pages) means that there is no page, and
+ * the tokens it would hold are neither written nor attended to.
+ *
+ * The two structs are HOST memory holding DEVICE pointers, read during the call only.
+ */
+typedef struct {
+    void* K;             /* page p, head g, token t in the page, channel c:                       */
+    void* V;             /*   p * page_stride + (g * page_tokens + t) * d + c, in shape->dtype    */
+    int64_t n_pages;     /* pages of the pool, 0 .. INT32_MAX                                     */
+    int64_t page_stride; /* elements from a page to the next; 0 = n_kv_heads * page_tokens * d    */
+    int32_t page_tokens; /* 16, 32, 64, 128 or 256 (else FEDRAG_ERR_UNSUPPORTED)                  */
+} fedrag_paged_cache;
+
+typedef struct {
+    const void* data;     /* row t of head h begins at h * head_stride + t * token_stride, d elements without gaps */
+    int64_t head_stride;  /* elements, >= 0, multiples of 16 bytes                                                  */
+    int64_t token_stride;
+} fedrag_rows;
+
+/*
+ * The bookkeeping of one step, from the requests' lengths.  Request b has cached_lens[b] tokens in the cache and brings
+ * new_lens[b] more; its table row names a page for every page_tokens tokens of the cached ones.
+ *     q_start = exclusive prefix sums of new_lens, q_start[batch] their total;   kv_lens[b] = cached_lens[b] + new_lens[b];
+ *     the pages that kv_lens[b] tokens need beyond those that cached_lens[b] need are taken from the top of the stack
+ *     free_pages[0 .. *free_count-1], the first one for the first request that needs one, and entered in the table;
+ *     *free_left = what is left on the stack;
+ *     row t of request b: positions[t] = cached_lens[b] + t - q_start[b],
+ *                         slots[t] = block_table[b][positions[t] / page_tokens] * page_tokens + positions[t] % page_tokens;
+ *     padding rows: both -1.
+ * cached_lens, new_lens, kv_lens : int32 [batch];  q_start : int32 [batch + 1];  block_table : int32 [batch, max_pages],
+ * in and out, entries of no new page keep what they hold;  slots : int64 [n_rows], 8-byte aligned;  positions : int32
+ * [n_rows] or NULL;  free_pages : int32 [n_free];  free_count, free_left, flags : int32 [1].
+ * kv_lens may be cached_lens and free_left may be free_count (the same address): the call then advances the state of
+ * its own accord, and a recorded step can be replayed.  No other output may overlap anything (FEDRAG_ERR_ALIAS).
+ * flags receives 0, or the sum of
+ *     1  the stack ran out: tokens without a page have the table entry -1 and the slot -1;
+ *     2  a request needs more than max_pages pages: tokens beyond them have the slot -1;
+ *     4  new_lens come to more than n_rows: the rows beyond are cut off, and so are the lengths in q_start and kv_lens;
+ *     8  a length below zero (taken as 0), tokens beyond INT32_MAX (cached_lens is cut), or *free_count outside
+ *        [0, n_free] (taken as the nearer of the two).
+ * To release a request's pages, put their ids back on the stack and add their number to the count.
+ * One launch up to some thousand rows, two beyond.  batch, n_rows, max_pages, n_free : 0 .. INT32_MAX; n_free may be 0
+ * with free_pages NULL, and tensors of no elements may be NULL.
+ */
+#define FEDRAG_MAP_NO_PAGES 1
+#define FEDRAG_MAP_NO_COLUMNS 2
+#define FEDRAG_MAP_NO_ROWS 4
+#define FEDRAG_MAP_BAD_LENGTH 8
+fedrag_status fedrag_paged_map(int32_t batch, int64_t n_rows, int32_t page_tokens, int64_t max_pages,
+                               const int32_t* cached_lens, const int32_t* new_lens,
+                               const int32_t* free_pages, int64_t n_free, const int32_t* free_count,
+                               int32_t* block_table, int32_t* q_start, int32_t* kv_lens, int64_t* slots,
+                               int32_t* positions, int32_t* free_left, int32_t* flags, void* stream);
+
+/*
+ * Rows into pages: for every row t and KV head h,
+ *     K page slots[t] / page_tokens, head h, token slots[t] % page_tokens  <-  row t of head h of K_rows;  V likewise.
+ * A row whose slot lies outside [0, n_pages * page_tokens) is not written.  Slots must be distinct among those rows: two
+ * rows of one slot leave a mixture of the two.  Bytes are moved as they are.  shape: n_kv_heads, d_head, dtype (batch
+ * and n_q_heads are not used, but must be valid).  K_rows, V_rows : n_rows rows of n_kv_heads heads, 16-byte aligned,
+ * each with strides of its own (views of a projection's output, or what fedrag_scramble_kv returned).  The pages must
+ * not overlap the rows, nor K's pages V's (FEDRAG_ERR_ALIAS; pages that take turns in one tensor are fine).
+ */
+fedrag_status fedrag_paged_write(const fedrag_shape* shape, int64_t n_rows, const fedrag_rows* K_rows,
+                                 const fedrag_rows* V_rows, const int64_t* slots, const fedrag_paged_cache* cache,
+                                 void* stream);
+
+/*
+ * Attention of a step's rows over the paged cache, in which the step's own rows are already.  shape->batch = number of
+ * requests.  Row i of request b, i = 0 .. n-1 with n = q_start[b+1] - q_start[b], sees the first
+ *     kv_lens[b] tokens of the request (causal = 0: a Compute Node's part, Section 4.1), or of them the first
+ *     kv_lens[b] - n + i + 1 (causal = 1: the new rows are the last tokens, and a token sees itself and what comes
+ *     before; the Inquirer's own part, Section 5.3),
+ * as far as block_table[b][..] names pages for them.  A token that a row does not see does not touch it, whatever its
+ * K and V hold (NaN and infinities among it).
+ *     O[h,t,:] = softmax(<Q[h,t], K> * softmax_scale) . V,   lse[h,t] = ln sum exp(<Q[h,t], K> * softmax_scale)
+ * with n_q_heads / n_kv_heads query heads to a KV head; a row that sees nothing has O = 0, lse = -inf.
+ * Q : n_rows rows of n_q_heads heads with strides;  O : fp32 [n_q_heads, n_rows, d], lse : fp32 [n_q_heads, n_rows],
+ * dense; padding rows of both keep what they held.
+ * block_table : int32 [batch, max_pages];  q_start : int32 [batch + 1], not decreasing;  kv_lens : int32 [batch].
+ * Values of q_start outside [0, n_rows] are taken as the nearer bound, kv_lens below 0 as 0.
+ * max_q_len : the most rows that a request is expected to have, 0 = not known.  It decides which kernels are launched,
+ * never the result: requests with more rows are attended to all the same, only more slowly.
+ * 16-bit storage: probabilities enter the second product as two storage-type terms, so that a sum keeps about 16
+ * significant bits of each; everything else is fp32.
+ * workspace : at least fedrag_paged_attn_workspace_bytes(...) bytes for the same arguments, 16-byte aligned.  The longest
+ * requests' keys are cut into runs that are attended to side by side, and their partials land there.
+ */
+fedrag_status fedrag_paged_attn(const fedrag_shape* shape, int64_t n_rows, const fedrag_rows* Q,
+                                const fedrag_paged_cache* cache, const int32_t* block_table, int64_t max_pages,
+                                const int32_t* q_start, const int32_t* kv_lens, int64_t max_q_len, int32_t causal,
+                                float softmax_scale, float* O, float* lse,
+                                void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace fedrag_paged_attn needs for these sizes; 0 for arguments it would reject.  Like the other size it
+ * depends on the compute units of the device that is current in the calling thread. */
+size_t fedrag_paged_attn_workspace_bytes(const fedrag_shape* shape, int64_t n_rows, int64_t max_pages,
+                                         int32_t page_tokens, int64_t max_q_len);
 
 /* inv_out[perm[j]] = j for j in [0, L): the gather array that undoes `perm`.  Device pointers. */
 fedrag_status fedrag_invert_perm(const int32_t* perm, int64_t L, int32_t* inv_out, void* stream);

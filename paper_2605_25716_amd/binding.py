@@ -28,9 +28,13 @@ EXPORTS = ("fedrag_scramble_kv", "fedrag_scramble_q", "fedrag_partial_attn", "fe
            "fedrag_scramble_kv_structured", "fedrag_scramble_q_structured", "fedrag_unscramble_structured",
            "fedrag_local_attn", "fedrag_unpermute_lse", "fedrag_partial_attn_varlen", "fedrag_quantize_rows",
            "fedrag_dequantize_rows", "fedrag_scramble_kv_quantized", "fedrag_scramble_kv_structured_quantized",
-           "fedrag_partial_attn_quantized", "fedrag_partial_attn_varlen_quantized", "fedrag_invert_perm",
+           "fedrag_partial_attn_quantized", "fedrag_partial_attn_varlen_quantized", "fedrag_paged_map",
+           "fedrag_paged_write", "fedrag_paged_attn", "fedrag_paged_attn_workspace_bytes", "fedrag_invert_perm",
            "fedrag_validate_perm", "fedrag_status_string",
            "fedrag_version")
+
+# what fedrag_paged_map's flags are the sum of
+MAP_NO_PAGES, MAP_NO_COLUMNS, MAP_NO_ROWS, MAP_BAD_LENGTH = 1, 2, 4, 8
 
 
 class Shape(ctypes.Structure):
@@ -42,6 +46,17 @@ class StructuredKey(ctypes.Structure):
     """fedrag_structured_key: host struct of four device pointers, [Hkv, d] each."""
     _fields_ = [("scale_in", ctypes.c_void_p), ("perm_in", ctypes.c_void_p), ("perm_out", ctypes.c_void_p),
                 ("scale_out", ctypes.c_void_p)]
+
+
+class PagedCache(ctypes.Structure):
+    """fedrag_paged_cache: host struct of two device pointers and the pages' sizes."""
+    _fields_ = [("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("n_pages", ctypes.c_int64), ("page_stride", ctypes.c_int64),
+                ("page_tokens", ctypes.c_int32)]
+
+
+class Rows(ctypes.Structure):
+    """fedrag_rows: host struct of a device pointer and two strides, in elements."""
+    _fields_ = [("data", ctypes.c_void_p), ("head_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64)]
 
 
 class FedragError(RuntimeError):
@@ -101,6 +116,13 @@ def load() -> ctypes.CDLL:
                                                       vp, ctypes.c_size_t, vp]
         lib.fedrag_partial_attn_varlen_quantized.argtypes = [sp, i64, i64, vp, vp, vp, vp, vp, i32, vp, vp,
                                                              ctypes.c_float, f32p, f32p, vp, ctypes.c_size_t, vp]
+        cp, rp = ctypes.POINTER(PagedCache), ctypes.POINTER(Rows)
+        lib.fedrag_paged_map.argtypes = [i32, i64, i32, i64, vp, vp, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+        lib.fedrag_paged_write.argtypes = [sp, i64, rp, rp, vp, cp, vp]
+        lib.fedrag_paged_attn.argtypes = [sp, i64, rp, cp, vp, i64, vp, vp, i64, i32, ctypes.c_float, f32p, f32p, vp,
+                                          ctypes.c_size_t, vp]
+        lib.fedrag_paged_attn_workspace_bytes.argtypes = [sp, i64, i64, i32, i64]
+        lib.fedrag_paged_attn_workspace_bytes.restype = ctypes.c_size_t
         lib.fedrag_invert_perm.argtypes = [vp, i64, vp, vp]
         lib.fedrag_validate_perm.argtypes = [vp, i32, i64, vp, vp, vp]
         lib.fedrag_status_string.argtypes = [ctypes.c_int]
@@ -113,7 +135,8 @@ def load() -> ctypes.CDLL:
                      "fedrag_unpermute_lse", "fedrag_partial_attn_varlen", "fedrag_quantize_rows",
                      "fedrag_dequantize_rows", "fedrag_scramble_kv_quantized",
                      "fedrag_scramble_kv_structured_quantized", "fedrag_partial_attn_quantized",
-                     "fedrag_partial_attn_varlen_quantized"):
+                     "fedrag_partial_attn_varlen_quantized", "fedrag_paged_map", "fedrag_paged_write",
+                     "fedrag_paged_attn"):
             getattr(lib, name).restype = ctypes.c_int
         _lib = lib
     return _lib
@@ -510,6 +533,141 @@ def fedrag_scramble_kv_quantized(K, V, phi_k, phi_v, perm_kv, bits: int, n_q_hea
                                                  _stream())
     _check(st, "fedrag_scramble_kv_quantized")
     return Kc, Kp, Vc, Vp
+
+
+# ------------------------------------------------------------------------------------------- the paged cache
+def _on(device, **tensors):
+    """The tensors of a paged call share a device, which is the current one: the call goes to its current stream."""
+    if device.type != "cuda":
+        raise ValueError("the library works on device memory: pass CUDA tensors")
+    if device.index != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on {device}, which is not the current device")
+    for name, t in tensors.items():
+        if t is not None and t.device != device:
+            raise ValueError(f"{name} is on {t.device}, the others are on {device}")
+
+
+def _typed(dtype, n, **tensors):
+    for name, t in tensors.items():
+        if t is not None and (t.dtype != dtype or t.numel() < n):
+            raise ValueError(f"{name}: {dtype} of at least {n} values, not {t.dtype} of {t.numel()}")
+
+
+def _of_shape(dtype, *shape, **tensors):
+    for name, t in tensors.items():
+        if t is not None and (t.dtype != dtype or tuple(t.shape) != shape):
+            raise ValueError(f"{name}: {dtype} of shape {list(shape)}, not {t.dtype} of {list(t.shape)}")
+
+
+def _rows(name, X) -> Rows:
+    """[H, T, d] or [1, H, T, d], any strides but the last: for rows kept [T, H, d] pass X.transpose(0, 1)."""
+    if X.dim() == 4 and X.shape[0] == 1:
+        X = X[0]
+    if X.dim() != 3:
+        raise ValueError(f"{name}: [H, T, d] or [1, H, T, d], not {list(X.shape)}")
+    if X.shape[2] > 1 and X.stride(2) != 1:
+        raise ValueError(f"{name}: the channels of a row have to lie side by side")
+    # (the stride of a dimension of one entry says nothing)
+    return Rows(X.data_ptr(), X.stride(0) if X.shape[0] > 1 else 0, X.stride(1) if X.shape[1] > 1 else 0)
+
+
+def _pages(K_pages, V_pages) -> PagedCache:
+    if K_pages.dim() != 4 or K_pages.shape != V_pages.shape or K_pages.dtype != V_pages.dtype or K_pages.stride() != V_pages.stride():
+        raise ValueError("K_pages and V_pages: [n_pages, Hkv, page_tokens, d], alike in shape, type and strides")
+    n, H, P, d = K_pages.shape
+    if any(size > 1 and K_pages.stride(i) != want for i, size, want in ((1, H, P * d), (2, P, d), (3, d, 1))):
+        raise ValueError("a page has to be dense: [Hkv, page_tokens, d] without gaps")
+    return PagedCache(K_pages.data_ptr(), V_pages.data_ptr(), n, K_pages.stride(0) if n > 1 else 0, P)
+
+
+def fedrag_paged_map(cached_lens, new_lens, block_table, free_pages, free_count, page_tokens: int, n_rows: int, q_start=None,
+                     kv_lens=None, slots=None, positions=None, free_left=None, flags=None):
+    """Plans a step over the paged cache from the requests' lengths: (q_start int32 [B+1], kv_lens int32 [B], slots int64
+    [n_rows], positions int32 [n_rows], free_left int32 [1], flags int32 [1]); new pages are taken from the top of the stack
+    free_pages[:free_count] and entered in block_table int32 [B, max_pages], in place.  kv_lens may be cached_lens and
+    free_left may be free_count: the state then advances in place.  flags: 0 or a sum of MAP_*."""
+    if block_table.dim() != 2:
+        raise ValueError("block_table: int32 [B, max_pages]")
+    (B, columns), n_rows, dev = block_table.shape, index(n_rows), block_table.device
+    if n_rows < 0:
+        raise ValueError("n_rows is not negative")
+    new = lambda n, dt=torch.int32: torch.empty(n, dtype=dt, device=dev)  # noqa: E731
+    q_start = new(B + 1) if q_start is None else q_start
+    kv_lens = new(B) if kv_lens is None else kv_lens
+    slots = new(n_rows, torch.int64) if slots is None else slots
+    positions = new(n_rows) if positions is None else positions
+    free_left = new(1) if free_left is None else free_left
+    flags = new(1) if flags is None else flags
+    _on(dev, cached_lens=cached_lens, new_lens=new_lens, free_pages=free_pages, free_count=free_count, q_start=q_start,
+        kv_lens=kv_lens, slots=slots, positions=positions, free_left=free_left, flags=flags)
+    _of_shape(torch.int32, B, cached_lens=cached_lens, new_lens=new_lens, kv_lens=kv_lens)
+    _of_shape(torch.int32, B, columns, block_table=block_table)
+    _typed(torch.int32, 0, free_pages=free_pages)
+    _typed(torch.int32, 1, free_count=free_count, free_left=free_left, flags=flags)
+    _typed(torch.int32, B + 1, q_start=q_start)
+    _typed(torch.int32, n_rows, positions=positions)
+    _typed(torch.int64, n_rows, slots=slots)
+    st = load().fedrag_paged_map(B, n_rows, index(page_tokens), columns, _ptr(cached_lens), _ptr(new_lens), _ptr(free_pages),
+                                 free_pages.numel(), _ptr(free_count), _ptr(block_table), _ptr(q_start), _ptr(kv_lens),
+                                 _ptr(slots), _ptr(positions), _ptr(free_left), _ptr(flags), _stream())
+    _check(st, "fedrag_paged_map")
+    return q_start, kv_lens, slots, positions, free_left, flags
+
+
+def fedrag_paged_write(K, V, slots, K_pages, V_pages):
+    """Rows K, V ([Hkv, T, d] or [1, Hkv, T, d], any strides) into the pages [n_pages, Hkv, page_tokens, d], row t to slots[t]
+    (int64 [T]); rows whose slot lies outside the pages are left out."""
+    dev = K_pages.device
+    _on(dev, K=K, V=V, slots=slots, V_pages=V_pages)
+    rk, rv, cache = _rows("K", K), _rows("V", V), _pages(K_pages, V_pages)
+    H, T, d = K.shape[-3:]
+    if V.shape[-3:] != K.shape[-3:] or (H, d) != (K_pages.shape[1], K_pages.shape[3]) or not K.dtype == V.dtype == K_pages.dtype:
+        raise ValueError("K, V [Hkv, T, d] and the pages [n_pages, Hkv, page_tokens, d] do not match")
+    _typed(torch.int64, T, slots=slots)
+    st = load().fedrag_paged_write(_shape_ref(1, H, H, d, K.dtype), T, ctypes.byref(rk), ctypes.byref(rv), _ptr(slots),
+                                   ctypes.byref(cache), _stream())
+    _check(st, "fedrag_paged_write")
+    return K_pages, V_pages
+
+
+def fedrag_paged_attn_workspace_bytes(batch, n_q_heads, n_kv_heads, d_head, dtype, n_rows, max_pages, page_tokens, max_q_len) -> int:
+    shape = _shape_ref_of_numbers(batch, n_q_heads, n_kv_heads, d_head, dtype)
+    return int(load().fedrag_paged_attn_workspace_bytes(shape, n_rows, max_pages, page_tokens, max_q_len))
+
+
+def fedrag_paged_attn(Q, K_pages, V_pages, block_table, q_start, kv_lens, max_q_len: int = 0, causal: bool = True,
+                      softmax_scale: Optional[float] = None, O_part=None, lse=None, workspace=None):
+    """A step's rows over the paged cache.  Q [Hq, T, d] or [1, Hq, T, d], any strides; request b's rows are
+    q_start[b] .. q_start[b+1]-1 and see its first kv_lens[b] tokens, causal: up to themselves.  -> fp32 [1, Hq, T, d],
+    fp32 [1, Hq, T]; rows behind the last request are not written.  max_q_len: the most rows of a request, 0 if not known
+    (speed only)."""
+    dev = K_pages.device
+    _on(dev, Q=Q, V_pages=V_pages, block_table=block_table, q_start=q_start, kv_lens=kv_lens, O_part=O_part, lse=lse,
+        workspace=workspace)
+    rq, cache = _rows("Q", Q), _pages(K_pages, V_pages)
+    Hq, T, d = Q.shape[-3:]
+    _, Hkv, P, dk = K_pages.shape
+    if d != dk or Q.dtype != K_pages.dtype:
+        raise ValueError("Q [Hq, T, d] and the pages [n_pages, Hkv, page_tokens, d] do not match")
+    if block_table.dim() != 2:
+        raise ValueError("block_table: int32 [B, max_pages]")
+    B, columns = block_table.shape
+    _of_shape(torch.int32, B, columns, block_table=block_table)
+    _of_shape(torch.int32, B, kv_lens=kv_lens)
+    _typed(torch.int32, B + 1, q_start=q_start)
+    if softmax_scale is None:
+        softmax_scale = float(d) ** -0.5
+    O_part = torch.empty((1, Hq, T, d), dtype=torch.float32, device=dev) if O_part is None else O_part
+    lse = torch.empty((1, Hq, T), dtype=torch.float32, device=dev) if lse is None else lse
+    _typed(torch.float32, Hq * T * d, O_part=O_part)
+    _typed(torch.float32, Hq * T, lse=lse)
+    shape, max_q_len = _shape_ref(B, Hq, Hkv, d, Q.dtype), index(max_q_len)
+    workspace, ws_bytes = _workspace(workspace, Q, "fedrag_paged_attn_workspace_bytes", shape, T, columns, P, max_q_len)
+    st = load().fedrag_paged_attn(shape, T, ctypes.byref(rq), ctypes.byref(cache), _ptr(block_table), columns, _ptr(q_start),
+                                  _ptr(kv_lens), max_q_len, 1 if causal else 0, softmax_scale, _ptr(O_part), _ptr(lse),
+                                  _ptr(workspace), ws_bytes, _stream())
+    _check(st, "fedrag_paged_attn")
+    return O_part, lse
 
 
 def fedrag_invert_perm(perm, inv_out=None):

@@ -56,6 +56,71 @@ void set_key(RowsJob& j, int i, const fedrag_structured_key* k) {
     j.s_out[i] = k->scale_out;
 }
 
+// ---- the paged cache.  Byte extents are kept below 2^62, so that sums and differences of addresses stay in 64 bits.
+constexpr int64_t kMostBytes = (int64_t)1 << 62;
+
+bool mul_fits(int64_t a, int64_t b, int64_t* out) {
+    if (a < 0 || b < 0 || (b != 0 && a > kMostBytes / b)) return false;
+    *out = a * b;
+    return true;
+}
+
+// Rows with strides: FEDRAG_OK and their extent in bytes.
+fedrag_status check_rows(const fedrag_rows* r, int64_t n_rows, int32_t heads, const fedrag_shape* s, size_t* extent) {
+    if (!r || !r->data) return FEDRAG_ERR_NULL;
+    const int64_t e = (int64_t)elem_size(s->dtype);
+    int64_t a, b;
+    if (r->head_stride < 0 || r->token_stride < 0) return FEDRAG_ERR_SHAPE;
+    if (r->head_stride > kMostBytes / e || r->token_stride > kMostBytes / e) return FEDRAG_ERR_SHAPE;
+    if (!mul_fits(heads - 1, r->head_stride * e, &a) || !mul_fits(n_rows - 1, r->token_stride * e, &b) || a > kMostBytes / 2 ||
+        b > kMostBytes / 2)
+        return FEDRAG_ERR_SHAPE;
+    if (!aligned16(r->data) || (r->head_stride * e) % 16 != 0 || (r->token_stride * e) % 16 != 0) return FEDRAG_ERR_ALIAS;
+    *extent = (size_t)(a + b) + (size_t)(s->d_head * e);
+    return FEDRAG_OK;
+}
+
+bool page_tokens_ok(int32_t n) { return n == 16 || n == 32 || n == 64 || n == 128 || n == 256; }
+
+// The cache's numbers; its pointers are looked at only if it has pages.
+fedrag_status check_cache(const fedrag_paged_cache* c, const fedrag_shape* s, Pages* out, size_t* extent, size_t* block) {
+    if (!c) return FEDRAG_ERR_NULL;
+    if (!page_tokens_ok(c->page_tokens)) return FEDRAG_ERR_UNSUPPORTED;
+    if (c->n_pages < 0 || c->n_pages > INT32_MAX || c->page_stride < 0) return FEDRAG_ERR_SHAPE;
+    const int64_t e = (int64_t)elem_size(s->dtype);
+    const int64_t dense = (int64_t)s->n_kv_heads * c->page_tokens * s->d_head;
+    const int64_t stride = c->page_stride ? c->page_stride : dense;
+    int64_t all;
+    if (stride < dense || stride > kMostBytes / e || !mul_fits(c->n_pages, stride * e, &all)) return FEDRAG_ERR_SHAPE;
+    if ((stride * e) % 16 != 0) return FEDRAG_ERR_ALIAS;
+    if (c->n_pages > 0) {
+        if (!c->K || !c->V) return FEDRAG_ERR_NULL;
+        if (!aligned16(c->K) || !aligned16(c->V)) return FEDRAG_ERR_ALIAS;
+    }
+    out->K = (const char*)c->K;
+    out->V = (const char*)c->V;
+    out->n_pages = (uint32_t)c->n_pages;
+    out->shift = __builtin_ctz((unsigned)c->page_tokens);
+    out->page_bytes = stride * e;
+    *block = (size_t)(dense * e);
+    *extent = c->n_pages > 0 ? (size_t)all - (size_t)(stride * e) + *block : 0;
+    return FEDRAG_OK;
+}
+
+// K's pages and V's share bytes.  (They may take turns in one tensor: then their distance, modulo a page's stride, leaves
+// room for a page on either side.)
+bool pages_overlap(const Pages& p, size_t extent, size_t block) {
+    if (!overlaps(p.K, extent, p.V, extent)) return false;
+    const uintptr_t k = reinterpret_cast<uintptr_t>(p.K), v = reinterpret_cast<uintptr_t>(p.V);
+    const size_t d = (size_t)((k < v ? v - k : k - v) % (uintptr_t)p.page_bytes);
+    return d < block || (size_t)p.page_bytes - d < block;
+}
+
+fedrag_status check_paged_sizes(int64_t n_rows, int64_t max_pages, int64_t max_q_len) {
+    return n_rows < 0 || n_rows > INT32_MAX || max_pages < 0 || max_pages > INT32_MAX || max_q_len < 0 ? FEDRAG_ERR_SHAPE
+                                                                                                        : FEDRAG_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -704,12 +769,149 @@ fedrag_status fedrag_validate_perm(const int32_t* perm, int32_t n_perm, int64_t 
     return dev(launch_validate_perm(perm, n_perm, L, marks, flag_out, (hipStream_t)stream));
 }
 
+fedrag_status fedrag_paged_map(int32_t batch, int64_t n_rows, int32_t page_tokens, int64_t max_pages,
+                               const int32_t* cached_lens, const int32_t* new_lens, const int32_t* free_pages, int64_t n_free,
+                               const int32_t* free_count, int32_t* block_table, int32_t* q_start, int32_t* kv_lens, int64_t* slots,
+                               int32_t* positions, int32_t* free_left, int32_t* flags, void* stream) {
+    if (batch < 0 || n_free < 0 || n_free > INT32_MAX) return FEDRAG_ERR_SHAPE;
+    fedrag_status st = check_paged_sizes(n_rows, max_pages, 0);
+    if (st != FEDRAG_OK) return st;
+    if (!page_tokens_ok(page_tokens)) return FEDRAG_ERR_UNSUPPORTED;
+    if (!free_count || !q_start || !free_left || !flags || (batch > 0 && (!cached_lens || !new_lens || !kv_lens)) ||
+        (n_free > 0 && !free_pages) || (batch > 0 && max_pages > 0 && !block_table) || (n_rows > 0 && !slots))
+        return FEDRAG_ERR_NULL;
+    int64_t table_bytes;
+    if (!mul_fits((int64_t)batch * 4, max_pages, &table_bytes)) return FEDRAG_ERR_SHAPE;
+    const uintptr_t words = reinterpret_cast<uintptr_t>(cached_lens) | reinterpret_cast<uintptr_t>(new_lens) |
+                            reinterpret_cast<uintptr_t>(free_pages) | reinterpret_cast<uintptr_t>(free_count) |
+                            reinterpret_cast<uintptr_t>(block_table) | reinterpret_cast<uintptr_t>(q_start) |
+                            reinterpret_cast<uintptr_t>(kv_lens) | reinterpret_cast<uintptr_t>(positions) |
+                            reinterpret_cast<uintptr_t>(free_left) | reinterpret_cast<uintptr_t>(flags);
+    if ((words & 3u) || (reinterpret_cast<uintptr_t>(slots) & 7u)) return FEDRAG_ERR_ALIAS;
+    const size_t nb = (size_t)batch * 4, nr = (size_t)n_rows;
+    const struct { const void* p; size_t n; } in[] = {{cached_lens, nb}, {new_lens, nb}, {free_pages, (size_t)n_free * 4}, {free_count, 4}},
+        out[] = {{block_table, (size_t)table_bytes}, {q_start, nb + 4}, {kv_lens, nb}, {slots, nr * 8}, {positions, nr * 4}, {free_left, 4}, {flags, 4}};
+    for (const auto& o : out) {
+        for (const auto& i : in) {
+            const bool in_place = (o.p == kv_lens && i.p == cached_lens) || (o.p == free_left && i.p == free_count);
+            if (!(in_place && o.p == i.p) && overlaps(o.p, o.n, i.p, i.n)) return FEDRAG_ERR_ALIAS;
+        }
+        for (const auto& other : out)
+            if (&other != &o && overlaps(o.p, o.n, other.p, other.n)) return FEDRAG_ERR_ALIAS;
+    }
+    return dev(launch_paged_map(PagedMapJob{batch, n_rows, max_pages, n_free, page_tokens, cached_lens, new_lens, free_pages, free_count,
+                                            block_table, q_start, kv_lens, positions, free_left, flags, slots},
+                                (hipStream_t)stream));
+}
+
+fedrag_status fedrag_paged_write(const fedrag_shape* shape, int64_t n_rows, const fedrag_rows* K_rows, const fedrag_rows* V_rows,
+                                 const int64_t* slots, const fedrag_paged_cache* cache, void* stream) {
+    fedrag_status st = check_shape(shape, true);
+    if (st == FEDRAG_OK) st = check_paged_sizes(n_rows, 0, 0);
+    if (st != FEDRAG_OK) return st;
+    PagedWriteJob j{};
+    size_t extent, block, kb, vb;
+    st = check_cache(cache, shape, &j.pages, &extent, &block);
+    if (st != FEDRAG_OK) return st;
+    if (n_rows == 0 || cache->n_pages == 0) return FEDRAG_OK;  // nothing to write, or nowhere
+    st = check_rows(K_rows, n_rows, shape->n_kv_heads, shape, &kb);
+    if (st == FEDRAG_OK) st = check_rows(V_rows, n_rows, shape->n_kv_heads, shape, &vb);
+    if (st != FEDRAG_OK) return st;
+    if (!slots) return FEDRAG_ERR_NULL;
+    if (reinterpret_cast<uintptr_t>(slots) & 7u) return FEDRAG_ERR_ALIAS;
+    const size_t sb = (size_t)n_rows * 8;
+    for (const char* pages : {j.pages.K, j.pages.V})
+        if (overlaps(pages, extent, K_rows->data, kb) || overlaps(pages, extent, V_rows->data, vb) || overlaps(pages, extent, slots, sb))
+            return FEDRAG_ERR_ALIAS;
+    if (pages_overlap(j.pages, extent, block)) return FEDRAG_ERR_ALIAS;
+    const int64_t e = (int64_t)elem_size(shape->dtype);
+    const fedrag_rows* rows[2] = {K_rows, V_rows};
+    for (int i = 0; i < 2; ++i) {
+        j.rows[i] = rows[i]->data;
+        j.head_stride[i] = rows[i]->head_stride * e;
+        j.token_stride[i] = rows[i]->token_stride * e;
+    }
+    j.slots = slots;
+    j.n_rows = n_rows;
+    j.H = shape->n_kv_heads;
+    j.D = shape->d_head;
+    j.elem_bytes = (int)e;
+    return dev(launch_paged_write(j, (hipStream_t)stream));
+}
+
+size_t fedrag_paged_attn_workspace_bytes(const fedrag_shape* shape, int64_t n_rows, int64_t max_pages, int32_t page_tokens,
+                                         int64_t max_q_len) {
+    if (check_shape(shape, true) != FEDRAG_OK || check_paged_sizes(n_rows, max_pages, max_q_len) != FEDRAG_OK ||
+        !page_tokens_ok(page_tokens))
+        return 0;
+    return paged_attn_workspace_bytes(shape->batch, shape->n_q_heads, shape->n_kv_heads, shape->d_head, shape->dtype, n_rows, max_pages,
+                                      page_tokens, max_q_len);
+}
+
+fedrag_status fedrag_paged_attn(const fedrag_shape* shape, int64_t n_rows, const fedrag_rows* Q, const fedrag_paged_cache* cache,
+                                const int32_t* block_table, int64_t max_pages, const int32_t* q_start, const int32_t* kv_lens,
+                                int64_t max_q_len, int32_t causal, float softmax_scale, float* O, float* lse, void* workspace,
+                                size_t workspace_bytes, void* stream) {
+    fedrag_status st = check_shape(shape, true);
+    if (st == FEDRAG_OK) st = check_paged_sizes(n_rows, max_pages, max_q_len);
+    if (st != FEDRAG_OK) return st;
+    PagedAttnProblem p{};
+    size_t extent, block, qb;
+    st = check_cache(cache, shape, &p.pages, &extent, &block);
+    if (st != FEDRAG_OK) return st;
+    if (n_rows == 0 || shape->batch == 0) return FEDRAG_OK;  // no rows: nothing to do, tensor pointers may be NULL
+    if (!(softmax_scale > 0.0f) || softmax_scale - softmax_scale != 0.0f) return FEDRAG_ERR_SHAPE;  // finite, > 0
+    st = check_rows(Q, n_rows, shape->n_q_heads, shape, &qb);
+    if (st != FEDRAG_OK) return st;
+    if (!O || !lse || !q_start || !kv_lens || (max_pages > 0 && !block_table)) return FEDRAG_ERR_NULL;
+    int64_t n, rows, table;
+    if (!tensor_elems(1, shape->n_q_heads, n_rows, shape->d_head, &n) || !mul_fits(shape->n_q_heads, n_rows, &rows) ||
+        !mul_fits((int64_t)shape->batch * 4, max_pages, &table))
+        return FEDRAG_ERR_SHAPE;
+    const uintptr_t words = reinterpret_cast<uintptr_t>(block_table) | reinterpret_cast<uintptr_t>(q_start) |
+                            reinterpret_cast<uintptr_t>(kv_lens) | reinterpret_cast<uintptr_t>(lse);
+    if (!aligned16(O) || (words & 3u) || !aligned16(workspace)) return FEDRAG_ERR_ALIAS;
+    const size_t need = paged_attn_workspace_bytes(shape->batch, shape->n_q_heads, shape->n_kv_heads, shape->d_head, shape->dtype, n_rows,
+                                                   max_pages, cache->page_tokens, max_q_len);
+    if (need > 0 && (!workspace || workspace_bytes < need)) return FEDRAG_ERR_WORKSPACE;
+    const struct { const void* p; size_t n; } in[] = {{Q->data, qb}, {p.pages.K, extent}, {p.pages.V, extent}, {block_table, (size_t)table},
+                                                      {q_start, ((size_t)shape->batch + 1) * 4}, {kv_lens, (size_t)shape->batch * 4}},
+        out[] = {{O, (size_t)n * 4}, {lse, (size_t)rows * 4}, {workspace, need}};
+    for (const auto& o : out) {
+        for (const auto& i : in)
+            if (overlaps(o.p, o.n, i.p, i.n)) return FEDRAG_ERR_ALIAS;
+        for (const auto& other : out)
+            if (&other != &o && overlaps(o.p, o.n, other.p, other.n)) return FEDRAG_ERR_ALIAS;
+    }
+    const int64_t e = (int64_t)elem_size(shape->dtype);
+    p.B = shape->batch;
+    p.Hq = shape->n_q_heads;
+    p.Hkv = shape->n_kv_heads;
+    p.D = shape->d_head;
+    p.dtype = shape->dtype;
+    p.T = n_rows;
+    p.Q = (const char*)Q->data;
+    p.q_head_stride = Q->head_stride * e;
+    p.q_token_stride = Q->token_stride * e;
+    p.table = block_table;
+    p.max_pages = max_pages;
+    p.q_start = q_start;
+    p.kv_lens = kv_lens;
+    p.max_q_len = max_q_len;
+    p.causal = causal != 0;
+    p.scale = softmax_scale;
+    p.O = O;
+    p.lse = lse;
+    p.workspace = workspace;
+    return dev(launch_paged_attn(p, (hipStream_t)stream));
+}
+
 const char* fedrag_status_string(fedrag_status status) {
     switch (status) {
         case FEDRAG_OK: return "ok";
         case FEDRAG_ERR_NULL: return "a required pointer is NULL";
         case FEDRAG_ERR_SHAPE: return "invalid shape or size argument";
-        case FEDRAG_ERR_UNSUPPORTED: return "unsupported d_head or dtype";
+        case FEDRAG_ERR_UNSUPPORTED: return "unsupported d_head, dtype or page size";
         case FEDRAG_ERR_WORKSPACE: return "workspace missing or too small";
         case FEDRAG_ERR_ALIAS: return "output overlaps an input, or a pointer is misaligned";
         case FEDRAG_ERR_DEVICE: return "HIP launch failed";

@@ -225,4 +225,53 @@ struct CodecJob {
 };
 hipError_t launch_codec(const CodecJob& job, hipStream_t stream);
 
+// Bookkeeping of a step over the paged cache (fedrag_paged_map); all pointers are device memory.
+struct PagedMapJob {
+    int batch;
+    int64_t n_rows, max_pages, n_free;
+    int page_tokens;
+    const int32_t *cached_lens, *new_lens, *free_pages, *free_count;
+    int32_t *block_table, *q_start, *kv_lens, *positions, *free_left, *flags;
+    int64_t* slots;
+};
+hipError_t launch_paged_map(const PagedMapJob& job, hipStream_t stream);
+
+// The pages as the kernels see them.
+struct Pages {
+    const char* K;
+    const char* V;
+    uint32_t n_pages;
+    int shift;             // log2(page_tokens)
+    int64_t page_bytes;    // from a page to the next
+};
+struct PagedWriteJob {
+    const void* rows[2];   // K, V
+    int64_t head_stride[2], token_stride[2];  // bytes
+    const int64_t* slots;
+    Pages pages;
+    int64_t n_rows;
+    int H, D, elem_bytes;
+};
+hipError_t launch_paged_write(const PagedWriteJob& job, hipStream_t stream);
+
+// Attention of a ragged step over the pages (fedrag_paged_attn).
+struct PagedAttnProblem {
+    int B, Hq, Hkv, D, dtype;
+    int64_t T;               // rows of all requests
+    const char* Q;
+    int64_t q_head_stride, q_token_stride;  // bytes
+    Pages pages;
+    const int32_t* table;    // [B, max_pages]
+    int64_t max_pages;
+    const int32_t *q_start, *kv_lens;
+    int64_t max_q_len;       // 0: not known
+    bool causal;
+    float scale;
+    float *O, *lse;
+    void* workspace;
+};
+hipError_t launch_paged_attn(const PagedAttnProblem& p, hipStream_t stream);
+size_t paged_attn_workspace_bytes(int B, int Hq, int Hkv, int D, int dtype, int64_t T, int64_t max_pages, int page_tokens,
+                                  int64_t max_q_len);
+
 }  // namespace fedrag

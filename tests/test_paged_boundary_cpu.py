@@ -1,0 +1,170 @@
+"""What the paged calls refuse, on the host, before anything is launched (made-up addresses are safe: every call fails)."""
+import ctypes
+import os
+import subprocess
+
+import pytest
+import torch
+
+from paper_2605_25716_amd import binding as fb
+from paper_2605_25716_amd import build as fbuild
+
+A = 1 << 32  # far apart, so that only what a test moves together overlaps
+
+
+@pytest.fixture(scope="module")
+def lib():
+    fbuild.build_library(force=False)
+    return fb.load()
+
+
+def P(x):
+    return None if x is None else ctypes.c_void_p(x)
+
+
+def shape(B=2, Hq=8, Hkv=2, d=128, dt=fb.BF16):
+    return ctypes.byref(fb.Shape(B, Hq, Hkv, d, dt))
+
+
+MAP = dict(batch=2, n_rows=40, page=16, columns=4, cached=A, new=2 * A, free=3 * A, n_free=9, count=4 * A, table=5 * A, q_start=6 * A,
+           kv=7 * A, slots=8 * A, positions=9 * A, left=10 * A, flags=11 * A)
+
+
+def map_call(lib, **kw):
+    a = {**MAP, **kw}
+    return lib.fedrag_paged_map(a["batch"], a["n_rows"], a["page"], a["columns"], P(a["cached"]), P(a["new"]), P(a["free"]), a["n_free"],
+                                P(a["count"]), P(a["table"]), P(a["q_start"]), P(a["kv"]), P(a["slots"]), P(a["positions"]), P(a["left"]),
+                                P(a["flags"]), None)
+
+
+def test_map_refusals(lib):
+    for k in ("cached", "new", "free", "count", "table", "q_start", "kv", "slots", "left", "flags"):
+        assert map_call(lib, **{k: None}) == fb.ERR_NULL, k
+    for k in ("cached", "new", "free", "count", "table", "q_start", "kv", "positions", "left", "flags"):
+        assert map_call(lib, **{k: MAP[k] + 2}) == fb.ERR_ALIAS, k
+    assert map_call(lib, slots=MAP["slots"] + 4) == fb.ERR_ALIAS
+    for k, v in (("batch", -1), ("n_rows", -1), ("n_rows", 1 << 31), ("columns", -1), ("columns", 1 << 31), ("n_free", -1), ("n_free", 1 << 31)):
+        assert map_call(lib, **{k: v}) == fb.ERR_SHAPE, (k, v)
+    for page in (0, 8, 24, 48, 512, -16):
+        assert map_call(lib, page=page) == fb.ERR_UNSUPPORTED
+    # what is written overlaps nothing but what it may be
+    outs = ("table", "q_start", "kv", "slots", "positions", "left", "flags")
+    for o in outs:
+        for other in ("cached", "new", "free", "count") + outs:
+            if o != other and (o, other) not in (("kv", "cached"), ("left", "count")):
+                assert map_call(lib, **{o: MAP[other]}) == fb.ERR_ALIAS, (o, other)
+    assert map_call(lib, kv=MAP["cached"] + 4) == fb.ERR_ALIAS  # in place, but shifted
+    assert map_call(lib, batch=3, cached=A, new=A + 4, kv=A + 8) == fb.ERR_ALIAS
+
+
+ATTN = dict(shape=None, n_rows=40, Q=A, hs=128, ts=1024, K=2 * A, V=3 * A, n_pages=10, ps=0, page=16, table=4 * A, columns=4, q_start=5 * A,
+            kv=6 * A, max_q=8, causal=1, scale=0.1, O=7 * A, lse=8 * A, ws=9 * A, ws_bytes=1 << 31)
+
+
+def attn_call(lib, **kw):
+    a = {**ATTN, **kw}
+    rows = fb.Rows(a["Q"], a["hs"], a["ts"])
+    cache = fb.PagedCache(a["K"], a["V"], a["n_pages"], a["ps"], a["page"])
+    return lib.fedrag_paged_attn(a["shape"] or shape(), a["n_rows"], None if a["Q"] == "none" else ctypes.byref(rows),
+                                 None if a["K"] == "none" else ctypes.byref(cache), P(a["table"]), a["columns"], P(a["q_start"]), P(a["kv"]),
+                                 a["max_q"], a["causal"], a["scale"], P(a["O"]), P(a["lse"]), P(a["ws"]), a["ws_bytes"], None)
+
+
+def test_attn_refusals(lib):
+    for k in ("Q", "K", "V", "table", "q_start", "kv", "O", "lse"):
+        assert attn_call(lib, **{k: None}) == fb.ERR_NULL, k
+    assert lib.fedrag_paged_attn(shape(), 4, None, None, None, 0, None, None, 0, 0, 0.1, None, None, None, 0, None) == fb.ERR_NULL
+    assert lib.fedrag_paged_attn(None, 4, None, None, None, 0, None, None, 0, 0, 0.1, None, None, None, 0, None) == fb.ERR_NULL
+    for k, v in (("n_rows", -1), ("n_rows", 1 << 31), ("columns", -1), ("columns", 1 << 31), ("max_q", -1), ("n_pages", -1),
+                 ("n_pages", 1 << 31), ("ps", -8), ("ps", 16 * 128 * 2 - 8), ("hs", -8), ("ts", -8), ("hs", 1 << 62), ("ts", 1 << 62),
+                 ("scale", 0.0), ("scale", -1.0), ("scale", float("inf")), ("scale", float("nan"))):
+        assert attn_call(lib, **{k: v}) == fb.ERR_SHAPE, (k, v)
+    for page in (0, 8, 17, 48, 512):
+        assert attn_call(lib, page=page) == fb.ERR_UNSUPPORTED
+    assert attn_call(lib, shape=shape(d=96)) == fb.ERR_UNSUPPORTED
+    assert attn_call(lib, shape=shape(dt=5)) == fb.ERR_UNSUPPORTED
+    assert attn_call(lib, shape=shape(Hq=7)) == fb.ERR_SHAPE
+    assert attn_call(lib, shape=shape(B=-1)) == fb.ERR_SHAPE
+    for k in ("Q", "K", "V", "O", "ws"):
+        assert attn_call(lib, **{k: ATTN[k] + 8}) == fb.ERR_ALIAS, k
+    for k in ("table", "q_start", "kv", "lse"):
+        assert attn_call(lib, **{k: ATTN[k] + 2}) == fb.ERR_ALIAS, k
+    for k, v in (("hs", 4), ("ts", 1020), ("ps", 16 * 128 * 2 + 4)):
+        assert attn_call(lib, **{k: v}) == fb.ERR_ALIAS, k
+    for k in ("Q", "K", "V", "table", "q_start", "kv", "lse"):
+        assert attn_call(lib, O=ATTN[k]) == fb.ERR_ALIAS, k
+        if k != "lse":
+            assert attn_call(lib, lse=ATTN[k]) == fb.ERR_ALIAS, k
+    # nothing to do: no rows, or no requests
+    assert attn_call(lib, n_rows=0, Q=None, O=None, lse=None, q_start=None, kv=None) == fb.OK
+    assert attn_call(lib, shape=shape(B=0), Q=None, O=None, lse=None, q_start=None, kv=None) == fb.OK
+
+
+def test_attn_workspace(lib):
+    big = dict(shape=shape(B=2, Hq=32, Hkv=8), n_rows=2, columns=4096, hs=128, ts=4096, max_q=1)
+    need = lib.fedrag_paged_attn_workspace_bytes(big["shape"], 2, 4096, 16, 1)
+    if need:
+        assert attn_call(lib, **big, ws=None) == fb.ERR_WORKSPACE
+        assert attn_call(lib, **big, ws_bytes=need - 1) == fb.ERR_WORKSPACE
+        for k in ("Q", "K", "V", "table", "q_start", "kv", "O", "lse"):
+            assert attn_call(lib, **big, ws=ATTN[k]) == fb.ERR_ALIAS, k
+    for bad in ((shape(d=96), 2, 4, 16, 1), (shape(), -1, 4, 16, 1), (shape(), 2, -4, 16, 1), (shape(), 2, 4, 24, 1), (shape(), 2, 4, 16, -1),
+                (None, 2, 4, 16, 1)):
+        assert lib.fedrag_paged_attn_workspace_bytes(*bad) == 0
+
+
+WRITE = dict(shape=None, n_rows=40, K=A, V=2 * A, hs=128, ts=1024, slots=3 * A, Kp=4 * A, Vp=5 * A, n_pages=10, ps=0, page=16)
+
+
+def write_call(lib, **kw):
+    a = {**WRITE, **kw}
+    k, v = fb.Rows(a["K"], a["hs"], a["ts"]), fb.Rows(a["V"], 128, 1024)
+    cache = fb.PagedCache(a["Kp"], a["Vp"], a["n_pages"], a["ps"], a["page"])
+    return lib.fedrag_paged_write(a["shape"] or shape(), a["n_rows"], ctypes.byref(k), ctypes.byref(v), P(a["slots"]), ctypes.byref(cache), None)
+
+
+def test_write_refusals(lib):
+    for k in ("K", "V", "slots", "Kp", "Vp"):
+        assert write_call(lib, **{k: None}) == fb.ERR_NULL, k
+    assert lib.fedrag_paged_write(shape(), 4, None, None, P(A), None, None) == fb.ERR_NULL
+    for k, v in (("n_rows", -1), ("n_rows", 1 << 31), ("n_pages", -1), ("hs", -8), ("ts", -8), ("ps", 8), ("ts", 1 << 62)):
+        assert write_call(lib, **{k: v}) == fb.ERR_SHAPE, (k, v)
+    for k in ("K", "V", "Kp", "Vp"):
+        assert write_call(lib, **{k: WRITE[k] + 8}) == fb.ERR_ALIAS, k
+    assert write_call(lib, slots=WRITE["slots"] + 4) == fb.ERR_ALIAS
+    assert write_call(lib, hs=132) == fb.ERR_ALIAS
+    for k in ("K", "V", "slots"):
+        assert write_call(lib, Kp=WRITE[k]) == fb.ERR_ALIAS
+        assert write_call(lib, Vp=WRITE[k]) == fb.ERR_ALIAS
+    assert write_call(lib, Vp=WRITE["Kp"]) == fb.ERR_ALIAS
+    block = 2 * 16 * 128 * 2  # bytes
+    assert write_call(lib, Vp=WRITE["Kp"] + block, ps=2 * block // 2 - 8) == fb.ERR_ALIAS  # a page of V begins where one of K ends, the next too early
+    assert write_call(lib, Vp=WRITE["Kp"] + block, ps=0) == fb.ERR_ALIAS
+    assert write_call(lib, n_rows=0, K=None, V=None, slots=None) == fb.OK
+    assert write_call(lib, n_pages=0, Kp=None, Vp=None) == fb.OK
+
+
+def test_binding_refuses_host_tensors():
+    z = torch.zeros
+    with pytest.raises(ValueError):
+        fb.fedrag_paged_map(z(1, dtype=torch.int32), z(1, dtype=torch.int32), z((1, 2), dtype=torch.int32), z(4, dtype=torch.int32),
+                            z(1, dtype=torch.int32), 16, 4)
+    with pytest.raises(ValueError):
+        fb.fedrag_paged_write(z(2, 3, 64), z(2, 3, 64), z(3, dtype=torch.int64), z(4, 2, 16, 64), z(4, 2, 16, 64))
+    with pytest.raises(ValueError):
+        fb.fedrag_paged_attn(z(2, 3, 64), z(4, 2, 16, 64), z(4, 2, 16, 64), z((1, 2), dtype=torch.int32), z(2, dtype=torch.int32),
+                             z(1, dtype=torch.int32))
+
+
+def test_structs_match_the_header(tmp_path):
+    """The binding's structs have the header's sizes and offsets."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    src = tmp_path / "sizes.c"
+    src.write_text('#include <stdio.h>\n#include "fedrag.h"\nint main(void) { printf("%zu %zu %zu %zu %zu\\n", sizeof(fedrag_paged_cache), '
+                   'offsetof(fedrag_paged_cache, page_stride), offsetof(fedrag_paged_cache, page_tokens), sizeof(fedrag_rows), '
+                   'offsetof(fedrag_rows, token_stride)); return 0; }\n')
+    exe = str(tmp_path / "sizes")
+    subprocess.run(["gcc", "-std=c99", "-I", os.path.join(root, "include"), str(src), "-o", exe], check=True)
+    got = [int(x) for x in subprocess.run([exe], capture_output=True, text=True, check=True).stdout.split()]
+    assert got == [ctypes.sizeof(fb.PagedCache), fb.PagedCache.page_stride.offset, fb.PagedCache.page_tokens.offset, ctypes.sizeof(fb.Rows),
+                   fb.Rows.token_stride.offset]
