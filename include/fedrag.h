@@ -435,7 +435,8 @@ fedrag_status fedrag_paged_write(const fedrag_shape* shape, int64_t n_rows, cons
  * with n_q_heads / n_kv_heads query heads to a KV head; a row that sees nothing has O = 0, lse = -inf.
  * Q : n_rows rows of n_q_heads heads with strides;  O : fp32 [n_q_heads, n_rows, d], lse : fp32 [n_q_heads, n_rows],
  * dense; padding rows of both keep what they held.
- * block_table : int32 [batch, max_pages];  q_start : int32 [batch + 1], not decreasing;  kv_lens : int32 [batch].
+ * block_table : int32 [batch, max_pages], max_pages * page_tokens <= INT32_MAX - 255;  q_start : int32 [batch + 1], not
+ * decreasing;  kv_lens : int32 [batch].
  * Values of q_start outside [0, n_rows] are taken as the nearer bound, kv_lens below 0 as 0.
  * max_q_len : the most rows that a request is expected to have, 0 = not known.  It decides which kernels are launched,
  * never the result: requests with more rows are attended to all the same, only more slowly.

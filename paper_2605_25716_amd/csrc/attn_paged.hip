@@ -1,13 +1,12 @@
 // Attention of a ragged step over a paged cache (fedrag_paged_attn).
-#include "fedrag_device.h"
-#include "fedrag_host.h"
+#include "attn_paged.h"
 
 namespace fedrag {
 
 // The plainest form: one wave per row and query head, 64 keys at a time.  Lane = key in the first product, = D / 64 channels in
 // the second; running maximum and sum.
 template <class E, int D>
-FEDRAG_KERNEL __launch_bounds__(64) void paged_attn_rows_kernel(PagedAttnProblem p, int n_tokens) {
+FEDRAG_KERNEL __launch_bounds__(64) void paged_attn_rows_kernel(PagedAttnProblem p, int n_tokens, int few) {
     constexpr int DC = D / 64;
     __shared__ float q[D];
     const int lane = threadIdx.x;
@@ -21,7 +20,7 @@ FEDRAG_KERNEL __launch_bounds__(64) void paged_attn_rows_kernel(PagedAttnProblem
         else hi = mid - 1;
     }
     const int64_t begin = p.q_start[lo], end = p.q_start[lo + 1];
-    if (t < begin || t >= end) return;
+    if (t < begin || t >= end || (end - begin) * (p.Hq / p.Hkv) < few) return;
     int64_t L = p.kv_lens[lo] < 0 ? 0 : p.kv_lens[lo];
     if (p.causal) {
         L = L - (end - begin) + (t - begin) + 1;
@@ -72,15 +71,168 @@ FEDRAG_KERNEL __launch_bounds__(64) void paged_attn_rows_kernel(PagedAttnProblem
     if (lane == 0) p.lse[(int64_t)h * p.T + t] = l > 0.f || l != l ? m + logf(l) : -INFINITY;
 }
 
-size_t paged_attn_workspace_bytes(int, int, int, int, int, int64_t, int64_t, int, int64_t) { return 0; }
+// The aggregation (Section 4.1) of the tiles whose keys were cut into runs: a workgroup takes 8 or 16 rows of one of them, a
+// thread 4 columns of a row.  The lanes of a row share out the weights, 16 runs at a time.
+constexpr int kPagedMergeThreads = 256;
+template <int D>
+FEDRAG_KERNEL __launch_bounds__(kPagedMergeThreads) void paged_merge_kernel(const PagedArgs a) {
+    constexpr int TPR = D / 4;
+    const PagedPiece p = paged_piece<true>(a, blockIdx.x);
+    if (p.b < 0 || p.slot + (uint32_t)p.runs * (uint32_t)a.Hkv > a.slots) return;  // (the latter where q_start decreases)
+    const int row0 = p.tile * a.cut.tile, n = blockIdx.y * (kPagedMergeThreads / TPR) + threadIdx.x / TPR;
+    const int c = threadIdx.x % TPR, k = c % 16, group = threadIdx.x % kWave & 48;
+    const int last = (row0 + a.cut.tile < p.req.R ? row0 + a.cut.tile : p.req.R) - 1;
+    if (row0 + n > last) return;
+    // runs that hold keys which some row of the tile sees
+    const int64_t run_keys = (int64_t)p.per << a.cut.unit_shift;
+    const int64_t seen = paged_limit(a, p.req, last);
+    const int S = seen > 0 ? (int)((seen + run_keys - 1) / run_keys) : 1;
+    const float* lp = a.part_lse + (int64_t)p.slot * a.cut.tile + n;
+    const float* op = a.part_O + ((int64_t)p.slot * a.cut.tile + n) * D + c * 4;
+    const int64_t step = (int64_t)a.Hkv * a.cut.tile;  // from a run's partial to the next
+    constexpr int NB = 16;
+    f32x4_t o[NB];
+    auto load_o = [&](int i0) {
+#pragma unroll
+        for (int u = 0; u < NB; ++u) o[u] = *(const f32x4_t*)(op + (i0 + u < S ? i0 + u : S - 1) * step * D);
+    };
+    load_o(0);
+    float M = -INFINITY;
+    for (int i = k; i < S; i += 16) M = fmaxf(M, lp[i * step]);
+    M = group_max<16>(M);
+    f32x4_t acc = zero_vec<f32x4_t>();
+    float den = 0.f;
+    for (int i0 = 0; i0 < S; i0 += NB) {
+        if (i0) load_o(i0);
+        const float l = i0 + k < S ? lp[(i0 + k) * step] : -INFINITY;
+        const float mine = l == -INFINITY ? 0.f : expf(l - M);
+#pragma unroll
+        for (int u = 0; u < NB; ++u) {
+            const float w = __shfl(mine, group + u);
+            den += w;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[e] = __builtin_fmaf(w, w != 0.f ? o[u][e] : 0.f, acc[e]);
+        }
+    }
+    const bool any = den != 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[e] = any ? acc[e] / den : 0.f;
+    const uint32_t t = a.by_g.div((uint32_t)(row0 + n)), g = (uint32_t)(row0 + n) - t * a.by_g.d;
+    const int64_t at = ((int64_t)p.head * a.G + g) * a.T + p.req.begin + t;
+    *(f32x4_t*)(a.O + at * D + c * 4) = acc;
+    if (c == 0) a.lse[at] = any ? M + logf(den) : -INFINITY;
+}
+
+// ------------------------------------------------------------------------------------------------ the launches
+// What a launch may need, from the sizes the host knows.
+struct PagedLaunch {
+    PagedCut cut;
+    int64_t grid;    // at least the pieces
+    int64_t slots;   // at least the split pieces
+    int64_t merges;  // at least the split tiles
+};
+constexpr int kPagedDecodeRows = 16;
+
+static int target_shift_of(int64_t workgroups) { return 63 - __builtin_clzll((uint64_t)workgroups); }
+
+// tiles: at least the tiles of all requests and heads; keys: at most a request's.
+static PagedLaunch paged_launch(const PagedCut& cut, int64_t tiles, int64_t keys) {
+    const int64_t target = (int64_t)1 << cut.target_shift;
+    const int64_t units = (keys + ((int64_t)1 << cut.unit_shift) - 1) >> cut.unit_shift;
+    const int64_t most_runs = units > cut.least ? (units + cut.least - 1) / cut.least : 1;
+    PagedLaunch l;
+    l.cut = cut;
+    l.grid = target + tiles < tiles * most_runs ? target + tiles : tiles * most_runs;
+    l.slots = most_runs == 1 ? 0 : (l.grid < 2 * target ? l.grid : 2 * target);
+    l.merges = most_runs == 1 ? 0 : (tiles < target ? tiles : target);
+    return l;
+}
+static size_t paged_bytes(const PagedLaunch& l, int D) { return ((size_t)l.slots * l.cut.tile * (D + 1) * 4 + 15) / 16 * 16; }
+
+// At least the tiles of `tile` rows that T rows of B requests come to in `Hkv` heads of G rows each.
+static int64_t paged_tiles(int B, int Hkv, int64_t G, int64_t T, int tile) {
+    return (T * G / tile + (B < T ? B : T)) * Hkv;
+}
+static PagedLaunch decode_launch(const PagedAttnProblem& p, bool only) {
+    PagedCut cut{};
+    cut.tile = kPagedDecodeRows;
+    cut.unit_shift = 7;
+    cut.least = 2;
+    cut.target_shift = target_shift_of(2 * (int64_t)attn_target_wgs());
+    cut.few = 1;
+    cut.many = only ? INT32_MAX : kPagedDecodeRows;
+    const int64_t tiles = only ? paged_tiles(p.B, p.Hkv, p.Hq / p.Hkv, p.T, cut.tile) : (p.B < p.T ? p.B : p.T) * p.Hkv;
+    return paged_launch(cut, tiles, p.max_pages << p.pages.shift);
+}
+// Only requests of few rows are expected: one kernel takes whatever comes.
+static bool decode_only(const PagedAttnProblem& p) {
+    const int64_t G = p.Hq / p.Hkv;
+    return p.dtype != FEDRAG_F32 && (p.T * G <= kPagedDecodeRows || (p.max_q_len > 0 && p.max_q_len <= kPagedDecodeRows / G));
+}
+
+size_t paged_attn_workspace_bytes(int B, int Hq, int Hkv, int D, int dtype, int64_t T, int64_t max_pages, int page_tokens,
+                                  int64_t max_q_len) {
+    if (T == 0 || B == 0 || dtype == FEDRAG_F32) return 0;
+    PagedAttnProblem p{};
+    p.B = B;
+    p.Hq = Hq;
+    p.Hkv = Hkv;
+    p.D = D;
+    p.dtype = dtype;
+    p.T = T;
+    p.max_pages = max_pages;
+    p.pages.shift = __builtin_ctz((unsigned)page_tokens);
+    p.max_q_len = max_q_len;
+    return paged_bytes(decode_launch(p, decode_only(p)), D);
+}
+
+static hipError_t launch_paged_merge(const PagedArgs& a, const PagedLaunch& l, int D, hipStream_t stream) {
+    const int64_t groups = (l.cut.tile * (D / 4) + kPagedMergeThreads - 1) / kPagedMergeThreads;
+    if (!grid_fits(l.merges * groups, kPagedMergeThreads)) return hipErrorInvalidValue;
+    hipLaunchKernelGGL(D == 128 ? paged_merge_kernel<128> : paged_merge_kernel<64>, dim3((unsigned)l.merges, (unsigned)groups),
+                       dim3(kPagedMergeThreads), 0, stream, a);
+    return hipGetLastError();
+}
 
 hipError_t launch_paged_attn(const PagedAttnProblem& p, hipStream_t stream) {
+    const int G = p.Hq / p.Hkv;
+    if (p.T * G > INT32_MAX) return hipErrorInvalidValue;
+    PagedArgs a{};
+    a.Q = p.Q;
+    a.q_head_stride = p.q_head_stride;
+    a.q_token_stride = p.q_token_stride;
+    a.pages = p.pages;
+    a.table = p.table;
+    a.q_start = p.q_start;
+    a.kv_lens = p.kv_lens;
+    a.max_pages = p.max_pages;
+    a.B = p.B;
+    a.T = (int)p.T;
+    a.G = G;
+    a.Hkv = p.Hkv;
+    a.causal = p.causal ? 1 : 0;
+    a.by_g = FastDiv(G);
+    a.by_hkv = FastDiv(p.Hkv);
+    a.scale = p.scale;
+    a.O = p.O;
+    a.lse = p.lse;
+    const bool only = decode_only(p);
+    if (p.dtype != FEDRAG_F32) {
+        const PagedLaunch l = decode_launch(p, only);
+        a.cut = l.cut;
+        a.part_O = (float*)p.workspace;
+        a.slots = (uint32_t)l.slots;
+        a.part_lse = a.part_O + l.slots * l.cut.tile * p.D;
+        hipError_t e = launch_paged_decode(a, p.D, p.dtype, l.grid, stream);
+        if (e == hipSuccess && l.merges > 0) e = launch_paged_merge(a, l, p.D, stream);
+        if (e != hipSuccess || only) return e;
+    }
     if (p.Hq > 65535 || !grid_fits(p.T * p.Hq, 64)) return hipErrorInvalidValue;
     const dim3 grid((unsigned)p.T, (unsigned)p.Hq);
 #define FEDRAG_ROWS(E) (p.D == 128 ? paged_attn_rows_kernel<E, 128> : paged_attn_rows_kernel<E, 64>)
     const auto kernel = p.dtype == FEDRAG_F32 ? FEDRAG_ROWS(float) : p.dtype == FEDRAG_BF16 ? FEDRAG_ROWS(__bf16) : FEDRAG_ROWS(_Float16);
 #undef FEDRAG_ROWS
-    hipLaunchKernelGGL(kernel, grid, dim3(64), 0, stream, p, 1 << p.pages.shift);
+    hipLaunchKernelGGL(kernel, grid, dim3(64), 0, stream, p, 1 << p.pages.shift, p.dtype == FEDRAG_F32 ? 0 : kPagedDecodeRows + 1);
     return hipGetLastError();
 }
 

@@ -80,6 +80,8 @@ fedrag_status check_rows(const fedrag_rows* r, int64_t n_rows, int32_t heads, co
     return FEDRAG_OK;
 }
 
+constexpr int64_t kMostTokens = INT32_MAX - 255;  // of a request: a tile's end is still an int32
+
 bool page_tokens_ok(int32_t n) { return n == 16 || n == 32 || n == 64 || n == 128 || n == 256; }
 
 // The cache's numbers; its pointers are looked at only if it has pages.
@@ -842,7 +844,7 @@ fedrag_status fedrag_paged_write(const fedrag_shape* shape, int64_t n_rows, cons
 size_t fedrag_paged_attn_workspace_bytes(const fedrag_shape* shape, int64_t n_rows, int64_t max_pages, int32_t page_tokens,
                                          int64_t max_q_len) {
     if (check_shape(shape, true) != FEDRAG_OK || check_paged_sizes(n_rows, max_pages, max_q_len) != FEDRAG_OK ||
-        !page_tokens_ok(page_tokens))
+        !page_tokens_ok(page_tokens) || max_pages * page_tokens > kMostTokens)
         return 0;
     return paged_attn_workspace_bytes(shape->batch, shape->n_q_heads, shape->n_kv_heads, shape->d_head, shape->dtype, n_rows, max_pages,
                                       page_tokens, max_q_len);
@@ -859,6 +861,7 @@ fedrag_status fedrag_paged_attn(const fedrag_shape* shape, int64_t n_rows, const
     size_t extent, block, qb;
     st = check_cache(cache, shape, &p.pages, &extent, &block);
     if (st != FEDRAG_OK) return st;
+    if (max_pages * cache->page_tokens > kMostTokens) return FEDRAG_ERR_SHAPE;
     if (n_rows == 0 || shape->batch == 0) return FEDRAG_OK;  // no rows: nothing to do, tensor pointers may be NULL
     if (!(softmax_scale > 0.0f) || softmax_scale - softmax_scale != 0.0f) return FEDRAG_ERR_SHAPE;  // finite, > 0
     st = check_rows(Q, n_rows, shape->n_q_heads, shape, &qb);

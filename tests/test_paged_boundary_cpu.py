@@ -75,7 +75,7 @@ def test_attn_refusals(lib):
         assert attn_call(lib, **{k: None}) == fb.ERR_NULL, k
     assert lib.fedrag_paged_attn(shape(), 4, None, None, None, 0, None, None, 0, 0, 0.1, None, None, None, 0, None) == fb.ERR_NULL
     assert lib.fedrag_paged_attn(None, 4, None, None, None, 0, None, None, 0, 0, 0.1, None, None, None, 0, None) == fb.ERR_NULL
-    for k, v in (("n_rows", -1), ("n_rows", 1 << 31), ("columns", -1), ("columns", 1 << 31), ("max_q", -1), ("n_pages", -1),
+    for k, v in (("n_rows", -1), ("n_rows", 1 << 31), ("columns", -1), ("columns", 1 << 31), ("columns", 1 << 27), ("max_q", -1), ("n_pages", -1),
                  ("n_pages", 1 << 31), ("ps", -8), ("ps", 16 * 128 * 2 - 8), ("hs", -8), ("ts", -8), ("hs", 1 << 62), ("ts", 1 << 62),
                  ("scale", 0.0), ("scale", -1.0), ("scale", float("inf")), ("scale", float("nan"))):
         assert attn_call(lib, **{k: v}) == fb.ERR_SHAPE, (k, v)
