@@ -190,5 +190,6 @@ __device__ __forceinline__ int paged_limit(const PagedArgs& a, const PagedReques
 }
 
 hipError_t launch_paged_decode(const PagedArgs& a, int D, int dtype, int64_t grid, hipStream_t stream);
+hipError_t launch_paged_chunk(const PagedArgs& a, int D, int dtype, int64_t grid, hipStream_t stream);
 
 }  // namespace fedrag

@@ -6,7 +6,7 @@ namespace fedrag {
 // The plainest form: one wave per row and query head, 64 keys at a time.  Lane = key in the first product, = D / 64 channels in
 // the second; running maximum and sum.
 template <class E, int D>
-FEDRAG_KERNEL __launch_bounds__(64) void paged_attn_rows_kernel(PagedAttnProblem p, int n_tokens, int few) {
+FEDRAG_KERNEL __launch_bounds__(64) void paged_attn_rows_kernel(PagedAttnProblem p, int n_tokens) {
     constexpr int DC = D / 64;
     __shared__ float q[D];
     const int lane = threadIdx.x;
@@ -20,7 +20,7 @@ FEDRAG_KERNEL __launch_bounds__(64) void paged_attn_rows_kernel(PagedAttnProblem
         else hi = mid - 1;
     }
     const int64_t begin = p.q_start[lo], end = p.q_start[lo + 1];
-    if (t < begin || t >= end || (end - begin) * (p.Hq / p.Hkv) < few) return;
+    if (t < begin || t >= end) return;
     int64_t L = p.kv_lens[lo] < 0 ? 0 : p.kv_lens[lo];
     if (p.causal) {
         L = L - (end - begin) + (t - begin) + 1;
@@ -78,7 +78,7 @@ template <int D>
 FEDRAG_KERNEL __launch_bounds__(kPagedMergeThreads) void paged_merge_kernel(const PagedArgs a) {
     constexpr int TPR = D / 4;
     const PagedPiece p = paged_piece<true>(a, blockIdx.x);
-    if (p.b < 0 || p.slot + (uint32_t)p.runs * (uint32_t)a.Hkv > a.slots) return;  // (the latter where q_start decreases)
+    if (p.b < 0 || p.slot + (uint32_t)(p.runs - 1) * (uint32_t)a.Hkv >= a.slots) return;  // (the latter where q_start decreases)
     const int row0 = p.tile * a.cut.tile, n = blockIdx.y * (kPagedMergeThreads / TPR) + threadIdx.x / TPR;
     const int c = threadIdx.x % TPR, k = c % 16, group = threadIdx.x % kWave & 48;
     const int last = (row0 + a.cut.tile < p.req.R ? row0 + a.cut.tile : p.req.R) - 1;
@@ -132,8 +132,7 @@ struct PagedLaunch {
     int64_t merges;  // at least the split tiles
 };
 constexpr int kPagedDecodeRows = 16;
-
-static int target_shift_of(int64_t workgroups) { return 63 - __builtin_clzll((uint64_t)workgroups); }
+constexpr int kPagedChunkRows = 4 * kPreQ;
 
 // tiles: at least the tiles of all requests and heads; keys: at most a request's.
 static PagedLaunch paged_launch(const PagedCut& cut, int64_t tiles, int64_t keys) {
@@ -149,41 +148,31 @@ static PagedLaunch paged_launch(const PagedCut& cut, int64_t tiles, int64_t keys
 }
 static size_t paged_bytes(const PagedLaunch& l, int D) { return ((size_t)l.slots * l.cut.tile * (D + 1) * 4 + 15) / 16 * 16; }
 
-// At least the tiles of `tile` rows that T rows of B requests come to in `Hkv` heads of G rows each.
-static int64_t paged_tiles(int B, int Hkv, int64_t G, int64_t T, int tile) {
-    return (T * G / tile + (B < T ? B : T)) * Hkv;
-}
-static PagedLaunch decode_launch(const PagedAttnProblem& p, bool only) {
-    PagedCut cut{};
-    cut.tile = kPagedDecodeRows;
-    cut.unit_shift = 7;
-    cut.least = 2;
-    cut.target_shift = target_shift_of(2 * (int64_t)attn_target_wgs());
-    cut.few = 1;
-    cut.many = only ? INT32_MAX : kPagedDecodeRows;
-    const int64_t tiles = only ? paged_tiles(p.B, p.Hkv, p.Hq / p.Hkv, p.T, cut.tile) : (p.B < p.T ? p.B : p.T) * p.Hkv;
-    return paged_launch(cut, tiles, p.max_pages << p.pages.shift);
-}
-// Only requests of few rows are expected: one kernel takes whatever comes.
-static bool decode_only(const PagedAttnProblem& p) {
-    const int64_t G = p.Hq / p.Hkv;
-    return p.dtype != FEDRAG_F32 && (p.T * G <= kPagedDecodeRows || (p.max_q_len > 0 && p.max_q_len <= kPagedDecodeRows / G));
+// The launches of a call: requests of few rows, of many, or both, where the host cannot know that there are none.
+struct PagedPlan {
+    bool few, many;
+    PagedLaunch decode, chunk;
+    size_t bytes(int D) const { return (few ? paged_bytes(decode, D) : 0) + (many ? paged_bytes(chunk, D) : 0); }
+};
+static PagedPlan paged_plan(int B, int Hq, int Hkv, int64_t T, int64_t keys, int64_t max_q_len) {
+    const int64_t G = Hq / Hkv, some = B < T ? B : T;
+    // at least the tiles that T rows of B requests come to
+    auto tiles = [&](int rows) { return (T * G / rows + some) * Hkv; };
+    const int64_t most = max_q_len > 0 && max_q_len < T ? max_q_len : T;
+    const int shift = 63 - __builtin_clzll(2 * (uint64_t)attn_target_wgs());  // two workgroups to a compute unit, rounded down
+    PagedPlan p;
+    p.many = most * G > kPagedDecodeRows;
+    p.few = !p.many || B > 1;
+    p.decode = paged_launch(PagedCut{kPagedDecodeRows, 7, 2, shift, 1, p.many ? kPagedDecodeRows : INT32_MAX},
+                            p.many ? some * Hkv : tiles(kPagedDecodeRows), keys);
+    p.chunk = paged_launch(PagedCut{kPagedChunkRows, 6, 4, shift, p.few ? kPagedDecodeRows + 1 : 1, INT32_MAX}, tiles(kPagedChunkRows), keys);
+    return p;
 }
 
 size_t paged_attn_workspace_bytes(int B, int Hq, int Hkv, int D, int dtype, int64_t T, int64_t max_pages, int page_tokens,
                                   int64_t max_q_len) {
     if (T == 0 || B == 0 || dtype == FEDRAG_F32) return 0;
-    PagedAttnProblem p{};
-    p.B = B;
-    p.Hq = Hq;
-    p.Hkv = Hkv;
-    p.D = D;
-    p.dtype = dtype;
-    p.T = T;
-    p.max_pages = max_pages;
-    p.pages.shift = __builtin_ctz((unsigned)page_tokens);
-    p.max_q_len = max_q_len;
-    return paged_bytes(decode_launch(p, decode_only(p)), D);
+    return paged_plan(B, Hq, Hkv, T, max_pages * page_tokens, max_q_len).bytes(D);
 }
 
 static hipError_t launch_paged_merge(const PagedArgs& a, const PagedLaunch& l, int D, hipStream_t stream) {
@@ -216,23 +205,27 @@ hipError_t launch_paged_attn(const PagedAttnProblem& p, hipStream_t stream) {
     a.scale = p.scale;
     a.O = p.O;
     a.lse = p.lse;
-    const bool only = decode_only(p);
     if (p.dtype != FEDRAG_F32) {
-        const PagedLaunch l = decode_launch(p, only);
-        a.cut = l.cut;
-        a.part_O = (float*)p.workspace;
-        a.slots = (uint32_t)l.slots;
-        a.part_lse = a.part_O + l.slots * l.cut.tile * p.D;
-        hipError_t e = launch_paged_decode(a, p.D, p.dtype, l.grid, stream);
-        if (e == hipSuccess && l.merges > 0) e = launch_paged_merge(a, l, p.D, stream);
-        if (e != hipSuccess || only) return e;
+        const PagedPlan plan = paged_plan(p.B, p.Hq, p.Hkv, p.T, p.max_pages << p.pages.shift, p.max_q_len);
+        char* scratch = (char*)p.workspace;
+        hipError_t e = hipSuccess;
+        auto run = [&](const PagedLaunch& l, auto kernel) {
+            a.cut = l.cut;
+            a.slots = (uint32_t)l.slots;
+            a.part_O = (float*)scratch;
+            a.part_lse = a.part_O + l.slots * l.cut.tile * p.D;
+            scratch += paged_bytes(l, p.D);
+            e = kernel(a, p.D, p.dtype, l.grid, stream);
+            if (e == hipSuccess && l.merges > 0) e = launch_paged_merge(a, l, p.D, stream);
+        };
+        if (plan.many) run(plan.chunk, launch_paged_chunk);
+        if (e == hipSuccess && plan.few) run(plan.decode, launch_paged_decode);
+        return e;
     }
     if (p.Hq > 65535 || !grid_fits(p.T * p.Hq, 64)) return hipErrorInvalidValue;
     const dim3 grid((unsigned)p.T, (unsigned)p.Hq);
-#define FEDRAG_ROWS(E) (p.D == 128 ? paged_attn_rows_kernel<E, 128> : paged_attn_rows_kernel<E, 64>)
-    const auto kernel = p.dtype == FEDRAG_F32 ? FEDRAG_ROWS(float) : p.dtype == FEDRAG_BF16 ? FEDRAG_ROWS(__bf16) : FEDRAG_ROWS(_Float16);
-#undef FEDRAG_ROWS
-    hipLaunchKernelGGL(kernel, grid, dim3(64), 0, stream, p, 1 << p.pages.shift, p.dtype == FEDRAG_F32 ? 0 : kPagedDecodeRows + 1);
+    const auto kernel = p.D == 128 ? paged_attn_rows_kernel<float, 128> : paged_attn_rows_kernel<float, 64>;
+    hipLaunchKernelGGL(kernel, grid, dim3(64), 0, stream, p, 1 << p.pages.shift);
     return hipGetLastError();
 }
 

@@ -1,0 +1,462 @@
+// Attention over a paged cache for requests of many rows (a chunk of a prompt), 16-bit storage.  Bound by the matrix pipe, which
+// the two-term probabilities give half as much again to do, and by the vector work that does not hide behind it.
+//
+// One workgroup = 4 waves x 32 flattened rows (token r / G, head r % G: all heads of a KV head's group share its keys, and a
+// tile spans few tokens, so that little of it lies above the diagonal) of one request and KV head x one run of keys.
+//   * K, V tiles of 64 keys are shared by the waves through LDS, two slots each, filled by LDS-direct loads one iteration ahead.
+//     A load covers rows of one page (it is 4 or 8 of them): its buffer descriptor begins at those rows and ends with what the
+//     tile sees of the request, or is empty where the table names no page, and what it does not cover arrives as zeros.  Page ids
+//     come 64 loads at a time, one a lane, asked for that long ahead.
+//   * S^T = K Q^T and O^T += V^T P^T (32x32x16 MFMA): the scores already sit in the lanes in which the second product wants the
+//     probabilities.  V^T operands come through the transposing LDS read.  Slots are swizzled against bank conflicts.
+//   * A wave works on two tiles at a time, so that vector work has matrix instructions to hide behind: iteration t issues
+//       A(t):   S^T(t) = K(t) Q^T       with B2(t-1): probabilities of keys 32..63 of tile t-1, whose maximum is known;
+//       C(t-1): O^T += V(t-1)^T P^T     with B1(t):   maximum, rescale factor and probabilities of keys 0..31 of tile t.
+//   * Tiles are visited from the last to the first: those that some row does not see whole (the diagonal, the end of the request)
+//     come first and are finished one by one, up to the last of them, with which the pipeline starts.
+#include "attn_paged.h"
+
+namespace fedrag {
+
+constexpr int kChunkAhead = 4;  // MFMA operands are read from LDS this many MFMAs ahead
+
+template <class T, int D, int NW>
+FEDRAG_KERNEL __launch_bounds__(NW * kWave, 2) void paged_chunk_kernel(const PagedArgs a, float scale_log2) {
+    typedef typename T::elem elem;
+    typedef typename T::vec8 vec8;
+    constexpr int kThreads = NW * kWave;
+    constexpr int ROWB = D * 2;
+    constexpr int SLOT = kPreK * ROWB;
+    constexpr int KS = D / 16;              // contraction steps of S^T
+    constexpr int MT = D / 32;              // 32-row tiles of O^T
+    constexpr int CH = D / 8;               // 16-byte chunks per row
+    constexpr int RPW = kWave / CH;         // rows per load of a wave
+    constexpr int LPT = kPreK / (NW * RPW); // loads per wave and tile
+    constexpr int IDT = kWave / LPT;        // tiles whose page ids a wave holds
+    __shared__ __attribute__((aligned(16))) char ks0[SLOT], ks1[SLOT], vs0[SLOT], vs1[SLOT];
+    __shared__ int sm_odd;
+
+    const int tid = threadIdx.x;
+    const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const int lane = tid % kWave;
+    const int li = lane % 32, lh = lane / 32;
+    const PagedPiece p = paged_piece<false>(a, blockIdx.x);
+    if (p.b < 0) return;
+    const PagedRequest& rq = p.req;
+    const int row0 = p.tile * (NW * kPreQ);
+    const int last = (row0 + NW * kPreQ < rq.R ? row0 + NW * kPreQ : rq.R) - 1;
+    const int lim_min = paged_limit(a, rq, row0), lim_max = paged_limit(a, rq, last);
+    const int k_begin = (int)((int64_t)p.run * p.per << a.cut.unit_shift);
+    const int64_t run_end = (int64_t)k_begin + ((int64_t)p.per << a.cut.unit_shift);
+    const int L = (run_end < lim_max ? (int)run_end : lim_max) - k_begin;  // keys to visit
+    if (p.run > 0 && L <= 0) return;  // a run behind what the tile sees: its partial is not asked for
+
+    const int row_w = row0 + wave * kPreQ;            // this wave's first row
+    const int row = row_w + li < rq.R ? row_w + li : rq.R - 1;
+    const uint32_t tok = a.by_g.div((uint32_t)row), hg = (uint32_t)row - tok * a.by_g.d;
+    // where a row of the request goes: its partial, or its place in O and lse
+    auto place = [&](int r) {
+        if (p.runs > 1) return (int64_t)p.slot * a.cut.tile + (r - row0);
+        const uint32_t t = a.by_g.div((uint32_t)r), g = (uint32_t)r - t * a.by_g.d;
+        return ((int64_t)p.head * a.G + g) * a.T + rq.begin + t;
+    };
+    float* const O = p.runs > 1 ? a.part_O : a.O;
+    float* const lse = p.runs > 1 ? a.part_lse : a.lse;
+    if (L <= 0) {  // no keys (workgroup-uniform, before any barrier)
+        if (row_w + li < rq.R) {
+            const int64_t at = place(row);
+            for (int c = lh * (D / 2); c < (lh + 1) * (D / 2); c += 4) *(f32x4_t*)(O + at * D + c) = zero_vec<f32x4_t>();
+            if (lh == 0) lse[at] = -INFINITY;
+        }
+        return;
+    }
+    const int n_tiles = (L + kPreK - 1) / kPreK;
+    const int whole = lim_min - k_begin < L ? lim_min - k_begin : L;  // keys that every row sees
+    int t_mask0 = whole > 0 ? whole / kPreK : 0;                      // first tile that some row does not see whole
+    const int own = paged_limit(a, rq, row) - k_begin;
+    const int key_lim = own < L ? own : L;                            // this lane's row sees keys < key_lim
+
+    // ---- page ids of this wave's loads, lane l: load l % LPT of the tile l / LPT below `top`
+    const int64_t table0 = (int64_t)p.b * a.max_pages;
+    const int shift = a.pages.shift;
+    auto ask_ids = [&](int top) {
+        const int key = (top - lane / LPT) * kPreK + (lane % LPT * NW + wave) * RPW;
+        int id = -1;
+        if (key >= 0 && key < L) id = a.table[table0 + ((k_begin + key) >> shift)];
+        return id;
+    };
+    auto valid = [&](int id) { return (uint32_t)id < a.pages.n_pages ? id : -1; };
+    // whether the table names a page for all keys of the run; if not, every tile is masked, key by key
+    bool hole = false;
+    for (int64_t key = (int64_t)tid << shift; key < L + ((int64_t)1 << shift); key += (int64_t)kThreads << shift) {
+        const int64_t at = (k_begin >> shift) + (key >> shift);  // (a run may begin inside a page)
+        if ((at << shift) < (int64_t)k_begin + L && valid(a.table[table0 + at]) < 0) hole = true;
+    }
+    int ids_top = n_tiles - 1;  // `ids` is of this tile and the IDT - 1 below
+    int ids = ask_ids(ids_top), ids_next = ask_ids(ids_top - IDT);
+    if (tid == 0) sm_odd = 0;
+    __syncthreads();
+    if (__builtin_amdgcn_ballot_w64(hole) != 0 && lane == 0) sm_odd = 1;
+    ids = valid(ids);
+
+    f32x16_t acc_o[MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) acc_o[i] = zero_vec<f32x16_t>();
+    // the lowest finite value, not -inf: a row may see nothing of a tile, and -inf - m has to be -inf then
+    float m_run = -__FLT_MAX__, l_run = 0.f;
+
+    // ---- pages -> LDS.  LDS slot p of row r holds chunk p ^ swz(r): K swz(r) = r % CH, V (4 (r % 4)) % CH.
+    const int ld_r = lane / CH, ld_p = lane % CH;
+    const int tile_r = wave * RPW + ld_r;  // row in the tile, but for multiples of NW * RPW
+    static_assert((NW * RPW) % 16 == 0, "swizzle must not depend on the load index");
+    const int ld_k = ld_r * ROWB + ((ld_p ^ (tile_r % CH)) << 4);
+    const int ld_v = ld_r * ROWB + ((ld_p ^ ((4 * (tile_r % 4)) % CH)) << 4);
+    int id_of[LPT];  // pages of the tile whose K was asked for last
+    auto load_rows = [&](const char* base, char* slot, int tile, int voff) {
+#pragma unroll
+        for (int j = 0; j < LPT; ++j) {
+            const int key = tile * kPreK + (j * NW + wave) * RPW;
+            const int left = L - key < RPW ? L - key : RPW;
+            const char* page = base + (int64_t)(id_of[j] < 0 ? 0 : id_of[j]) * a.pages.page_bytes +
+                               (((int64_t)p.head << shift) + ((k_begin + key) & ((1 << shift) - 1))) * ROWB;
+            const __amdgpu_buffer_rsrc_t rs =
+                __builtin_amdgcn_make_buffer_rsrc((void*)page, 0, tile < 0 || left < 0 || id_of[j] < 0 ? 0 : left * ROWB, 0x00020000);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (void __attribute__((address_space(3)))*)(slot + (j * NW + wave) * (RPW * ROWB)), 16,
+                                                     voff, 0, 0, 0);
+        }
+    };
+    auto load_k = [&](int tile, char* slot) {
+        if (ids_top - tile == IDT) {  // (workgroup-uniform)
+            ids = valid(ids_next);
+            ids_top -= IDT;
+            ids_next = ask_ids(ids_top - IDT);
+        }
+#pragma unroll
+        for (int j = 0; j < LPT; ++j) id_of[j] = __builtin_amdgcn_readlane(ids, (ids_top - tile) * LPT + j);
+        load_rows(a.pages.K, slot, tile, ld_k);
+    };
+    auto load_v = [&](int tile, char* slot) { load_rows(a.pages.V, slot, tile, ld_v); };  // the tile that load_k had last
+
+    // ---- per-lane LDS read offsets (as the operands of the two products want them)
+    int k_off[KS];
+#pragma unroll
+    for (int i = 0; i < KS; ++i) k_off[i] = li * ROWB + ((((2 * i + lh) % CH) ^ (li % CH)) << 4);
+    const int s16 = lane % 16, gq = lane / 16;
+    int v_off[MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+        const int chunk = 4 * i + 2 * (gq % 2) + (s16 % 4) / 2;
+        v_off[i] = (4 * lh + s16 / 4) * ROWB + (((chunk % CH) ^ ((4 * ((s16 / 4) % 4)) % CH)) << 4) + 8 * ((s16 % 4) % 2);
+    }
+
+    int tile = n_tiles - 1;
+    load_k(tile, ks0);
+    vec8 qop[KS];  // Q^T operands: column li, channels 16 i + 8 lh
+    const char* Qr = a.Q + ((int64_t)p.head * a.G + hg) * a.q_head_stride + ((int64_t)rq.begin + tok) * a.q_token_stride;
+#pragma unroll
+    for (int i = 0; i < KS; ++i) qop[i] = *(const vec8*)(Qr + (i * 16 + lh * 8) * 2);
+
+    f32x16_t S0;                // S^T of the current tile, keys 0..31
+    f32x16_t S1[2];             // S1[t & 1]: keys 32..63 of tile t, kept one iteration longer
+    vec8 P[2][4], Plo[2][4];    // [t & 1]: P^T operands of tile t, one per 16 keys, and what their narrowing left
+    float alph[2];              // [t & 1]: rescale factor of the output that goes with P(t)
+    auto put_p = [&](int par, int kk, int e, float pe) {
+        const elem hi = T::from_float(pe);
+        P[par][kk][e] = hi;
+        Plo[par][kk][e] = T::from_float(pe - T::to_float(hi));
+    };
+    auto pin_p = [&](int par, int kk, int w) {  // a pair's first narrowing stays in its slice
+        u32x4_t v = __builtin_bit_cast(u32x4_t, P[par][kk]);
+        uint32_t x = v[w];
+        pin_here(x);
+        v[w] = x;
+        P[par][kk] = __builtin_bit_cast(vec8, v);
+    };
+    auto read_vop = [&](const char* vt, int kk, int i) -> vec8 {
+        const char* at = vt + kk * 16 * ROWB + v_off[i];
+        const u32x2_t lo = lds_read_tr16(at), hi = lds_read_tr16(at + 8 * ROWB);
+        u32x4_t w;
+        w[0] = lo[0]; w[1] = lo[1]; w[2] = hi[0]; w[3] = hi[1];
+        return __builtin_bit_cast(vec8, w);
+    };
+
+    // par: t & 1 as a constant, so that the double sets are addressed statically.  kFirst: A and B1 of a tile (masked if need be);
+    // kLast: B2 and C of the one before; kSteady: all, on tiles that every row sees whole.
+    enum { kFirst, kSteady, kLast };
+    auto iteration = [&](int tile, int next, auto par, auto stage, bool ld_next) {
+        constexpr int c = decltype(par)::value;
+        constexpr int o = 1 - c;
+        constexpr int kind = decltype(stage)::value;
+        constexpr bool doC = kind != kFirst;
+        constexpr bool doAB = kind != kLast;
+        constexpr int NM = 4 * MT;
+        if constexpr (doAB) load_v(tile, c ? vs1 : vs0);   // slot last read by C(t-2)
+        if (ld_next) load_k(next, o ? ks1 : ks0);          // slot last read by A(t-1)
+
+        // lane: row li and, per 32-key half, keys 8 (r / 4) + 4 lh + r % 4, r = 0..15
+        const char* kt = c ? ks1 : ks0;
+        if constexpr (doAB) {
+            constexpr int NA = 2 * KS;
+            vec8 kop[NA];
+#pragma unroll
+            for (int j = 0; j < kChunkAhead; ++j) kop[j] = *(const vec8*)(kt + (j % 2) * 32 * ROWB + k_off[j / 2]);
+            S0 = zero_vec<f32x16_t>();
+            S1[c] = zero_vec<f32x16_t>();
+            float psum = 0.f;
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int j = 0; j < NA; ++j) {
+                if (j + kChunkAhead < NA)
+                    kop[j + kChunkAhead] = *(const vec8*)(kt + ((j + kChunkAhead) % 2) * 32 * ROWB + k_off[(j + kChunkAhead) / 2]);
+                if (j % 2 == 0) S0 = T::mfma32(kop[j], qop[j / 2], S0);
+                else S1[c] = T::mfma32(kop[j], qop[j / 2], S1[c]);
+                if constexpr (doC) {
+                    const int r0 = (j * 16) / NA, r1 = ((j + 1) * 16) / NA;
+#pragma unroll
+                    for (int r = r0; r < r1; ++r) {
+                        const float pe = fast_exp2(__builtin_fmaf(S1[o][r], scale_log2, -m_run));
+                        psum += pe;
+                        put_p(o, 2 + r / 8, r % 8, pe);
+                        if (r % 2) pin_p(o, 2 + r / 8, (r % 8) / 2);
+                    }
+                    pin_here(psum);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            l_run += psum;
+            if (kind == kFirst && tile >= t_mask0) {
+                const int key0 = tile * kPreK + 4 * lh;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int key = key0 + 8 * (r / 4) + (r % 4);
+                    if (key >= key_lim) S0[r] = -INFINITY;
+                    if (key + 32 >= key_lim) S1[c][r] = -INFINITY;
+                }
+                if (t_mask0 < 0) {  // pages are missing: 16 keys lie in one
+                    bool gone[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int key = tile * kPreK + 16 * i;
+                        gone[i] = key < L && valid(a.table[table0 + ((k_begin + key) >> shift)]) < 0;
+                    }
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        if (gone[r / 8]) S0[r] = -INFINITY;
+                        if (gone[2 + r / 8]) S1[c][r] = -INFINITY;
+                    }
+                }
+            }
+        } else {
+            float psum = 0.f;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const float pe = fast_exp2(__builtin_fmaf(S1[o][r], scale_log2, -m_run));
+                psum += pe;
+                put_p(o, 2 + r / 8, r % 8, pe);
+            }
+            l_run += psum;
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        const char* vt = o ? vs1 : vs0;
+        if constexpr (doC) {
+            if (__builtin_amdgcn_ballot_w64(alph[o] != 1.0f) != 0) {
+#pragma unroll
+                for (int i = 0; i < MT; ++i) acc_o[i] *= alph[o];
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        {
+            constexpr int FIRST = 2;  // slices 0, 1: the row maximum; 2: new maximum and factor; from 2 on: probabilities
+            vec8 vop[NM];
+            if constexpr (doC) {
+#pragma unroll
+                for (int j = 0; j < kChunkAhead; ++j) vop[j] = read_vop(vt, j / MT, j % MT);
+            }
+            float mx = S0[0];
+            float m_new = 0.f, psum = 0.f;
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int j = 0; j < NM; ++j) {
+                if constexpr (doC) {
+                    if (j + kChunkAhead < NM) vop[j + kChunkAhead] = read_vop(vt, (j + kChunkAhead) / MT, (j + kChunkAhead) % MT);
+                    acc_o[j % MT] = T::mfma32(vop[j], P[o][j / MT], acc_o[j % MT]);
+                    acc_o[j % MT] = T::mfma32(vop[j], Plo[o][j / MT], acc_o[j % MT]);
+                }
+                if constexpr (doAB) {
+                    if (j == 0) {
+#pragma unroll
+                        for (int r = 1; r < 16; ++r) mx = fmaxf(mx, S0[r]);
+                    }
+                    if (j == 1) {
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, S1[c][r]);
+                    }
+                    if (j == FIRST) {
+                        mx = xor32_max(mx);
+                        m_new = fmaxf(m_run, mx * scale_log2);
+                        alph[c] = fast_exp2(m_run - m_new);
+                    }
+                    if (j >= FIRST) {
+                        constexpr int NS = NM - FIRST;
+                        const int r0 = ((j - FIRST) * 16) / NS, r1 = ((j - FIRST + 1) * 16) / NS;
+#pragma unroll
+                        for (int r = r0; r < r1; ++r) {
+                            const float pe = fast_exp2(__builtin_fmaf(S0[r], scale_log2, -m_new));
+                            psum += pe;
+                            put_p(c, r / 8, r % 8, pe);
+                            if (r % 2) pin_p(c, r / 8, (r % 8) / 2);
+                        }
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if constexpr (doAB) {
+                l_run = l_run * alph[c] + psum;
+                m_run = m_new;
+            }
+        }
+        if constexpr (doAB) {
+            // keep this iteration's results above the barrier that follows
+#pragma unroll
+            for (int kk = 0; kk < 2; ++kk) {
+                u32x4_t w = __builtin_bit_cast(u32x4_t, P[c][kk]), wl = __builtin_bit_cast(u32x4_t, Plo[c][kk]);
+                pin_here(w);
+                pin_here(wl);
+                P[c][kk] = __builtin_bit_cast(vec8, w);
+                Plo[c][kk] = __builtin_bit_cast(vec8, wl);
+            }
+            pin_here(l_run);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    std::integral_constant<int, 0> even;
+    std::integral_constant<int, 1> odd;
+    std::integral_constant<int, kFirst> first;
+    std::integral_constant<int, kSteady> steady;
+    std::integral_constant<int, kLast> last_stage;
+    auto tile_barrier = [&]() {  // a wave's own LDS-direct loads, then everyone's
+        __builtin_amdgcn_s_waitcnt(0x0f70);
+        __syncthreads();
+    };
+
+    // Some rows see a token of this tile that others do not (its scores are computed, its V lies in vs0, nothing has used it yet).
+    // Where its V is not finite, a product with the probability 0 would bring it to them: such values are taken out of the tile,
+    // and added by themselves for the rows that see them.
+    constexpr uint32_t kExp = std::is_same<T, BF16>::value ? 0x7f80u : 0x7c00u;
+    auto mend = [&](int tile) {
+        bool bad = false;
+#pragma unroll
+        for (int j = 0; j < SLOT / 16 / kThreads; ++j) {
+            const u32x4_t v = *(const u32x4_t*)(vs0 + (j * kThreads + tid) * 16);
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const bool lo = (v[w] & kExp) == kExp, up = (v[w] >> 16 & kExp) == kExp;
+                bad |= lo || up;
+            }
+        }
+        if (__builtin_amdgcn_ballot_w64(bad) != 0 && lane == 0) sm_odd = 1;
+        __syncthreads();
+        if (sm_odd == 0) return;  // workgroup-uniform
+#pragma unroll
+        for (int i = 0; i < MT; ++i) acc_o[i] *= alph[0];
+        alph[0] = 1.0f;
+        for (int k = 0; k < kPreK && tile * kPreK + k < key_lim; ++k)
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {  // channel 32 i + 8 (r / 4) + 4 lh + r % 4
+                    const int ch = 4 * i + r / 4;
+                    const uint16_t v = *(const uint16_t*)(vs0 + k * ROWB + ((ch ^ ((4 * (k % 4)) % CH)) << 4) + lh * 8 + r % 4 * 2);
+                    if ((v & kExp) == kExp) acc_o[i][r] += T::to_float(__builtin_bit_cast(elem, v));
+                }
+        __syncthreads();
+        for (int j = 0; j < SLOT / 16 / kThreads; ++j) {
+            u32x4_t* at = (u32x4_t*)(vs0 + (j * kThreads + tid) * 16);
+            u32x4_t v = *at;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                uint32_t x = v[w];
+                if ((x & kExp) == kExp) x &= 0xffff0000u;
+                if ((x >> 16 & kExp) == kExp) x &= 0xffffu;
+                v[w] = x;
+            }
+            *at = v;
+        }
+        if (tid == 0) sm_odd = 0;
+        __syncthreads();
+    };
+    const bool differ = lim_min != lim_max;
+
+    alph[0] = alph[1] = 1.0f;
+    tile_barrier();
+    if (sm_odd != 0) t_mask0 = -1;
+    __syncthreads();
+    if (tid == 0) sm_odd = 0;
+    __syncthreads();
+    while (tile >= 0 && (tile > t_mask0 || (tile & 1))) {
+        iteration(tile, 0, even, first, false);
+        tile_barrier();
+        if (differ && tile >= t_mask0) mend(tile);
+        --tile;
+        load_k(tile, ks0);
+        iteration(0, 0, odd, last_stage, false);
+        tile_barrier();
+    }
+    if (tile >= 0) {
+        iteration(tile, tile - 1, even, first, true);
+        tile_barrier();
+        if (differ && tile >= t_mask0) mend(tile);
+        for (; tile > 0; tile -= 2) {
+            iteration(tile - 1, tile - 2, odd, steady, true);
+            tile_barrier();
+            iteration(tile - 2, tile - 3, even, steady, true);
+            tile_barrier();
+        }
+        iteration(0, 0, odd, last_stage, false);
+    }
+
+    // The rows go out through LDS (the tiles are dead; every wave has its share), so that a store covers whole lines.
+    const float l_tot = xor32_sum(l_run);
+    __syncthreads();
+    constexpr int WB = 4 * SLOT / NW;
+    constexpr int PC = WB / (kPreQ * 4) < D ? WB / (kPreQ * 4) : D;  // columns per pass
+    constexpr int PCH = PC / 4;
+    static_assert(PC % 32 == 0 && D % PC == 0, "a pass is whole 32-column tiles");
+    const int slot_w = wave * 4 / NW;
+    char* mine = (slot_w == 0 ? ks0 : slot_w == 1 ? ks1 : slot_w == 2 ? vs0 : vs1) + (wave % (NW / 4)) * WB;
+    const float inv = l_tot != 0.f ? 1.0f / l_tot : 0.f;  // (not a number where a score was not)
+#pragma unroll
+    for (int c0 = 0; c0 < D; c0 += PC) {
+#pragma unroll
+        for (int i = c0 / 32; i < (c0 + PC) / 32; ++i)
+#pragma unroll
+            for (int r4 = 0; r4 < 4; ++r4) {
+                f32x4_t o;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) o[r] = l_tot != 0.f ? acc_o[i][4 * r4 + r] * inv : 0.f;
+                const int chunk = 8 * (i - c0 / 32) + 2 * r4 + lh;
+                *(f32x4_t*)(mine + li * (PC * 4) + ((chunk ^ (li % PCH)) << 4)) = o;
+            }
+        wave_lds_fence();
+#pragma unroll
+        for (int u = 0; u < kPreQ * PCH / kWave; ++u) {
+            const int e = u * kWave + lane;
+            const int r = e / PCH, chunk = e % PCH;
+            const f32x4_t o = *(const f32x4_t*)(mine + r * (PC * 4) + ((chunk ^ (r % PCH)) << 4));
+            if (row_w + r < rq.R) *(f32x4_t*)(O + place(row_w + r) * D + c0 + chunk * 4) = o;
+        }
+        wave_lds_fence();
+    }
+    if (lh == 0 && row_w + li < rq.R) lse[place(row)] = l_tot != 0.f ? (m_run + fast_log2(l_tot)) * kLn2 : -INFINITY;
+}
+
+hipError_t launch_paged_chunk(const PagedArgs& a, int D, int dtype, int64_t grid, hipStream_t stream) {
+    constexpr int NW = 4;
+    if (!grid_fits(grid, NW * kWave)) return hipErrorInvalidValue;
+    const auto kernel = dtype == FEDRAG_BF16 ? (D == 128 ? paged_chunk_kernel<BF16, 128, NW> : paged_chunk_kernel<BF16, 64, NW>)
+                                             : (D == 128 ? paged_chunk_kernel<F16, 128, NW> : paged_chunk_kernel<F16, 64, NW>);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(NW * kWave), 0, stream, a, a.scale * kLog2e);
+    return hipGetLastError();
+}
+
+}  // namespace fedrag
