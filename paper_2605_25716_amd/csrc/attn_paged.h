@@ -59,21 +59,6 @@ __device__ __forceinline__ PagedRequest paged_request(const PagedArgs& a, int b)
     return r;
 }
 
-// Inclusive sum over the wave's lanes by data-parallel moves: inside rows of 16, then row 0's total to row 1 and 2's to 3, then
-// the lower half's to the upper.
-template <int CTRL, int ROWS>
-__device__ __forceinline__ uint32_t dpp_or_zero(uint32_t x) {
-    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, false);
-}
-__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
-    x += dpp_or_zero<0x111, 0xf>(x);  // row_shr 1, 2, 4, 8
-    x += dpp_or_zero<0x112, 0xf>(x);
-    x += dpp_or_zero<0x114, 0xf>(x);
-    x += dpp_or_zero<0x118, 0xf>(x);
-    x += dpp_or_zero<0x142, 0xa>(x);  // row_bcast 15
-    x += dpp_or_zero<0x143, 0xc>(x);  // row_bcast 31
-    return x;
-}
 __device__ __forceinline__ uint32_t lane_value(uint32_t x, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)x, lane); }
 __device__ __forceinline__ uint32_t wave_total(uint32_t x) { return lane_value(wave_scan(x), kWave - 1); }
 
@@ -190,6 +175,7 @@ __device__ __forceinline__ int paged_limit(const PagedArgs& a, const PagedReques
 }
 
 hipError_t launch_paged_decode(const PagedArgs& a, int D, int dtype, int64_t grid, hipStream_t stream);
+hipError_t launch_paged_f32(const PagedArgs& a, int D, int dtype, int64_t grid, hipStream_t stream);
 hipError_t launch_paged_chunk(const PagedArgs& a, int D, int dtype, int64_t grid, hipStream_t stream);
 
 }  // namespace fedrag

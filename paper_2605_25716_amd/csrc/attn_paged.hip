@@ -3,74 +3,6 @@
 
 namespace fedrag {
 
-// The plainest form: one wave per row and query head, 64 keys at a time.  Lane = key in the first product, = D / 64 channels in
-// the second; running maximum and sum.
-template <class E, int D>
-FEDRAG_KERNEL __launch_bounds__(64) void paged_attn_rows_kernel(PagedAttnProblem p, int n_tokens) {
-    constexpr int DC = D / 64;
-    __shared__ float q[D];
-    const int lane = threadIdx.x;
-    const int64_t t = blockIdx.x;
-    const int h = blockIdx.y, g = h / (p.Hq / p.Hkv);
-    // the last request that starts at or before t
-    int lo = 0, hi = p.B - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) / 2;
-        if (p.q_start[mid] <= t) lo = mid;
-        else hi = mid - 1;
-    }
-    const int64_t begin = p.q_start[lo], end = p.q_start[lo + 1];
-    if (t < begin || t >= end) return;
-    int64_t L = p.kv_lens[lo] < 0 ? 0 : p.kv_lens[lo];
-    if (p.causal) {
-        L = L - (end - begin) + (t - begin) + 1;
-        L = L < 0 ? 0 : L;
-    }
-    const int64_t room = p.max_pages << p.pages.shift;
-    L = L < room ? L : room;
-    const E* Q = (const E*)(p.Q + h * p.q_head_stride + t * p.q_token_stride);
-    for (int c = lane; c < D; c += 64) q[c] = (float)Q[c];
-    __syncthreads();
-    float m = -INFINITY, l = 0.f, acc[DC] = {};
-    auto row_of = [&](const char* base, int64_t key, uint32_t id) {
-        return (const E*)(base + id * p.pages.page_bytes) + (((int64_t)g << p.pages.shift) + (key & (n_tokens - 1))) * D;
-    };
-    for (int64_t k0 = 0; k0 < L; k0 += 64) {
-        const int64_t key = k0 + lane;
-        uint32_t id = 0xffffffffu;
-        if (key < L) id = (uint32_t)p.table[lo * p.max_pages + (key >> p.pages.shift)];
-        float s = -INFINITY;
-        if (id < p.pages.n_pages) {
-            const E* K = row_of(p.pages.K, key, id);
-            float x = 0.f;
-            for (int c = 0; c < D; ++c) x = __builtin_fmaf((float)K[c], q[c], x);
-            s = x * p.scale;
-        }
-        float top = s;
-        for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
-        const float m_new = fmaxf(m, top);
-        if (m_new == -INFINITY) continue;
-        const float alpha = m == -INFINITY ? 0.f : expf(m - m_new);
-        const float w = s == -INFINITY ? 0.f : expf(s - m_new);
-        float sum = w;
-        for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
-        l = l * alpha + sum;
-        m = m_new;
-        for (int c = 0; c < DC; ++c) acc[c] *= alpha;
-        for (int k = 0; k < 64; ++k) {
-            const uint32_t kid = __shfl(id, k);
-            const float wk = __shfl(w, k);
-            if (kid >= p.pages.n_pages) continue;
-            const E* V = row_of(p.pages.V, k0 + k, kid);
-            for (int c = 0; c < DC; ++c) acc[c] = __builtin_fmaf(wk, (float)V[lane * DC + c], acc[c]);
-        }
-    }
-    const float inv = l > 0.f ? 1.f / l : (l == l ? 0.f : l);
-    float* O = p.O + ((int64_t)h * p.T + t) * D + lane * DC;
-    for (int c = 0; c < DC; ++c) O[c] = l > 0.f || l != l ? acc[c] * inv : 0.f;
-    if (lane == 0) p.lse[(int64_t)h * p.T + t] = l > 0.f || l != l ? m + logf(l) : -INFINITY;
-}
-
 // The aggregation (Section 4.1) of the tiles whose keys were cut into runs: a workgroup takes 8 or 16 rows of one of them, a
 // thread 4 columns of a row.  The lanes of a row share out the weights, 16 runs at a time.
 constexpr int kPagedMergeThreads = 256;
@@ -148,31 +80,41 @@ static PagedLaunch paged_launch(const PagedCut& cut, int64_t tiles, int64_t keys
 }
 static size_t paged_bytes(const PagedLaunch& l, int D) { return ((size_t)l.slots * l.cut.tile * (D + 1) * 4 + 15) / 16 * 16; }
 
-// The launches of a call: requests of few rows, of many, or both, where the host cannot know that there are none.
+// The launches of a call.  16-bit storage: requests of few rows, of many, or both, where the host cannot know that there are
+// none; fp32: one form for all, of 16 or 32 rows.
 struct PagedPlan {
-    bool few, many;
-    PagedLaunch decode, chunk;
-    size_t bytes(int D) const { return (few ? paged_bytes(decode, D) : 0) + (many ? paged_bytes(chunk, D) : 0); }
+    int n;
+    PagedLaunch l[2];
+    hipError_t (*kernel[2])(const PagedArgs&, int, int, int64_t, hipStream_t);
+    size_t bytes(int D) const { return (n > 0 ? paged_bytes(l[0], D) : 0) + (n > 1 ? paged_bytes(l[1], D) : 0); }
 };
-static PagedPlan paged_plan(int B, int Hq, int Hkv, int64_t T, int64_t keys, int64_t max_q_len) {
+static PagedPlan paged_plan(int B, int Hq, int Hkv, int dtype, int64_t T, int64_t keys, int64_t max_q_len) {
     const int64_t G = Hq / Hkv, some = B < T ? B : T;
     // at least the tiles that T rows of B requests come to
     auto tiles = [&](int rows) { return (T * G / rows + some) * Hkv; };
     const int64_t most = max_q_len > 0 && max_q_len < T ? max_q_len : T;
     const int shift = 63 - __builtin_clzll(2 * (uint64_t)attn_target_wgs());  // two workgroups to a compute unit, rounded down
-    PagedPlan p;
-    p.many = most * G > kPagedDecodeRows;
-    p.few = !p.many || B > 1;
-    p.decode = paged_launch(PagedCut{kPagedDecodeRows, 7, 2, shift, 1, p.many ? kPagedDecodeRows : INT32_MAX},
-                            p.many ? some * Hkv : tiles(kPagedDecodeRows), keys);
-    p.chunk = paged_launch(PagedCut{kPagedChunkRows, 6, 4, shift, p.few ? kPagedDecodeRows + 1 : 1, INT32_MAX}, tiles(kPagedChunkRows), keys);
+    const bool many = most * G > kPagedDecodeRows, few = !many || B > 1;
+    PagedPlan p{};
+    auto add = [&](auto kernel, int rows, int unit_shift, int least, int from, int to, int64_t most_tiles) {
+        p.l[p.n] = paged_launch(PagedCut{rows, unit_shift, least, shift, from, to}, most_tiles, keys);
+        p.kernel[p.n++] = kernel;
+    };
+    if (dtype == FEDRAG_F32) {
+        const int rows = many ? 32 : 16;
+        add(launch_paged_f32, rows, 6, 4, 1, INT32_MAX, tiles(rows));
+        return p;
+    }
+    if (many) add(launch_paged_chunk, kPagedChunkRows, 6, 4, few ? kPagedDecodeRows + 1 : 1, INT32_MAX, tiles(kPagedChunkRows));
+    if (few)
+        add(launch_paged_decode, kPagedDecodeRows, 7, 2, 1, many ? kPagedDecodeRows : INT32_MAX, many ? some * Hkv : tiles(kPagedDecodeRows));
     return p;
 }
 
 size_t paged_attn_workspace_bytes(int B, int Hq, int Hkv, int D, int dtype, int64_t T, int64_t max_pages, int page_tokens,
                                   int64_t max_q_len) {
-    if (T == 0 || B == 0 || dtype == FEDRAG_F32) return 0;
-    return paged_plan(B, Hq, Hkv, T, max_pages * page_tokens, max_q_len).bytes(D);
+    if (T == 0 || B == 0) return 0;
+    return paged_plan(B, Hq, Hkv, dtype, T, max_pages * page_tokens, max_q_len).bytes(D);
 }
 
 static hipError_t launch_paged_merge(const PagedArgs& a, const PagedLaunch& l, int D, hipStream_t stream) {
@@ -205,28 +147,20 @@ hipError_t launch_paged_attn(const PagedAttnProblem& p, hipStream_t stream) {
     a.scale = p.scale;
     a.O = p.O;
     a.lse = p.lse;
-    if (p.dtype != FEDRAG_F32) {
-        const PagedPlan plan = paged_plan(p.B, p.Hq, p.Hkv, p.T, p.max_pages << p.pages.shift, p.max_q_len);
-        char* scratch = (char*)p.workspace;
-        hipError_t e = hipSuccess;
-        auto run = [&](const PagedLaunch& l, auto kernel) {
-            a.cut = l.cut;
-            a.slots = (uint32_t)l.slots;
-            a.part_O = (float*)scratch;
-            a.part_lse = a.part_O + l.slots * l.cut.tile * p.D;
-            scratch += paged_bytes(l, p.D);
-            e = kernel(a, p.D, p.dtype, l.grid, stream);
-            if (e == hipSuccess && l.merges > 0) e = launch_paged_merge(a, l, p.D, stream);
-        };
-        if (plan.many) run(plan.chunk, launch_paged_chunk);
-        if (e == hipSuccess && plan.few) run(plan.decode, launch_paged_decode);
-        return e;
+    const PagedPlan plan = paged_plan(p.B, p.Hq, p.Hkv, p.dtype, p.T, p.max_pages << p.pages.shift, p.max_q_len);
+    char* scratch = (char*)p.workspace;
+    for (int i = 0; i < plan.n; ++i) {
+        const PagedLaunch& l = plan.l[i];
+        a.cut = l.cut;
+        a.slots = (uint32_t)l.slots;
+        a.part_O = (float*)scratch;
+        a.part_lse = a.part_O + l.slots * l.cut.tile * p.D;
+        scratch += paged_bytes(l, p.D);
+        hipError_t e = plan.kernel[i](a, p.D, p.dtype, l.grid, stream);
+        if (e == hipSuccess && l.merges > 0) e = launch_paged_merge(a, l, p.D, stream);
+        if (e != hipSuccess) return e;
     }
-    if (p.Hq > 65535 || !grid_fits(p.T * p.Hq, 64)) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)p.T, (unsigned)p.Hq);
-    const auto kernel = p.D == 128 ? paged_attn_rows_kernel<float, 128> : paged_attn_rows_kernel<float, 64>;
-    hipLaunchKernelGGL(kernel, grid, dim3(64), 0, stream, p, 1 << p.pages.shift);
-    return hipGetLastError();
+    return hipSuccess;
 }
 
 }  // namespace fedrag

@@ -122,6 +122,22 @@ __device__ __forceinline__ float group_max(float x) {
     return group_reduce<N>(x, [](float a, float b) { return fmaxf(a, b); });
 }
 
+// Inclusive sum over the wave's lanes by data-parallel moves: inside rows of 16, then row 0's total to row 1 and 2's to 3, then
+// the lower half's to the upper.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t dpp_or_zero(uint32_t x) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, false);
+}
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
+    x += dpp_or_zero<0x111, 0xf>(x);  // row_shr 1, 2, 4, 8
+    x += dpp_or_zero<0x112, 0xf>(x);
+    x += dpp_or_zero<0x114, 0xf>(x);
+    x += dpp_or_zero<0x118, 0xf>(x);
+    x += dpp_or_zero<0x142, 0xa>(x);  // row_bcast 15
+    x += dpp_or_zero<0x143, 0xc>(x);  // row_bcast 31
+    return x;
+}
+
 // The same reduction of a minimum and a maximum at once, one instruction per step and value: the data-parallel move is
 // folded into the minimum / maximum (the compiler emits a move, a canonicalising maximum and the operation itself).  A
 // register has to be two instructions old before a data-parallel read, which the other value's step and a nop give it.
