@@ -1,4 +1,4 @@
-// What the kernels of attention over a paged cache share: the step as they see it, and how they find their piece of it.
+// What the kernels of attention over a paged cache share: the step as they see it, and how they find their part of it.
 #pragma once
 #include <type_traits>
 
@@ -7,13 +7,17 @@
 
 namespace fedrag {
 
-// The work of a launch, cut up on the device: the host knows no lengths.  Request b has R = rows * G flattened query rows per
-// KV head (row r = token r / G, head r % G of the group), in tiles of `tile` rows, and n = ceil(keys / unit) units of keys for each
-// of them.  Runs of at most `per` units, per = max(least, ceil(sum of tiles * n * Hkv / target)), are a workgroup's piece; so
-//   pieces       <= target + tiles of all requests and heads   (the grid),
-//   split pieces <= 2 target                                   (a tile in two or more runs has n > per: their partials),
-//   split tiles  <= target                                     (what the aggregation has to visit).
-// `target` is a power of two: no division of the 64-bit sum.
+// The work of a launch is cut up on the device: the host knows no lengths.  Request b has R = rows * G flattened query rows per
+// KV head (row r = token r / G, head r % G of the group), in tiles of `tile` rows, and n = ceil(keys / unit) units of keys (at least
+// one: a row without keys has an output all the same) for each of them.  All units together are below 2^31, which the host sees
+// to by way of `unit_shift`.  There are two ways to cut:
+//   runs    a tile's keys in equal runs of at most `per` = max(least, ceil(units of all / target)); a workgroup takes one.
+//             runs         <= target + tiles of all requests and heads   (the grid),
+//             split runs   <= 2 target                                   (a tile in two or more has n > per: their partials),
+//             split tiles  <= target                                     (what the aggregation has to visit);
+//   shares  the units of all tiles in a row, and an even share of them to each workgroup, wherever in a tile it begins and ends:
+//           all workgroups end together, whatever the lengths.  For kernels whose partials are small.
+// `target` is a power of two.
 struct PagedCut {
     int tile, unit_shift, least, target_shift;
     int few, many;  // only requests with few <= R <= many are this launch's
@@ -34,143 +38,226 @@ struct PagedArgs {
     PagedCut cut;
 };
 
+// The arguments (of a kernel whose first they are), read again from memory from here on: what is needed between inner loops would
+// otherwise sit in scalar registers throughout, and those that do not fit in lanes of vector registers or in scratch memory.
+typedef const __attribute__((address_space(4))) PagedArgs PagedArgsLate;
+__device__ __forceinline__ PagedArgsLate& late_args() {
+    PagedArgsLate* p = (PagedArgsLate*)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return *p;
+}
+
 struct PagedRequest {
-    int begin, rows, R;  // its first row, how many, times G
-    int kv;              // keys the request has
-    int keys;            // those that its table has columns for
-    int tiles, n;        // tiles of query rows, units of keys
+    int begin, R;  // its first row, and the flattened ones
+    int kv;        // keys the request has
+    int keys;      // those that its table has columns for
 };
 
-__device__ __forceinline__ PagedRequest paged_request(const PagedArgs& a, int b) {
-    int s = a.q_start[b], e = a.q_start[b + 1], kv = a.kv_lens[b];
-    s = s < 0 ? 0 : (s < a.T ? s : a.T);
-    e = e < 0 ? 0 : (e < a.T ? e : a.T);
+// Request b, in two steps: the loads, which many requests have in flight at once, and the rest.
+struct PagedLens {
+    int s, e, kv;
+};
+template <class Args>
+__device__ __forceinline__ PagedLens paged_lens(Args& a, int b) { return PagedLens{a.q_start[b], a.q_start[b + 1], a.kv_lens[b]}; }
+template <class Args>
+__device__ __forceinline__ PagedRequest paged_request(Args& a, PagedLens l) {
+    const int s = l.s < 0 ? 0 : (l.s < a.T ? l.s : a.T), e = l.e < 0 ? 0 : (l.e < a.T ? l.e : a.T);
+    const int64_t room = a.max_pages << a.pages.shift;
     PagedRequest r;
     r.begin = s;
-    r.rows = e > s ? e - s : 0;
-    r.kv = kv < 0 ? 0 : kv;
-    const int64_t room = a.max_pages << a.pages.shift;
+    r.R = e > s ? (e - s) * a.G : 0;  // below 2^31: checked by the host
+    r.kv = l.kv < 0 ? 0 : l.kv;
     r.keys = r.kv < room ? r.kv : (int)room;
-    const int64_t R = (int64_t)r.rows * a.G;
-    r.R = (int)R;  // below 2^31: checked by the host
-    const bool mine = r.R >= a.cut.few && r.R <= a.cut.many;
-    r.tiles = mine ? (r.R + a.cut.tile - 1) / a.cut.tile : 0;
-    r.n = (int)(((int64_t)r.keys + (1 << a.cut.unit_shift) - 1) >> a.cut.unit_shift);
     return r;
+}
+template <class Args>
+__device__ __forceinline__ uint32_t paged_tiles(Args& a, const PagedRequest& r) {
+    return r.R >= a.cut.few && r.R <= a.cut.many ? ((uint32_t)r.R + (uint32_t)a.cut.tile - 1) / (uint32_t)a.cut.tile : 0;
+}
+template <class Args>
+__device__ __forceinline__ uint32_t paged_units(Args& a, const PagedRequest& r) {
+    return r.keys > 0 ? ((uint32_t)(r.keys - 1) >> a.cut.unit_shift) + 1 : 1;
 }
 
 __device__ __forceinline__ uint32_t lane_value(uint32_t x, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)x, lane); }
-__device__ __forceinline__ uint32_t wave_total(uint32_t x) { return lane_value(wave_scan(x), kWave - 1); }
-
-// Units of keys of the longest run, from each lane's share of the work.  (Held below 2^49 a lane, where it already comes to runs
-// of any length.)
-__device__ __forceinline__ uint32_t paged_per(const PagedArgs& a, uint64_t cost) {
-    cost = cost < ((uint64_t)1 << 49) ? cost : (uint64_t)1 << 49;
-    const uint64_t sum = ((uint64_t)wave_total((uint32_t)(cost >> 24)) << 24) + wave_total((uint32_t)cost & 0xffffff);
-    const uint64_t per = (sum + ((uint64_t)1 << a.cut.target_shift) - 1) >> a.cut.target_shift;
-    const uint32_t p = per > 0x7fffffff ? 0x7fffffff : (uint32_t)per;
-    return p > (uint32_t)a.cut.least ? p : (uint32_t)a.cut.least;
-}
-__device__ __forceinline__ uint32_t paged_runs(const PagedRequest& r, uint32_t per) {
-    return (uint32_t)r.n <= per ? 1 : ((uint32_t)r.n + per - 1) / per;
+__device__ __forceinline__ PagedRequest lane_request(const PagedRequest& r, int lane) {
+    return PagedRequest{(int)lane_value((uint32_t)r.begin, lane), (int)lane_value((uint32_t)r.R, lane), (int)lane_value((uint32_t)r.kv, lane),
+                        (int)lane_value((uint32_t)r.keys, lane)};
 }
 
-// A piece of the work, uniform over the wave.
-struct PagedPiece {
-    int b;             // request; < 0: there is no such piece
-    PagedRequest req;
-    int tile, head, run, runs, per;  // tile of rows, KV head, run of keys of `per` units
-    uint32_t slot;     // of its partial, if runs > 1; for SPLIT that of run 0
-};
-
-// Piece `index` of the launch, or (SPLIT) of its split tiles: each wave finds it by itself, a lane per ceil(B / 64) requests that
-// follow each other.  One trip to memory up to 64 requests.  The pieces of a request: tile by tile, the last one first (with a
-// mask the longest), run by run, the heads innermost: workgroups are dealt to the XCDs in turn, so with 8 KV heads the pieces that
-// read the same keys share an L2.
-template <bool SPLIT>
-__device__ __forceinline__ PagedPiece paged_piece(const PagedArgs& a, uint32_t index) {
-    const int lane = threadIdx.x % kWave;
-    const int k = (a.B + kWave - 1) / kWave;  // requests per lane
-    const int64_t b0 = (int64_t)lane * k;
-    PagedRequest one{};
-    uint64_t cost = 0;
-    auto add_cost = [&](const PagedRequest& r) { cost += (uint64_t)((uint32_t)r.tiles * (uint32_t)a.Hkv) * (uint32_t)r.n; };
-    PagedPiece p{};
-    p.b = -1;
-    uint32_t pieces = 0, split = 0;
-    auto count = [&](const PagedRequest& r, uint32_t per) {
-        const uint32_t runs = paged_runs(r, per), n = (uint32_t)r.tiles * (uint32_t)a.Hkv;
-        split += runs > 1 ? n * runs : 0;
-        pieces += SPLIT ? (runs > 1 ? n : 0) : n * runs;
-    };
-    uint32_t per;
+// A lane's requests, k = ceil(B / 64) that follow each other: f(request, there is one) for each, the loads of four at a time in
+// flight together.
+template <class Args, class F>
+__device__ __forceinline__ void paged_each(Args& a, F f) {
+    const int k = (a.B + kWave - 1) / kWave, b0 = threadIdx.x % kWave * k;
     if (k == 1) {
-        if (b0 < a.B) one = paged_request(a, (int)b0);
-        add_cost(one);
-        per = paged_per(a, cost);
-        count(one, per);
-    } else {
-        for (int i = 0; i < k; ++i)
-            if (b0 + i < a.B) add_cost(paged_request(a, (int)(b0 + i)));
-        per = paged_per(a, cost);
-        for (int i = 0; i < k; ++i)
-            if (b0 + i < a.B) count(paged_request(a, (int)(b0 + i)), per);
+        f(paged_request(a, paged_lens(a, b0 < a.B ? b0 : a.B - 1)), b0 < a.B);
+        return;
     }
-    uint32_t pieces_to = wave_scan(pieces), split_to = wave_scan(split);
-    const uint64_t past = __builtin_amdgcn_ballot_w64(pieces_to <= index);
-    int at = __builtin_popcountll(past);
-    if (at == kWave) return p;
-    uint32_t base = at ? lane_value(pieces_to, at - 1) : 0, slot = at ? lane_value(split_to, at - 1) : 0;
-    int b = at;
+    for (int i = 0; i < k; i += 4) {
+        PagedLens l[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) l[u] = paged_lens(a, b0 + i + u < a.B ? b0 + i + u : a.B - 1);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) f(paged_request(a, l[u]), i + u < k && b0 + i + u < a.B);
+    }
+}
+
+// The request that holds number `x` of something that every request has some of, given the sums up to each lane's last request
+// (`to`; some lane's is above x), what a lane's one request is (k == 1), and what a request has of it.  base: the sum of the
+// requests before.
+template <class Args, class Count>
+__device__ __forceinline__ PagedRequest paged_find(Args& a, uint32_t x, uint32_t to, PagedRequest one, Count count, int* b, uint32_t* base) {
+    const int k = (a.B + kWave - 1) / kWave, lane = threadIdx.x % kWave;
+    int at = __builtin_popcountll(__builtin_amdgcn_ballot_w64(to <= x));
+    *base = at ? lane_value(to, at - 1) : 0;
+    *b = at;
     if (k > 1) {  // among that lane's requests, 64 at a time
-        for (int i0 = 0;; i0 += kWave) {
-            const int64_t c = (int64_t)at * k + i0 + lane;
-            const bool is = i0 + lane < k && c < a.B;
-            one = PagedRequest{};
-            if (is) one = paged_request(a, (int)c);
-            pieces = split = 0;
-            if (is) count(one, per);
-            pieces_to = wave_scan(pieces);
-            split_to = wave_scan(split);
-            const int in = __builtin_popcountll(__builtin_amdgcn_ballot_w64(base + pieces_to <= index));
-            if (in < kWave || i0 + kWave >= k) {  // (there is one: the lane's sum said so)
-                const int j = in < kWave ? in : kWave - 1;
-                b = at * k + i0 + j;
-                if (j) {
-                    slot += lane_value(split_to, j - 1);
-                    base += lane_value(pieces_to, j - 1);
-                }
-                at = j;
+        const int first = at * k;
+        for (int i0 = 0; i0 < k; i0 += kWave) {
+            const bool is = i0 + lane < k && first + i0 + lane < a.B;
+            one = paged_request(a, paged_lens(a, is ? first + i0 + lane : a.B - 1));
+            const uint32_t sums = *base + wave_scan(is ? count(one) : 0);
+            at = __builtin_popcountll(__builtin_amdgcn_ballot_w64(sums <= x));
+            *b = first + i0 + at;
+            if (at < kWave) {
+                if (at) *base = lane_value(sums, at - 1);
                 break;
             }
-            base += lane_value(pieces_to, kWave - 1);
-            slot += lane_value(split_to, kWave - 1);
+            *base = lane_value(sums, kWave - 1);
         }
+        at &= kWave - 1;
     }
-    p.b = b;
-    p.req.begin = (int)lane_value((uint32_t)one.begin, at);
-    p.req.rows = (int)lane_value((uint32_t)one.rows, at);
-    p.req.R = (int)lane_value((uint32_t)one.R, at);
-    p.req.kv = (int)lane_value((uint32_t)one.kv, at);
-    p.req.keys = (int)lane_value((uint32_t)one.keys, at);
-    p.req.tiles = (int)lane_value((uint32_t)one.tiles, at);
-    p.req.n = (int)lane_value((uint32_t)one.n, at);
-    const uint32_t runs = paged_runs(p.req, per), i = index - base;
-    const uint32_t rest = a.by_hkv.div(i);
+    return lane_request(one, at);
+}
+
+// ---- runs
+struct PagedPiece {
+    int b;                     // request; < 0: there is no such piece
+    PagedRequest req;
+    int tile, head, run, runs, per;  // tile of rows, KV head, run of keys of `per` units
+    uint32_t slot;             // of its partial, if runs > 1; SPLIT: of run 0
+};
+
+// Piece `index` of the launch, or (SPLIT) of its split tiles; each wave finds it by itself.  The pieces of a request: tile by
+// tile, the last one first (with a mask the longest), run by run, the heads innermost: workgroups are dealt to the XCDs in turn, so
+// with 8 KV heads the pieces that read the same keys share an L2.
+template <bool SPLIT, class Args>
+__device__ __forceinline__ PagedPiece paged_piece(Args& a, uint32_t index) {
+    PagedRequest one{};
+    uint32_t cost = 0;
+    paged_each(a, [&](const PagedRequest& r, bool is) {
+        one = r;
+        cost += is ? paged_tiles(a, r) * (uint32_t)a.Hkv * paged_units(a, r) : 0;
+    });
+    const uint32_t sum = lane_value(wave_scan(cost), kWave - 1);
+    uint32_t per = (uint32_t)(((uint64_t)sum + ((uint64_t)1 << a.cut.target_shift) - 1) >> a.cut.target_shift);
+    per = per > (uint32_t)a.cut.least ? per : (uint32_t)a.cut.least;
+    auto runs_of = [&](const PagedRequest& r) {
+        const uint32_t n = paged_units(a, r);
+        return n <= per ? 1 : (n + per - 1) / per;
+    };
+    auto pieces_of = [&](const PagedRequest& r) {
+        const uint32_t runs = runs_of(r), n = paged_tiles(a, r) * (uint32_t)a.Hkv;
+        return SPLIT ? (runs > 1 ? n : 0) : n * runs;
+    };
+    auto split_of = [&](const PagedRequest& r) {
+        const uint32_t runs = runs_of(r);
+        return runs > 1 ? paged_tiles(a, r) * (uint32_t)a.Hkv * runs : 0;
+    };
+    uint32_t pieces = 0, split = 0;
+    paged_each(a, [&](const PagedRequest& r, bool is) {
+        pieces += is ? pieces_of(r) : 0;
+        split += is ? split_of(r) : 0;
+    });
+    const uint32_t to = wave_scan(pieces), split_to = wave_scan(split);
+    PagedPiece p{};
+    p.b = -1;
+    if (lane_value(to, kWave - 1) <= index) return p;
+    const int at = __builtin_popcountll(__builtin_amdgcn_ballot_w64(to <= index));
+    uint32_t base;
+    p.req = paged_find(a, index, to, one, pieces_of, &p.b, &base);
+    uint32_t slot = at ? lane_value(split_to, at - 1) : 0;
+    const int k = (a.B + kWave - 1) / kWave;
+    for (int b = at * k; b < p.b; ++b) slot += split_of(paged_request(a, paged_lens(a, b)));
+    const uint32_t runs = runs_of(p.req), i = index - base, n = paged_units(a, p.req);
+    const uint32_t rest = FastDiv::div_by(a.by_hkv.m, a.by_hkv.s, i);
     p.head = (int)(i - rest * a.by_hkv.d);
     const uint32_t tile = SPLIT || runs == 1 ? rest : rest / runs;
     p.run = SPLIT || runs == 1 ? 0 : (int)(rest - tile * runs);
-    p.tile = p.req.tiles - 1 - (int)tile;
+    const uint32_t tiles = paged_tiles(a, p.req);
+    p.tile = (int)(tiles - 1 - tile);
     p.runs = (int)runs;
-    p.per = (int)(((uint32_t)p.req.n + runs - 1) / runs);
-    p.slot = slot + (SPLIT ? (tile * runs) * (uint32_t)a.Hkv + (uint32_t)p.head : i);  // run r's: r * Hkv further
+    p.per = (int)((n + runs - 1) / runs);
+    p.slot = slot + (SPLIT ? tile * runs * (uint32_t)a.Hkv + (uint32_t)p.head : i);  // run r's: r * Hkv further
+    if (tile >= tiles) p.b = -1;  // (only sums beyond 32 bits, by a q_start that decreases, lead here)
     return p;
 }
 
-// Keys that a flattened row sees: row r of the request is token r / G.
+// ---- shares
+// A share is max(least, ceil(units of all / target)) units.  It begins at the end of a tile of few units that it would cut (at most
+// `least`, or an eighth of a share).  Partials: workgroup w's of a tile that another began in slot 2 w, of one that it begins and does
+// not end in slot 2 w + 1.
+struct PagedSpan {
+    PagedRequest req;
+    int b, tile, head;  // b < 0: behind the last
+    uint32_t begin, n;  // where the tile begins in the row of units, and its units
+};
+// What each lane has found out about its requests, in LDS: a search costs no trip to memory, and no registers in between.
+struct PagedLanes {
+    uint32_t to[kWave];       // units up to the lane's last request
+    PagedRequest one[kWave];  // its request, where it has one
+};
+template <class Args>
+struct PagedShares {
+    PagedLanes& lanes;
+    uint32_t total, share, whole;  // a tile of no more than `whole` units is not cut
+
+    static __device__ __forceinline__ uint32_t cost(Args& a, const PagedRequest& r) {
+        return paged_tiles(a, r) * (uint32_t)a.Hkv * paged_units(a, r);
+    }
+    // By all threads: the first wave counts, the others wait for it.
+    __device__ __forceinline__ PagedShares(Args& a, PagedLanes& found) : lanes(found) {
+        const int lane = threadIdx.x % kWave;
+        if (threadIdx.x < kWave) {
+            PagedRequest one{};
+            uint32_t mine = 0;
+            paged_each(a, [&](const PagedRequest& r, bool is) {
+                one = r;
+                mine += is ? cost(a, r) : 0;
+            });
+            lanes.to[lane] = wave_scan(mine);
+            lanes.one[lane] = one;
+        }
+        __syncthreads();
+        total = lane_value(lanes.to[kWave - 1], 0);
+        share = (uint32_t)(((uint64_t)total + ((uint64_t)1 << a.cut.target_shift) - 1) >> a.cut.target_shift);
+        share = share > (uint32_t)a.cut.least ? share : (uint32_t)a.cut.least;
+        whole = share / 8 > (uint32_t)a.cut.least ? share / 8 : (uint32_t)a.cut.least;
+    }
+    // The tile that unit `pos` belongs to.
+    __device__ __forceinline__ PagedSpan find(Args& a, uint32_t pos) const {
+        PagedSpan s{};
+        s.b = -1;
+        if (pos >= total) return s;
+        uint32_t base;
+        const int lane = threadIdx.x % kWave;
+        s.req = paged_find(a, pos, lanes.to[lane], lanes.one[lane], [&](const PagedRequest& r) { return cost(a, r); }, &s.b, &base);
+        s.n = paged_units(a, s.req);
+        const uint32_t i = (pos - base) / s.n, tile = FastDiv::div_by(a.by_hkv.m, a.by_hkv.s, i);
+        s.begin = base + i * s.n;
+        s.head = (int)(i - tile * a.by_hkv.d);
+        const uint32_t tiles = paged_tiles(a, s.req);
+        s.tile = (int)(tiles - 1 - tile);
+        if (tile >= tiles) s.b = -1;  // (only sums beyond 32 bits, by a q_start that decreases, lead here)
+        return s;
+    }
+};
+
+// Keys that a flattened row sees: row r of the request is token r / G, and rows / G the last.
 __device__ __forceinline__ int paged_limit(const PagedArgs& a, const PagedRequest& q, int r) {
     if (!a.causal) return q.keys;
-    const int64_t own = (int64_t)q.kv - q.rows + (int)a.by_g.div((uint32_t)r) + 1;
+    const int64_t own = (int64_t)q.kv - (int)a.by_g.div((uint32_t)q.R) + (int)a.by_g.div((uint32_t)r) + 1;
     return own < 0 ? 0 : (own < q.keys ? (int)own : q.keys);
 }
 

@@ -3,40 +3,67 @@
 
 namespace fedrag {
 
-// The aggregation (Section 4.1) of the tiles whose keys were cut into runs: a workgroup takes 8 or 16 rows of one of them, a
-// thread 4 columns of a row.  The lanes of a row share out the weights, 16 runs at a time.
+// The aggregation (Section 4.1) of the tiles whose keys are in several partials: a workgroup takes 8 or 16 rows of one of them, a
+// thread 4 columns of a row.  The lanes of a row share out the weights, 16 partials at a time.
+// Which tile: SHARES: the one that workgroup blockIdx.x + 1's share begins inside of, if no share before does; else the
+// blockIdx.x-th of those in several runs.
 constexpr int kPagedMergeThreads = 256;
-template <int D>
+template <int D, bool SHARES>
 FEDRAG_KERNEL __launch_bounds__(kPagedMergeThreads) void paged_merge_kernel(const PagedArgs a) {
     constexpr int TPR = D / 4;
-    const PagedPiece p = paged_piece<true>(a, blockIdx.x);
-    if (p.b < 0 || p.slot + (uint32_t)(p.runs - 1) * (uint32_t)a.Hkv >= a.slots) return;  // (the latter where q_start decreases)
-    const int row0 = p.tile * a.cut.tile, n = blockIdx.y * (kPagedMergeThreads / TPR) + threadIdx.x / TPR;
+    PagedRequest req;
+    int tile, head, S = 0;
+    int64_t slot, step, first = 0;  // partial i lies in slot + i * step, partial 0 in `first` if SHARES
+    if constexpr (SHARES) {
+        __shared__ PagedLanes lanes;
+        const PagedShares<const PagedArgs> shares(a, lanes);
+        const uint32_t w = blockIdx.x + 1, pos = w * shares.share;
+        const PagedSpan p = shares.find(a, pos);
+        if (p.b < 0 || pos == p.begin || p.n <= shares.whole) return;
+        const uint32_t w0 = p.begin / shares.share;
+        if (w0 + 1 != w) return;
+        req = p.req;
+        tile = p.tile;
+        head = p.head;
+        S = (int)((p.begin + p.n - 1) / shares.share - w0) + 1;
+        if (2 * (w0 + (uint32_t)S) > a.slots) return;  // (where q_start decreases)
+        slot = 2 * (int64_t)w0;
+        step = 2;
+        first = slot + 1;
+    } else {
+        const PagedPiece p = paged_piece<true>(a, blockIdx.x);
+        if (p.b < 0 || p.slot + (uint32_t)(p.runs - 1) * (uint32_t)a.Hkv >= a.slots) return;  // (the latter where q_start decreases)
+        req = p.req;
+        tile = p.tile;
+        head = p.head;
+        slot = first = p.slot;
+        step = a.Hkv;
+        S = p.per;  // units of a run, for now
+    }
+    const int row0 = tile * a.cut.tile, n = blockIdx.y * (kPagedMergeThreads / TPR) + threadIdx.x / TPR;
     const int c = threadIdx.x % TPR, k = c % 16, group = threadIdx.x % kWave & 48;
-    const int last = (row0 + a.cut.tile < p.req.R ? row0 + a.cut.tile : p.req.R) - 1;
+    const int last = (row0 + a.cut.tile < req.R ? row0 + a.cut.tile : req.R) - 1;
     if (row0 + n > last) return;
-    // runs that hold keys which some row of the tile sees
-    const int64_t run_keys = (int64_t)p.per << a.cut.unit_shift;
-    const int64_t seen = paged_limit(a, p.req, last);
-    const int S = seen > 0 ? (int)((seen + run_keys - 1) / run_keys) : 1;
-    const float* lp = a.part_lse + (int64_t)p.slot * a.cut.tile + n;
-    const float* op = a.part_O + ((int64_t)p.slot * a.cut.tile + n) * D + c * 4;
-    const int64_t step = (int64_t)a.Hkv * a.cut.tile;  // from a run's partial to the next
+    if constexpr (!SHARES) {  // runs that hold keys which some row of the tile sees
+        const int64_t run_keys = (int64_t)S << a.cut.unit_shift, seen = paged_limit(a, req, last);
+        S = seen > 0 ? (int)((seen + run_keys - 1) / run_keys) : 1;
+    }
+    auto place = [&](int i) { return ((i == 0 ? first : slot + i * step) * a.cut.tile) + n; };
     constexpr int NB = 16;
     f32x4_t o[NB];
     auto load_o = [&](int i0) {
 #pragma unroll
-        for (int u = 0; u < NB; ++u) o[u] = *(const f32x4_t*)(op + (i0 + u < S ? i0 + u : S - 1) * step * D);
+        for (int u = 0; u < NB; ++u) o[u] = *(const f32x4_t*)(a.part_O + place(i0 + u < S ? i0 + u : S - 1) * D + c * 4);
     };
     load_o(0);
     float M = -INFINITY;
-    for (int i = k; i < S; i += 16) M = fmaxf(M, lp[i * step]);
+    for (int i = k; i < S; i += 16) M = fmaxf(M, a.part_lse[place(i)]);
     M = group_max<16>(M);
     f32x4_t acc = zero_vec<f32x4_t>();
     float den = 0.f;
     for (int i0 = 0; i0 < S; i0 += NB) {
         if (i0) load_o(i0);
-        const float l = i0 + k < S ? lp[(i0 + k) * step] : -INFINITY;
+        const float l = i0 + k < S ? a.part_lse[place(i0 + k)] : -INFINITY;
         const float mine = l == -INFINITY ? 0.f : expf(l - M);
 #pragma unroll
         for (int u = 0; u < NB; ++u) {
@@ -50,7 +77,7 @@ FEDRAG_KERNEL __launch_bounds__(kPagedMergeThreads) void paged_merge_kernel(cons
 #pragma unroll
     for (int e = 0; e < 4; ++e) acc[e] = any ? acc[e] / den : 0.f;
     const uint32_t t = a.by_g.div((uint32_t)(row0 + n)), g = (uint32_t)(row0 + n) - t * a.by_g.d;
-    const int64_t at = ((int64_t)p.head * a.G + g) * a.T + p.req.begin + t;
+    const int64_t at = ((int64_t)head * a.G + g) * a.T + req.begin + t;
     *(f32x4_t*)(a.O + at * D + c * 4) = acc;
     if (c == 0) a.lse[at] = any ? M + logf(den) : -INFINITY;
 }
@@ -62,20 +89,41 @@ struct PagedLaunch {
     int64_t grid;    // at least the pieces
     int64_t slots;   // at least the split pieces
     int64_t merges;  // at least the split tiles
+    bool shares;
 };
 constexpr int kPagedDecodeRows = 16;
 constexpr int kPagedChunkRows = 4 * kPreQ;
 
 // tiles: at least the tiles of all requests and heads; keys: at most a request's.
-static PagedLaunch paged_launch(const PagedCut& cut, int64_t tiles, int64_t keys) {
+static int64_t paged_units_of(PagedCut& cut, int64_t tiles, int64_t keys) {
+    int64_t units = 1;
+    do {
+        units = keys > 0 ? ((keys - 1) >> cut.unit_shift) + 1 : 1;
+    } while (tiles > INT32_MAX / units && ++cut.unit_shift < 31);
+    return units;
+}
+static PagedLaunch paged_runs(PagedCut cut, int64_t tiles, int64_t keys) {
     const int64_t target = (int64_t)1 << cut.target_shift;
-    const int64_t units = (keys + ((int64_t)1 << cut.unit_shift) - 1) >> cut.unit_shift;
+    const int64_t units = paged_units_of(cut, tiles, keys);
     const int64_t most_runs = units > cut.least ? (units + cut.least - 1) / cut.least : 1;
     PagedLaunch l;
     l.cut = cut;
     l.grid = target + tiles < tiles * most_runs ? target + tiles : tiles * most_runs;
     l.slots = most_runs == 1 ? 0 : (l.grid < 2 * target ? l.grid : 2 * target);
     l.merges = most_runs == 1 ? 0 : (tiles < target ? tiles : target);
+    l.shares = false;
+    return l;
+}
+static PagedLaunch paged_shares(PagedCut cut, int64_t tiles, int64_t keys) {
+    const int64_t target = (int64_t)1 << cut.target_shift;
+    const int64_t units = paged_units_of(cut, tiles, keys);
+    const int64_t total = tiles * units;
+    PagedLaunch l;
+    l.cut = cut;
+    l.grid = (total + cut.least - 1) / cut.least < target ? (total + cut.least - 1) / cut.least : target;
+    l.slots = units <= cut.least ? 0 : 2 * l.grid;
+    l.merges = units <= cut.least ? 0 : l.grid - 1;
+    l.shares = true;
     return l;
 }
 static size_t paged_bytes(const PagedLaunch& l, int D) { return ((size_t)l.slots * l.cut.tile * (D + 1) * 4 + 15) / 16 * 16; }
@@ -96,18 +144,18 @@ static PagedPlan paged_plan(int B, int Hq, int Hkv, int dtype, int64_t T, int64_
     const int shift = 63 - __builtin_clzll(2 * (uint64_t)attn_target_wgs());  // two workgroups to a compute unit, rounded down
     const bool many = most * G > kPagedDecodeRows, few = !many || B > 1;
     PagedPlan p{};
-    auto add = [&](auto kernel, int rows, int unit_shift, int least, int from, int to, int64_t most_tiles) {
-        p.l[p.n] = paged_launch(PagedCut{rows, unit_shift, least, shift, from, to}, most_tiles, keys);
+    auto add = [&](auto kernel, auto how, int rows, int unit_shift, int least, int from, int to, int64_t most_tiles) {
+        p.l[p.n] = how(PagedCut{rows, unit_shift, least, shift, from, to}, most_tiles, keys);
         p.kernel[p.n++] = kernel;
     };
     if (dtype == FEDRAG_F32) {
         const int rows = many ? 32 : 16;
-        add(launch_paged_f32, rows, 6, 4, 1, INT32_MAX, tiles(rows));
+        add(launch_paged_f32, paged_runs, rows, 6, 4, 1, INT32_MAX, tiles(rows));
         return p;
     }
-    if (many) add(launch_paged_chunk, kPagedChunkRows, 6, 4, few ? kPagedDecodeRows + 1 : 1, INT32_MAX, tiles(kPagedChunkRows));
+    if (many) add(launch_paged_chunk, paged_runs, kPagedChunkRows, 6, 4, few ? kPagedDecodeRows + 1 : 1, INT32_MAX, tiles(kPagedChunkRows));
     if (few)
-        add(launch_paged_decode, kPagedDecodeRows, 7, 2, 1, many ? kPagedDecodeRows : INT32_MAX, many ? some * Hkv : tiles(kPagedDecodeRows));
+        add(launch_paged_decode, paged_shares, kPagedDecodeRows, 7, 2, 1, many ? kPagedDecodeRows : INT32_MAX, many ? some * Hkv : tiles(kPagedDecodeRows));
     return p;
 }
 
@@ -120,7 +168,9 @@ size_t paged_attn_workspace_bytes(int B, int Hq, int Hkv, int D, int dtype, int6
 static hipError_t launch_paged_merge(const PagedArgs& a, const PagedLaunch& l, int D, hipStream_t stream) {
     const int64_t groups = (l.cut.tile * (D / 4) + kPagedMergeThreads - 1) / kPagedMergeThreads;
     if (!grid_fits(l.merges * groups, kPagedMergeThreads)) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(D == 128 ? paged_merge_kernel<128> : paged_merge_kernel<64>, dim3((unsigned)l.merges, (unsigned)groups),
+    const auto kernel = l.shares ? (D == 128 ? paged_merge_kernel<128, true> : paged_merge_kernel<64, true>)
+                                 : (D == 128 ? paged_merge_kernel<128, false> : paged_merge_kernel<64, false>);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)l.merges, (unsigned)groups),
                        dim3(kPagedMergeThreads), 0, stream, a);
     return hipGetLastError();
 }

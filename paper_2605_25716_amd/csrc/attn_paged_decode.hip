@@ -1,7 +1,8 @@
 // Attention over a paged cache for requests of few rows (at most 16 to a KV head with its group's heads: a decoded token,
 // a few tokens), 16-bit storage.  Bound by HBM: every K, V byte is read once.
 //
-// One workgroup = one KV head of one request x one run of keys (attn_paged.h); its waves take 32-key tiles in turn.  A tile goes
+// One workgroup = an even share of all KV heads' keys of all requests (attn_paged.h), one span of a head's keys after the other; its
+// waves take 32-key tiles in turn.  A tile goes
 // from its pages to LDS in whole rows, 1 KiB of them a load, into slots that belong to one wave and need no barrier; K's slot is
 // filled again after the first product, V's after the second, so that two tiles' worth of loads fly behind every step, and two
 // workgroups share a compute unit: 128 KiB in flight at 128 columns.  A load's rows lie in one page (16 tokens at least), so
@@ -35,18 +36,19 @@ FEDRAG_KERNEL __launch_bounds__(kDecThreads, 2) void paged_decode_kernel(const P
     const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int lane = tid % kWave;
     const int lr = lane % 16, lq = lane / 16;
-    const PagedPiece p = paged_piece<false>(a, blockIdx.x);
-    if (p.b < 0) return;
+    __shared__ PagedLanes lanes;
+    const PagedShares<PagedArgsLate> shares(late_args(), lanes);
+    // `p`: the tile; units u0 .. u0 + take of its n
+    auto span = [&](const PagedSpan& p, uint32_t u0, uint32_t take) {
     const PagedRequest& q = p.req;
     const int row0 = p.tile * a.cut.tile;                                  // the tile's first flattened row
     const int R = q.R - row0 < 16 ? q.R - row0 : 16;
     const int row = row0 + (lr < R ? lr : R - 1);
     const int lim = paged_limit(a, q, row);                                // this lane's row sees keys < lim
     const int lim_min = __builtin_amdgcn_readlane(lim, 0), lim_max = __builtin_amdgcn_readlane(lim, 15);
-    const int k_begin = (int)((int64_t)p.run * p.per << a.cut.unit_shift);  // below the request's keys: 31 bits
-    const int64_t run_end = (int64_t)k_begin + ((int64_t)p.per << a.cut.unit_shift);
-    const int k_end = run_end < lim_max ? (int)run_end : lim_max;
-    if (p.run > 0 && k_end <= k_begin) return;  // a run behind what the tile sees: its partial is not asked for
+    const int k_begin = (int)((int64_t)u0 << a.cut.unit_shift);            // below the request's keys: 31 bits
+    const int64_t span_end = ((int64_t)u0 + take) << a.cut.unit_shift;
+    const int k_end = span_end < lim_max ? (int)span_end : lim_max;        // (may lie before k_begin: nothing to see)
 
     // Q^T operands: column lr, channels 32 ks + 8 lq; rows that are not there are zeros
     const uint32_t tok = a.by_g.div((uint32_t)row), hg = (uint32_t)row - tok * a.by_g.d;
@@ -249,6 +251,9 @@ FEDRAG_KERNEL __launch_bounds__(kDecThreads, 2) void paged_decode_kernel(const P
         for (int t = 0; t < DCH; ++t) *(f32x4_t*)(out_row(wave, lr) + 16 * t + 4 * lq) = acc[t];
     }
     __syncthreads();
+    const PagedArgsLate& z = late_args();
+    const bool part = take < p.n;
+    const int64_t slot = 2 * (int64_t)blockIdx.x + (u0 == 0 ? 1 : 0);
     for (int idx = tid; idx < R * (D / 4); idx += kDecThreads) {
         const int n = idx / (D / 4), c = idx % (D / 4) * 4;
         float M = sm_m[0][n];
@@ -268,10 +273,35 @@ FEDRAG_KERNEL __launch_bounds__(kDecThreads, 2) void paged_decode_kernel(const P
 #pragma unroll
         for (int e = 0; e < 4; ++e) num[e] = any ? num[e] / den : 0.f;
         const float lse = any ? (M + fast_log2(den)) * kLn2 : -INFINITY;
-        const uint32_t t = a.by_g.div((uint32_t)(row0 + n)), g = (uint32_t)(row0 + n) - t * a.by_g.d;
-        const int64_t at = p.runs > 1 ? (int64_t)p.slot * a.cut.tile + n : ((int64_t)p.head * a.G + g) * a.T + q.begin + t;
-        *(f32x4_t*)((p.runs > 1 ? a.part_O : a.O) + at * D + c) = num;
-        if (c == 0) (p.runs > 1 ? a.part_lse : a.lse)[at] = lse;
+        const uint32_t t = FastDiv::div_by(z.by_g.m, z.by_g.s, (uint32_t)(row0 + n)), g = (uint32_t)(row0 + n) - t * z.by_g.d;
+        const int64_t at = part ? slot * z.cut.tile + n : ((int64_t)p.head * z.G + g) * z.T + q.begin + t;
+        *(f32x4_t*)((part ? z.part_O : z.O) + at * D + c) = num;
+        if (c == 0) (part ? z.part_lse : z.lse)[at] = lse;
+    }
+    };
+    // Where the next share begins, where this one does, then its spans; one search in the code for all of them.
+    uint32_t pos = (blockIdx.x + 1) * shares.share, end = 0;
+    for (int stage = 0;;) {
+        PagedArgsLate& z = late_args();
+        const PagedSpan p = shares.find(z, pos);
+        if (stage < 2) {
+            // a share begins behind the few units that it lies among
+            const uint32_t begin = p.b < 0 ? shares.total : pos == p.begin || p.n > shares.whole ? pos : p.begin + p.n;
+            pos = begin;
+            if (stage++ == 0) {
+                end = begin;
+                pos = blockIdx.x * shares.share;
+                continue;
+            }
+            if (pos >= end) return;
+            if (p.b < 0 || pos >= p.begin + p.n) continue;
+        }
+        if (p.b < 0) return;
+        const uint32_t u0 = pos - p.begin, take = end - pos < p.n - u0 ? end - pos : p.n - u0;
+        span(p, u0, take);
+        pos += take;
+        if (pos >= end) return;
+        __syncthreads();  // the slots have been read by all, and are filled again
     }
 }
 

@@ -95,7 +95,8 @@ struct FastDiv {
         s = 31 + (div > 1 ? 64 - (uint32_t)__builtin_clzll((uint64_t)div - 1) : 0);  // + ceil(log2(div))
         m = (uint32_t)((((uint64_t)1 << s) + (uint64_t)div - 1) / (uint64_t)div);
     }
-    __host__ __device__ uint32_t div(uint32_t n) const { return (uint32_t)(((uint64_t)n * m) >> s); }
+    __host__ __device__ static uint32_t div_by(uint32_t m, uint32_t s, uint32_t n) { return (uint32_t)(((uint64_t)n * m) >> s); }
+    __host__ __device__ uint32_t div(uint32_t n) const { return div_by(m, s, n); }
     __host__ __device__ uint32_t mod(uint32_t n) const { return n - div(n) * d; }
 };
 
