@@ -8,7 +8,7 @@
 namespace fedrag {
 
 // The work of a launch is cut up on the device: the host knows no lengths.  Request b has R = rows * G flattened query rows per
-// KV head (row r = token r / G, head r % G of the group), in tiles of `tile` rows, and n = ceil(keys / unit) units of keys (at least
+// KV head (row r = token r / G, head r % G of the group), in tiles of 2^tile_shift rows, and n = ceil(keys / unit) units of keys (at least
 // one: a row without keys has an output all the same) for each of them.  All units together are below 2^31, which the host sees
 // to by way of `unit_shift`.  There are two ways to cut:
 //   runs    a tile's keys in equal runs of at most `per` = max(least, ceil(units of all / target)); a workgroup takes one.
@@ -19,7 +19,7 @@ namespace fedrag {
 //           all workgroups end together, whatever the lengths.  For kernels whose partials are small.
 // `target` is a power of two.
 struct PagedCut {
-    int tile, unit_shift, least, target_shift;
+    int tile_shift, unit_shift, least, target_shift;
     int few, many;  // only requests with few <= R <= many are this launch's
 };
 
@@ -33,7 +33,7 @@ struct PagedArgs {
     FastDiv by_g, by_hkv;
     float scale;
     float *O, *lse;
-    float *part_O, *part_lse;  // [slot][tile][D], [slot][tile]
+    float *part_O, *part_lse;  // [slot][rows of a tile][D], [slot][rows of a tile]
     uint32_t slots;
     PagedCut cut;
 };
@@ -72,7 +72,7 @@ __device__ __forceinline__ PagedRequest paged_request(Args& a, PagedLens l) {
 }
 template <class Args>
 __device__ __forceinline__ uint32_t paged_tiles(Args& a, const PagedRequest& r) {
-    return r.R >= a.cut.few && r.R <= a.cut.many ? ((uint32_t)r.R + (uint32_t)a.cut.tile - 1) / (uint32_t)a.cut.tile : 0;
+    return r.R >= a.cut.few && r.R <= a.cut.many ? ((uint32_t)r.R + (1u << a.cut.tile_shift) - 1) >> a.cut.tile_shift : 0;
 }
 template <class Args>
 __device__ __forceinline__ uint32_t paged_units(Args& a, const PagedRequest& r) {
@@ -141,7 +141,8 @@ struct PagedPiece {
 
 // Piece `index` of the launch, or (SPLIT) of its split tiles; each wave finds it by itself.  The pieces of a request: tile by
 // tile, the last one first (with a mask the longest), run by run, the heads innermost: workgroups are dealt to the XCDs in turn, so
-// with 8 KV heads the pieces that read the same keys share an L2.
+// with 8 KV heads the pieces that read the same keys share an L2.  Up to 64 requests go side by side, all their last tiles, then all
+// those before, so that long pieces start early (4 x 1000 tokens of 32 heads of 128 88 -> 83 us).
 template <bool SPLIT, class Args>
 __device__ __forceinline__ PagedPiece paged_piece(Args& a, uint32_t index) {
     PagedRequest one{};
@@ -174,29 +175,49 @@ __device__ __forceinline__ PagedPiece paged_piece(Args& a, uint32_t index) {
     PagedPiece p{};
     p.b = -1;
     if (lane_value(to, kWave - 1) <= index) return p;
-    const int at = __builtin_popcountll(__builtin_amdgcn_ballot_w64(to <= index));
-    uint32_t base;
-    p.req = paged_find(a, index, to, one, pieces_of, &p.b, &base);
-    uint32_t slot = at ? lane_value(split_to, at - 1) : 0;
     const int k = (a.B + kWave - 1) / kWave;
-    for (int b = at * k; b < p.b; ++b) slot += split_of(paged_request(a, paged_lens(a, b)));
-    const uint32_t runs = runs_of(p.req), i = index - base, n = paged_units(a, p.req);
-    const uint32_t rest = FastDiv::div_by(a.by_hkv.m, a.by_hkv.s, i);
-    p.head = (int)(i - rest * a.by_hkv.d);
-    const uint32_t tile = SPLIT || runs == 1 ? rest : rest / runs;
-    p.run = SPLIT || runs == 1 ? 0 : (int)(rest - tile * runs);
-    const uint32_t tiles = paged_tiles(a, p.req);
-    p.tile = (int)(tiles - 1 - tile);
+    uint32_t group = FastDiv::div_by(a.by_hkv.m, a.by_hkv.s, index);  // a tile and run of a request
+    uint32_t slot, before;                                            // before: tiles of the request that come before it
+    p.head = (int)(index - group * a.by_hkv.d);
+    if (!SPLIT && k == 1) {
+        const uint32_t tiles = (int)threadIdx.x % kWave < a.B ? paged_tiles(a, one) : 0, runs = runs_of(one);
+        auto below = [&](uint32_t level) { return lane_value(wave_scan((tiles < level ? tiles : level) * runs), kWave - 1); };
+        uint32_t level = 0;  // the most whose groups all lie before this one
+        for (uint32_t bit = (uint32_t)1 << (31 - __builtin_clz(((uint32_t)a.T * (uint32_t)a.G >> a.cut.tile_shift) + 1)); bit; bit >>= 1)
+            if (below(level + bit) <= group) level += bit;
+        const uint32_t here = wave_scan(tiles > level ? runs : 0);
+        group -= below(level);
+        p.b = __builtin_popcountll(__builtin_amdgcn_ballot_w64(here <= group));
+        if (p.b >= kWave) {  // (only by a q_start that decreases)
+            p.b = -1;
+            return p;
+        }
+        p.run = (int)(group - (p.b ? lane_value(here, p.b - 1) : 0));
+        p.req = lane_request(one, p.b);
+        slot = p.b ? lane_value(split_to, p.b - 1) : 0;
+        before = level;
+    } else {
+        const int at = __builtin_popcountll(__builtin_amdgcn_ballot_w64(to <= group * (uint32_t)a.Hkv));
+        uint32_t base;
+        p.req = paged_find(a, group * (uint32_t)a.Hkv, to, one, pieces_of, &p.b, &base);
+        slot = at ? lane_value(split_to, at - 1) : 0;
+        for (int b = at * k; b < p.b; ++b) slot += split_of(paged_request(a, paged_lens(a, b)));
+        const uint32_t runs = SPLIT ? 1 : runs_of(p.req), rest = group - FastDiv::div_by(a.by_hkv.m, a.by_hkv.s, base);
+        before = runs == 1 ? rest : rest / runs;
+        p.run = (int)(rest - before * runs);
+    }
+    const uint32_t runs = runs_of(p.req), n = paged_units(a, p.req), tiles = paged_tiles(a, p.req);
+    p.tile = (int)(tiles - 1 - before);
     p.runs = (int)runs;
     p.per = (int)((n + runs - 1) / runs);
-    p.slot = slot + (SPLIT ? tile * runs * (uint32_t)a.Hkv + (uint32_t)p.head : i);  // run r's: r * Hkv further
-    if (tile >= tiles) p.b = -1;  // (only sums beyond 32 bits, by a q_start that decreases, lead here)
+    p.slot = slot + (before * runs + (uint32_t)p.run) * (uint32_t)a.Hkv + (uint32_t)p.head;  // SPLIT: run 0's; run r's is r * Hkv further
+    if (before >= tiles) p.b = -1;  // (only sums beyond 32 bits, by a q_start that decreases, lead here)
     return p;
 }
 
 // ---- shares
-// A share is max(least, ceil(units of all / target)) units.  It begins at the end of a tile of few units that it would cut (at most
-// `least`, or an eighth of a share).  Partials: workgroup w's of a tile that another began in slot 2 w, of one that it begins and does
+// A share is ceil(units of all / target) units, or `least`.  A tile of few units (at most `least`, or an eighth of a share) is not
+// cut: it belongs as a whole to the share in which it begins.  Partials: workgroup w's of a tile that another began in slot 2 w, of one that it begins and does
 // not end in slot 2 w + 1.
 struct PagedSpan {
     PagedRequest req;

@@ -40,15 +40,15 @@ FEDRAG_KERNEL __launch_bounds__(kPagedMergeThreads) void paged_merge_kernel(cons
         step = a.Hkv;
         S = p.per;  // units of a run, for now
     }
-    const int row0 = tile * a.cut.tile, n = blockIdx.y * (kPagedMergeThreads / TPR) + threadIdx.x / TPR;
+    const int row0 = tile << a.cut.tile_shift, n = blockIdx.y * (kPagedMergeThreads / TPR) + threadIdx.x / TPR;
     const int c = threadIdx.x % TPR, k = c % 16, group = threadIdx.x % kWave & 48;
-    const int last = (row0 + a.cut.tile < req.R ? row0 + a.cut.tile : req.R) - 1;
+    const int last = (row0 + (1 << a.cut.tile_shift) < req.R ? row0 + (1 << a.cut.tile_shift) : req.R) - 1;
     if (row0 + n > last) return;
     if constexpr (!SHARES) {  // runs that hold keys which some row of the tile sees
         const int64_t run_keys = (int64_t)S << a.cut.unit_shift, seen = paged_limit(a, req, last);
         S = seen > 0 ? (int)((seen + run_keys - 1) / run_keys) : 1;
     }
-    auto place = [&](int i) { return ((i == 0 ? first : slot + i * step) * a.cut.tile) + n; };
+    auto place = [&](int i) { return ((i == 0 ? first : slot + i * step) << a.cut.tile_shift) + n; };
     constexpr int NB = 16;
     f32x4_t o[NB];
     auto load_o = [&](int i0) {
@@ -91,8 +91,7 @@ struct PagedLaunch {
     int64_t merges;  // at least the split tiles
     bool shares;
 };
-constexpr int kPagedDecodeRows = 16;
-constexpr int kPagedChunkRows = 4 * kPreQ;
+constexpr int kPagedDecodeRows = 16;  // a tile of the kernel for few rows
 
 // tiles: at least the tiles of all requests and heads; keys: at most a request's.
 static int64_t paged_units_of(PagedCut& cut, int64_t tiles, int64_t keys) {
@@ -126,7 +125,7 @@ static PagedLaunch paged_shares(PagedCut cut, int64_t tiles, int64_t keys) {
     l.shares = true;
     return l;
 }
-static size_t paged_bytes(const PagedLaunch& l, int D) { return ((size_t)l.slots * l.cut.tile * (D + 1) * 4 + 15) / 16 * 16; }
+static size_t paged_bytes(const PagedLaunch& l, int D) { return (((size_t)l.slots << l.cut.tile_shift) * (D + 1) * 4 + 15) / 16 * 16; }
 
 // The launches of a call.  16-bit storage: requests of few rows, of many, or both, where the host cannot know that there are
 // none; fp32: one form for all, of 16 or 32 rows.
@@ -139,23 +138,23 @@ struct PagedPlan {
 static PagedPlan paged_plan(int B, int Hq, int Hkv, int dtype, int64_t T, int64_t keys, int64_t max_q_len) {
     const int64_t G = Hq / Hkv, some = B < T ? B : T;
     // at least the tiles that T rows of B requests come to
-    auto tiles = [&](int rows) { return (T * G / rows + some) * Hkv; };
+    auto tiles = [&](int tile_shift) { return ((T * G >> tile_shift) + some) * Hkv; };
     const int64_t most = max_q_len > 0 && max_q_len < T ? max_q_len : T;
     const int shift = 63 - __builtin_clzll(2 * (uint64_t)attn_target_wgs());  // two workgroups to a compute unit, rounded down
     const bool many = most * G > kPagedDecodeRows, few = !many || B > 1;
     PagedPlan p{};
-    auto add = [&](auto kernel, auto how, int rows, int unit_shift, int least, int from, int to, int64_t most_tiles) {
-        p.l[p.n] = how(PagedCut{rows, unit_shift, least, shift, from, to}, most_tiles, keys);
+    auto add = [&](auto kernel, auto how, int tile_shift, int unit_shift, int least, int from, int to, int64_t most_tiles) {
+        p.l[p.n] = how(PagedCut{tile_shift, unit_shift, least, shift, from, to}, most_tiles, keys);
         p.kernel[p.n++] = kernel;
     };
     if (dtype == FEDRAG_F32) {
-        const int rows = many ? 32 : 16;
-        add(launch_paged_f32, paged_runs, rows, 6, 4, 1, INT32_MAX, tiles(rows));
+        const int tile = many ? 5 : 4;
+        add(launch_paged_f32, paged_runs, tile, 6, 4, 1, INT32_MAX, tiles(tile));
         return p;
     }
-    if (many) add(launch_paged_chunk, paged_runs, kPagedChunkRows, 6, 4, few ? kPagedDecodeRows + 1 : 1, INT32_MAX, tiles(kPagedChunkRows));
+    if (many) add(launch_paged_chunk, paged_runs, 7, 6, 4, few ? kPagedDecodeRows + 1 : 1, INT32_MAX, tiles(7));
     if (few)
-        add(launch_paged_decode, paged_shares, kPagedDecodeRows, 7, 2, 1, many ? kPagedDecodeRows : INT32_MAX, many ? some * Hkv : tiles(kPagedDecodeRows));
+        add(launch_paged_decode, paged_shares, 4, 8, 1, 1, many ? kPagedDecodeRows : INT32_MAX, many ? some * Hkv : tiles(4));
     return p;
 }
 
@@ -166,7 +165,7 @@ size_t paged_attn_workspace_bytes(int B, int Hq, int Hkv, int D, int dtype, int6
 }
 
 static hipError_t launch_paged_merge(const PagedArgs& a, const PagedLaunch& l, int D, hipStream_t stream) {
-    const int64_t groups = (l.cut.tile * (D / 4) + kPagedMergeThreads - 1) / kPagedMergeThreads;
+    const int64_t groups = ((D / 4 << l.cut.tile_shift) + kPagedMergeThreads - 1) / kPagedMergeThreads;
     if (!grid_fits(l.merges * groups, kPagedMergeThreads)) return hipErrorInvalidValue;
     const auto kernel = l.shares ? (D == 128 ? paged_merge_kernel<128, true> : paged_merge_kernel<64, true>)
                                  : (D == 128 ? paged_merge_kernel<128, false> : paged_merge_kernel<64, false>);
@@ -204,7 +203,7 @@ hipError_t launch_paged_attn(const PagedAttnProblem& p, hipStream_t stream) {
         a.cut = l.cut;
         a.slots = (uint32_t)l.slots;
         a.part_O = (float*)scratch;
-        a.part_lse = a.part_O + l.slots * l.cut.tile * p.D;
+        a.part_lse = a.part_O + (l.slots << l.cut.tile_shift) * p.D;
         scratch += paged_bytes(l, p.D);
         hipError_t e = plan.kernel[i](a, p.D, p.dtype, l.grid, stream);
         if (e == hipSuccess && l.merges > 0) e = launch_paged_merge(a, l, p.D, stream);

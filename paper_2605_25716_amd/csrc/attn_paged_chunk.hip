@@ -18,7 +18,7 @@
 
 namespace fedrag {
 
-constexpr int kChunkAhead = 4;  // MFMA operands are read from LDS this many MFMAs ahead
+constexpr int kAheadK = 4, kAheadV = 3;  // operands are read from LDS so many before they are used
 
 template <class T, int D, int NW>
 FEDRAG_KERNEL __launch_bounds__(NW * kWave, 2) void paged_chunk_kernel(const PagedArgs a, float scale_log2) {
@@ -54,19 +54,12 @@ FEDRAG_KERNEL __launch_bounds__(NW * kWave, 2) void paged_chunk_kernel(const Pag
     const int row_w = row0 + wave * kPreQ;            // this wave's first row
     const int row = row_w + li < rq.R ? row_w + li : rq.R - 1;
     const uint32_t tok = a.by_g.div((uint32_t)row), hg = (uint32_t)row - tok * a.by_g.d;
-    // where a row of the request goes: its partial, or its place in O and lse
-    auto place = [&](int r) {
-        if (p.runs > 1) return (int64_t)p.slot * a.cut.tile + (r - row0);
-        const uint32_t t = a.by_g.div((uint32_t)r), g = (uint32_t)r - t * a.by_g.d;
-        return ((int64_t)p.head * a.G + g) * a.T + rq.begin + t;
-    };
-    float* const O = p.runs > 1 ? a.part_O : a.O;
-    float* const lse = p.runs > 1 ? a.part_lse : a.lse;
-    if (L <= 0) {  // no keys (workgroup-uniform, before any barrier)
+    if (L <= 0) {  // no keys (workgroup-uniform, before any barrier); other tiles of the request may see several runs
         if (row_w + li < rq.R) {
-            const int64_t at = place(row);
+            const int64_t at = p.runs > 1 ? ((int64_t)p.slot << a.cut.tile_shift) + row - row0 : ((int64_t)p.head * a.G + hg) * a.T + rq.begin + tok;
+            float* const O = p.runs > 1 ? a.part_O : a.O;
             for (int c = lh * (D / 2); c < (lh + 1) * (D / 2); c += 4) *(f32x4_t*)(O + at * D + c) = zero_vec<f32x4_t>();
-            if (lh == 0) lse[at] = -INFINITY;
+            if (lh == 0) (p.runs > 1 ? a.part_lse : a.lse)[at] = -INFINITY;
         }
         return;
     }
@@ -76,28 +69,36 @@ FEDRAG_KERNEL __launch_bounds__(NW * kWave, 2) void paged_chunk_kernel(const Pag
     const int own = paged_limit(a, rq, row) - k_begin;
     const int key_lim = own < L ? own : L;                            // this lane's row sees keys < key_lim
 
-    // ---- page ids of this wave's loads, lane l: load l % LPT of the tile l / LPT below `top`
+    // ---- where this wave's loads begin, lane l: load l % LPT of the tile l / LPT below `top`
     const int64_t table0 = (int64_t)p.b * a.max_pages;
     const int shift = a.pages.shift;
+    auto key_of = [&](int top) { return (top - lane / LPT) * kPreK + (lane % LPT * NW + wave) * RPW; };
     auto ask_ids = [&](int top) {
-        const int key = (top - lane / LPT) * kPreK + (lane % LPT * NW + wave) * RPW;
+        const int key = key_of(top);
         int id = -1;
         if (key >= 0 && key < L) id = a.table[table0 + ((k_begin + key) >> shift)];
         return id;
     };
     auto valid = [&](int id) { return (uint32_t)id < a.pages.n_pages ? id : -1; };
+    // bytes from K's or V's first page to the load's rows; < 0: there are none, or no page
+    auto offset_of = [&](int id, int top) {
+        return valid(id) < 0 ? (int64_t)-1 : (int64_t)id * a.pages.page_bytes + (((int64_t)p.head << shift) + ((k_begin + key_of(top)) & ((1 << shift) - 1))) * ROWB;
+    };
     // whether the table names a page for all keys of the run; if not, every tile is masked, key by key
     bool hole = false;
     for (int64_t key = (int64_t)tid << shift; key < L + ((int64_t)1 << shift); key += (int64_t)kThreads << shift) {
         const int64_t at = (k_begin >> shift) + (key >> shift);  // (a run may begin inside a page)
         if ((at << shift) < (int64_t)k_begin + L && valid(a.table[table0 + at]) < 0) hole = true;
     }
-    int ids_top = n_tiles - 1;  // `ids` is of this tile and the IDT - 1 below
-    int ids = ask_ids(ids_top), ids_next = ask_ids(ids_top - IDT);
+    int top = n_tiles - 1;  // `offset` is of this tile and the IDT - 1 below
+    const int ids = ask_ids(top);
+    int ids_next = ask_ids(top - IDT);
     if (tid == 0) sm_odd = 0;
     __syncthreads();
     if (__builtin_amdgcn_ballot_w64(hole) != 0 && lane == 0) sm_odd = 1;
-    ids = valid(ids);
+    __syncthreads();
+    if (sm_odd != 0) t_mask0 = -1;
+    int64_t offset = offset_of(ids, top);
 
     f32x16_t acc_o[MT];
 #pragma unroll
@@ -111,36 +112,41 @@ FEDRAG_KERNEL __launch_bounds__(NW * kWave, 2) void paged_chunk_kernel(const Pag
     static_assert((NW * RPW) % 16 == 0, "swizzle must not depend on the load index");
     const int ld_k = ld_r * ROWB + ((ld_p ^ (tile_r % CH)) << 4);
     const int ld_v = ld_r * ROWB + ((ld_p ^ ((4 * (tile_r % 4)) % CH)) << 4);
-    int id_of[LPT];  // pages of the tile whose K was asked for last
+    const int full_tiles = t_mask0 < 0 ? 0 : L / kPreK;  // (pages are missing: none)
     auto load_rows = [&](const char* base, char* slot, int tile, int voff) {
+        auto begin = [&](int j) {
+            const int at = (top - tile) * LPT + j;
+            return ((int64_t)__builtin_amdgcn_readlane((int)(offset >> 32), at) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)offset, at);
+        };
+        auto to = [&](int j) { return slot + (j * NW + wave) * (RPW * ROWB); };
+        if ((unsigned)tile < (unsigned)full_tiles) {
+            // all rows are there: no descriptors, whose scalar instructions a wave issues one at a time like any others
 #pragma unroll
-        for (int j = 0; j < LPT; ++j) {
-            const int key = tile * kPreK + (j * NW + wave) * RPW;
-            const int left = L - key < RPW ? L - key : RPW;
-            const char* page = base + (int64_t)(id_of[j] < 0 ? 0 : id_of[j]) * a.pages.page_bytes +
-                               (((int64_t)p.head << shift) + ((k_begin + key) & ((1 << shift) - 1))) * ROWB;
-            const __amdgpu_buffer_rsrc_t rs =
-                __builtin_amdgcn_make_buffer_rsrc((void*)page, 0, tile < 0 || left < 0 || id_of[j] < 0 ? 0 : left * ROWB, 0x00020000);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (void __attribute__((address_space(3)))*)(slot + (j * NW + wave) * (RPW * ROWB)), 16,
-                                                     voff, 0, 0, 0);
+            for (int j = 0; j < LPT; ++j)
+                copy_to_lds(base + begin(j) + (uint32_t)voff, to(j));
+        } else if (tile >= 0) {
+#pragma unroll
+            for (int j = 0; j < LPT; ++j) {
+                const int left = L - (tile * kPreK + (j * NW + wave) * RPW);
+                const int64_t off = begin(j);
+                const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+                    (void*)(base + (off < 0 ? 0 : off)), 0, left <= 0 || off < 0 ? 0 : (left < RPW ? left : RPW) * ROWB, 0x00020000);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (void __attribute__((address_space(3)))*)to(j), 16, voff, 0, 0, 0);
+            }
         }
     };
-    auto load_k = [&](int tile, char* slot) {
-        if (ids_top - tile == IDT) {  // (workgroup-uniform)
-            ids = valid(ids_next);
-            ids_top -= IDT;
-            ids_next = ask_ids(ids_top - IDT);
+    auto load_k = [&](int tile, char* slot) {  // tile by tile downwards; a tile's V is asked for before the next one's K
+        if (top - tile == IDT) {
+            top -= IDT;
+            offset = offset_of(ids_next, top);
+            ids_next = ask_ids(top - IDT);
         }
-#pragma unroll
-        for (int j = 0; j < LPT; ++j) id_of[j] = __builtin_amdgcn_readlane(ids, (ids_top - tile) * LPT + j);
         load_rows(a.pages.K, slot, tile, ld_k);
     };
-    auto load_v = [&](int tile, char* slot) { load_rows(a.pages.V, slot, tile, ld_v); };  // the tile that load_k had last
+    auto load_v = [&](int tile, char* slot) { load_rows(a.pages.V, slot, tile, ld_v); };
 
     // ---- per-lane LDS read offsets (as the operands of the two products want them)
-    int k_off[KS];
-#pragma unroll
-    for (int i = 0; i < KS; ++i) k_off[i] = li * ROWB + ((((2 * i + lh) % CH) ^ (li % CH)) << 4);
+    const int k_base = li * ROWB + ((lh ^ (li % CH)) << 4);  // channels 16 i + 8 lh of row li: k_base ^ 32 i
     const int s16 = lane % 16, gq = lane / 16;
     int v_off[MT];
 #pragma unroll
@@ -157,20 +163,28 @@ FEDRAG_KERNEL __launch_bounds__(NW * kWave, 2) void paged_chunk_kernel(const Pag
     for (int i = 0; i < KS; ++i) qop[i] = *(const vec8*)(Qr + (i * 16 + lh * 8) * 2);
 
     f32x16_t S0;                // S^T of the current tile, keys 0..31
-    f32x16_t S1[2];             // S1[t & 1]: keys 32..63 of tile t, kept one iteration longer
-    vec8 P[2][4], Plo[2][4];    // [t & 1]: P^T operands of tile t, one per 16 keys, and what their narrowing left
+    f32x16_t S1[2];             // S1[t & 1]: keys 32..63 of tile t, kept one iteration longer; then their probabilities
+    uint32_t P[2][4][4];        // [t & 1]: P^T operands of tile t, one per 16 keys, in words of two,
+    uint32_t Plo[2][4][4];      //          and what their narrowing left
     float alph[2];              // [t & 1]: rescale factor of the output that goes with P(t)
-    auto put_p = [&](int par, int kk, int e, float pe) {
-        const elem hi = T::from_float(pe);
-        P[par][kk][e] = hi;
-        Plo[par][kk][e] = T::from_float(pe - T::to_float(hi));
+    auto operand = [&](const uint32_t (&w)[4]) -> vec8 {
+        u32x4_t v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = w[e];
+        return __builtin_bit_cast(vec8, v);
     };
-    auto pin_p = [&](int par, int kk, int w) {  // a pair's first narrowing stays in its slice
-        u32x4_t v = __builtin_bit_cast(u32x4_t, P[par][kk]);
-        uint32_t x = v[w];
-        pin_here(x);
-        v[w] = x;
-        P[par][kk] = __builtin_bit_cast(vec8, v);
+    // register r (even) of a half's scores and the next one <-> word r % 8 / 2 of the operand of 16 keys r / 8 (+ 2 for the second half)
+    auto put_hi = [&](int par, int kk, int w, float x, float y) {
+        P[par][kk][w] = T::pack(x, y);
+        pin_here(P[par][kk][w]);  // in its slice, not behind the phase
+    };
+    auto put_lo = [&](int par, int kk, int w, float x, float y) {
+        Plo[par][kk][w] = T::pack(x - T::low(P[par][kk][w]), y - T::high(P[par][kk][w]));
+        pin_here(Plo[par][kk][w]);
+    };
+    auto put = [&](int par, int kk, int w, float x, float y) {
+        put_hi(par, kk, w, x, y);
+        put_lo(par, kk, w, x, y);
     };
     auto read_vop = [&](const char* vt, int kk, int i) -> vec8 {
         const char* at = vt + kk * 16 * ROWB + v_off[i];
@@ -198,26 +212,30 @@ FEDRAG_KERNEL __launch_bounds__(NW * kWave, 2) void paged_chunk_kernel(const Pag
         if constexpr (doAB) {
             constexpr int NA = 2 * KS;
             vec8 kop[NA];
+            int k_off[KS];  // (made anew for each tile: eight instructions, and not eight registers in the other phase)
+            int kb = k_base;
+            pin_here(kb);
 #pragma unroll
-            for (int j = 0; j < kChunkAhead; ++j) kop[j] = *(const vec8*)(kt + (j % 2) * 32 * ROWB + k_off[j / 2]);
+            for (int i = 0; i < KS; ++i) k_off[i] = kb ^ (32 * i);
+#pragma unroll
+            for (int j = 0; j < kAheadK; ++j) kop[j] = *(const vec8*)(kt + (j % 2) * 32 * ROWB + k_off[j / 2]);
             S0 = zero_vec<f32x16_t>();
             S1[c] = zero_vec<f32x16_t>();
             float psum = 0.f;
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int j = 0; j < NA; ++j) {
-                if (j + kChunkAhead < NA)
-                    kop[j + kChunkAhead] = *(const vec8*)(kt + ((j + kChunkAhead) % 2) * 32 * ROWB + k_off[(j + kChunkAhead) / 2]);
+                if (j + kAheadK < NA)
+                    kop[j + kAheadK] = *(const vec8*)(kt + ((j + kAheadK) % 2) * 32 * ROWB + k_off[(j + kAheadK) / 2]);
                 if (j % 2 == 0) S0 = T::mfma32(kop[j], qop[j / 2], S0);
                 else S1[c] = T::mfma32(kop[j], qop[j / 2], S1[c]);
                 if constexpr (doC) {
-                    const int r0 = (j * 16) / NA, r1 = ((j + 1) * 16) / NA;
 #pragma unroll
-                    for (int r = r0; r < r1; ++r) {
+                    for (int r = (j * 16) / NA; r < ((j + 1) * 16) / NA; ++r) {
                         const float pe = fast_exp2(__builtin_fmaf(S1[o][r], scale_log2, -m_run));
                         psum += pe;
-                        put_p(o, 2 + r / 8, r % 8, pe);
-                        if (r % 2) pin_p(o, 2 + r / 8, (r % 8) / 2);
+                        S1[o][r] = pe;
+                        if (r % 2) put(o, 2 + r / 8, r % 8 / 2, S1[o][r - 1], pe);
                     }
                     pin_here(psum);
                 }
@@ -252,7 +270,8 @@ FEDRAG_KERNEL __launch_bounds__(NW * kWave, 2) void paged_chunk_kernel(const Pag
             for (int r = 0; r < 16; ++r) {
                 const float pe = fast_exp2(__builtin_fmaf(S1[o][r], scale_log2, -m_run));
                 psum += pe;
-                put_p(o, 2 + r / 8, r % 8, pe);
+                S1[o][r] = pe;
+                if (r % 2) put(o, 2 + r / 8, r % 8 / 2, S1[o][r - 1], pe);
             }
             l_run += psum;
         }
@@ -266,67 +285,64 @@ FEDRAG_KERNEL __launch_bounds__(NW * kWave, 2) void paged_chunk_kernel(const Pag
         }
         __builtin_amdgcn_sched_barrier(0);
         {
-            constexpr int FIRST = 2;  // slices 0, 1: the row maximum; 2: new maximum and factor; from 2 on: probabilities
+            // One matrix instruction a slice, with its share of the vector work, some six instructions a step: four steps of the row
+            // maximum, one of the new maximum and the factor, and three for each pair of probabilities of keys 0..31.  An output tile's two instructions are two apart: the second waits for the first, and a
+            // wave that waits issues no vector work either.
+            constexpr int NJ = 2 * NM;
+            constexpr int kSteps = 4 + 1 + 24;
             vec8 vop[NM];
             if constexpr (doC) {
 #pragma unroll
-                for (int j = 0; j < kChunkAhead; ++j) vop[j] = read_vop(vt, j / MT, j % MT);
+                for (int j = 0; j < kAheadV; ++j) vop[j] = read_vop(vt, j / MT, j % MT);
             }
-            float mx = S0[0];
+            float mx = -INFINITY;
             float m_new = 0.f, psum = 0.f;
-            __builtin_amdgcn_sched_barrier(0);
+            auto step = [&](int s) {
+                if (s < 4) {
+                    if constexpr (doAB) {
 #pragma unroll
-            for (int j = 0; j < NM; ++j) {
-                if constexpr (doC) {
-                    if (j + kChunkAhead < NM) vop[j + kChunkAhead] = read_vop(vt, (j + kChunkAhead) / MT, (j + kChunkAhead) % MT);
-                    acc_o[j % MT] = T::mfma32(vop[j], P[o][j / MT], acc_o[j % MT]);
-                    acc_o[j % MT] = T::mfma32(vop[j], Plo[o][j / MT], acc_o[j % MT]);
-                }
-                if constexpr (doAB) {
-                    if (j == 0) {
-#pragma unroll
-                        for (int r = 1; r < 16; ++r) mx = fmaxf(mx, S0[r]);
+                        for (int r = 4 * s; r < 4 * s + 4; ++r) mx = fmaxf(fmaxf(mx, S0[r]), S1[c][r]);
+                        pin_here(mx);
                     }
-                    if (j == 1) {
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, S1[c][r]);
-                    }
-                    if (j == FIRST) {
+                } else if (s == 4) {
+                    if constexpr (doAB) {
                         mx = xor32_max(mx);
                         m_new = fmaxf(m_run, mx * scale_log2);
                         alph[c] = fast_exp2(m_run - m_new);
                     }
-                    if (j >= FIRST) {
-                        constexpr int NS = NM - FIRST;
-                        const int r0 = ((j - FIRST) * 16) / NS, r1 = ((j - FIRST + 1) * 16) / NS;
-#pragma unroll
-                        for (int r = r0; r < r1; ++r) {
-                            const float pe = fast_exp2(__builtin_fmaf(S0[r], scale_log2, -m_new));
-                            psum += pe;
-                            put_p(c, r / 8, r % 8, pe);
-                            if (r % 2) pin_p(c, r / 8, (r % 8) / 2);
+                } else {
+                    if constexpr (doAB) {
+                        const int r = (s - 5) / 3 * 2, part = (s - 5) % 3;
+                        if (part < 2) {
+                            S0[r + part] = fast_exp2(__builtin_fmaf(S0[r + part], scale_log2, -m_new));
+                            psum += S0[r + part];
+                            pin_here(psum);
+                            if (part == 1) put_hi(c, r / 8, r % 8 / 2, S0[r], S0[r + 1]);
+                        } else {
+                            put_lo(c, r / 8, r % 8 / 2, S0[r], S0[r + 1]);
                         }
                     }
                 }
-                __builtin_amdgcn_sched_barrier(0);
+            };
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+                if constexpr (doC) {
+                    // of each four: tiles i, i + 1 with the first terms, then with the second
+                    const int at = j / 4 * 2 + j % 2, kk = at / MT, i = at % MT;
+                    if (j % 4 < 2 && at + kAheadV < NM) vop[at + kAheadV] = read_vop(vt, (at + kAheadV) / MT, (at + kAheadV) % MT);
+                    acc_o[i] = T::mfma32(vop[at], operand(j % 4 < 2 ? P[o][kk] : Plo[o][kk]), acc_o[i]);
+                }
+#pragma unroll
+                for (int s = j * kSteps / NJ; s < (j + 1) * kSteps / NJ; ++s) step(s);
+                if constexpr (doC) __builtin_amdgcn_sched_barrier(0);
             }
             if constexpr (doAB) {
                 l_run = l_run * alph[c] + psum;
                 m_run = m_new;
             }
         }
-        if constexpr (doAB) {
-            // keep this iteration's results above the barrier that follows
-#pragma unroll
-            for (int kk = 0; kk < 2; ++kk) {
-                u32x4_t w = __builtin_bit_cast(u32x4_t, P[c][kk]), wl = __builtin_bit_cast(u32x4_t, Plo[c][kk]);
-                pin_here(w);
-                pin_here(wl);
-                P[c][kk] = __builtin_bit_cast(vec8, w);
-                Plo[c][kk] = __builtin_bit_cast(vec8, wl);
-            }
-            pin_here(l_run);
-        }
+        if constexpr (doAB) pin_here(l_run);  // above the barrier that follows
         __builtin_amdgcn_sched_barrier(0);
     };
     std::integral_constant<int, 0> even;
@@ -344,6 +360,9 @@ FEDRAG_KERNEL __launch_bounds__(NW * kWave, 2) void paged_chunk_kernel(const Pag
     // and added by themselves for the rows that see them.
     constexpr uint32_t kExp = std::is_same<T, BF16>::value ? 0x7f80u : 0x7c00u;
     auto mend = [&](int tile) {
+        int tid = threadIdx.x;  // anew: what is rarely used is not kept in registers through the loops
+        pin_here(tid);
+        const int lane = tid % kWave, lh = lane / 32;
         bool bad = false;
 #pragma unroll
         for (int j = 0; j < SLOT / 16 / kThreads; ++j) {
@@ -364,12 +383,17 @@ FEDRAG_KERNEL __launch_bounds__(NW * kWave, 2) void paged_chunk_kernel(const Pag
 #pragma unroll
             for (int i = 0; i < MT; ++i)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {  // channel 32 i + 8 (r / 4) + 4 lh + r % 4
-                    const int ch = 4 * i + r / 4;
-                    const uint16_t v = *(const uint16_t*)(vs0 + k * ROWB + ((ch ^ ((4 * (k % 4)) % CH)) << 4) + lh * 8 + r % 4 * 2);
-                    if ((v & kExp) == kExp) acc_o[i][r] += T::to_float(__builtin_bit_cast(elem, v));
+                for (int r4 = 0; r4 < 4; ++r4) {  // channels 32 i + 8 r4 + 4 lh + 0..3: half of a 16-byte chunk
+                    const u32x2_t v = *(const u32x2_t*)(vs0 + k * ROWB + (((4 * i + r4) ^ ((4 * (k % 4)) % CH)) << 4) + lh * 8);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint32_t x = (e < 2 ? v[0] : v[1]) >> (e % 2 * 16) & 0xffffu;
+                        if ((x & kExp) == kExp) acc_o[i][4 * r4 + e] += T::to_float(__builtin_bit_cast(elem, (uint16_t)x));
+                    }
+                    __builtin_amdgcn_sched_barrier(0);  // (more of these reads in flight would take registers from the loops)
                 }
         __syncthreads();
+#pragma unroll 1
         for (int j = 0; j < SLOT / 16 / kThreads; ++j) {
             u32x4_t* at = (u32x4_t*)(vs0 + (j * kThreads + tid) * 16);
             u32x4_t v = *at;
@@ -389,8 +413,6 @@ FEDRAG_KERNEL __launch_bounds__(NW * kWave, 2) void paged_chunk_kernel(const Pag
 
     alph[0] = alph[1] = 1.0f;
     tile_barrier();
-    if (sm_odd != 0) t_mask0 = -1;
-    __syncthreads();
     if (tid == 0) sm_odd = 0;
     __syncthreads();
     while (tile >= 0 && (tile > t_mask0 || (tile & 1))) {
@@ -419,35 +441,43 @@ FEDRAG_KERNEL __launch_bounds__(NW * kWave, 2) void paged_chunk_kernel(const Pag
     const float l_tot = xor32_sum(l_run);
     __syncthreads();
     constexpr int WB = 4 * SLOT / NW;
-    constexpr int PC = WB / (kPreQ * 4) < D ? WB / (kPreQ * 4) : D;  // columns per pass
-    constexpr int PCH = PC / 4;
-    static_assert(PC % 32 == 0 && D % PC == 0, "a pass is whole 32-column tiles");
-    const int slot_w = wave * 4 / NW;
-    char* mine = (slot_w == 0 ? ks0 : slot_w == 1 ? ks1 : slot_w == 2 ? vs0 : vs1) + (wave % (NW / 4)) * WB;
-    const float inv = l_tot != 0.f ? 1.0f / l_tot : 0.f;  // (not a number where a score was not)
+    static_assert(WB == kPreQ * D * 4, "a wave's rows fit its share");
+    constexpr int PCH = D / 4;  // 16-byte chunks per row
+    int l = threadIdx.x % kWave;  // anew, as above
+    pin_here(l);
+    auto finish = [&](const int lane) {
+        const int li = lane % 32, lh = lane / 32;
+        const int slot_w = wave * 4 / NW;
+        char* mine = (slot_w == 0 ? ks0 : slot_w == 1 ? ks1 : slot_w == 2 ? vs0 : vs1) + (wave % (NW / 4)) * WB;
+        const PagedArgsLate& z = late_args();
+        const int r_in = row_w - row0 + li;  // this lane's row in the tile
+        const bool real = row_w + li < rq.R;
+        // its partial's place, or its own in O and lse: row t / G of head t % G
+        const uint32_t t = FastDiv::div_by(z.by_g.m, z.by_g.s, (uint32_t)(row_w + li)), g = (uint32_t)(row_w + li) - t * z.by_g.d;
+        const int64_t at = p.runs > 1 ? ((int64_t)p.slot << z.cut.tile_shift) + r_in : ((int64_t)p.head * z.G + g) * z.T + rq.begin + t;
+        float* const O = p.runs > 1 ? z.part_O : z.O;
+        const float inv = l_tot != 0.f ? 1.0f / l_tot : 0.f;  // (not a number where a score was not)
 #pragma unroll
-    for (int c0 = 0; c0 < D; c0 += PC) {
-#pragma unroll
-        for (int i = c0 / 32; i < (c0 + PC) / 32; ++i)
+        for (int i = 0; i < MT; ++i)
 #pragma unroll
             for (int r4 = 0; r4 < 4; ++r4) {
                 f32x4_t o;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) o[r] = l_tot != 0.f ? acc_o[i][4 * r4 + r] * inv : 0.f;
-                const int chunk = 8 * (i - c0 / 32) + 2 * r4 + lh;
-                *(f32x4_t*)(mine + li * (PC * 4) + ((chunk ^ (li % PCH)) << 4)) = o;
+                *(f32x4_t*)(mine + li * (D * 4) + (((8 * i + 2 * r4 + lh) ^ (li % PCH)) << 4)) = o;
             }
+        if (lh == 0 && real) (p.runs > 1 ? z.part_lse : z.lse)[at] = l_tot != 0.f ? (m_run + fast_log2(l_tot)) * kLn2 : -INFINITY;
         wave_lds_fence();
-#pragma unroll
+        // a store covers whole rows; where a row goes is with the lane of its number
+#pragma unroll 4
         for (int u = 0; u < kPreQ * PCH / kWave; ++u) {
-            const int e = u * kWave + lane;
-            const int r = e / PCH, chunk = e % PCH;
-            const f32x4_t o = *(const f32x4_t*)(mine + r * (PC * 4) + ((chunk ^ (r % PCH)) << 4));
-            if (row_w + r < rq.R) *(f32x4_t*)(O + place(row_w + r) * D + c0 + chunk * 4) = o;
+            const int r = (u * kWave + lane) / PCH, chunk = lane % PCH;
+            const f32x4_t o = *(const f32x4_t*)(mine + r * (D * 4) + ((chunk ^ (r % PCH)) << 4));
+            const int64_t to = ((int64_t)__shfl((int)(at >> 32), r) << 32) | (uint32_t)__shfl((int)at, r);
+            if (row_w + r < rq.R) *(f32x4_t*)(O + to * D + chunk * 4) = o;
         }
-        wave_lds_fence();
-    }
-    if (lh == 0 && row_w + li < rq.R) lse[place(row)] = l_tot != 0.f ? (m_run + fast_log2(l_tot)) * kLn2 : -INFINITY;
+    };
+    finish(l);
 }
 
 hipError_t launch_paged_chunk(const PagedArgs& a, int D, int dtype, int64_t grid, hipStream_t stream) {

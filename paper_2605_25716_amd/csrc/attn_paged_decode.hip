@@ -41,7 +41,7 @@ FEDRAG_KERNEL __launch_bounds__(kDecThreads, 2) void paged_decode_kernel(const P
     // `p`: the tile; units u0 .. u0 + take of its n
     auto span = [&](const PagedSpan& p, uint32_t u0, uint32_t take) {
     const PagedRequest& q = p.req;
-    const int row0 = p.tile * a.cut.tile;                                  // the tile's first flattened row
+    const int row0 = p.tile << a.cut.tile_shift;                                  // the tile's first flattened row
     const int R = q.R - row0 < 16 ? q.R - row0 : 16;
     const int row = row0 + (lr < R ? lr : R - 1);
     const int lim = paged_limit(a, q, row);                                // this lane's row sees keys < lim
@@ -73,30 +73,33 @@ FEDRAG_KERNEL __launch_bounds__(kDecThreads, 2) void paged_decode_kernel(const P
     const int shift = a.pages.shift;
     const int n_tiles = (k_end - k_begin + kDecTile - 1) / kDecTile;
     const int n_mine = n_tiles > wave ? (n_tiles - wave + WAVES - 1) / WAVES : 0;
-    // page of half tile `lane` of this wave's 32 tiles from the i-th on; -1: none
-    auto load_ids = [&](int i) {
+    // lane l: bytes from K's or V's first page to half tile l of this wave's 32 tiles from the i-th on; < 0: there are no rows, or no
+    // page for them
+    auto offsets = [&](int i) {
         const int64_t key = (int64_t)k_begin + ((int64_t)wave + (int64_t)(i + lane / 2) * WAVES) * kDecTile + lane % 2 * 16;
         int id = -1;
         if (key < k_end) id = a.table[table0 + (key >> shift)];
-        return (uint32_t)id < a.pages.n_pages ? id : -1;
+        return (uint32_t)id < a.pages.n_pages
+                   ? (int64_t)id * a.pages.page_bytes + (((int64_t)p.head << shift) + ((int)key & ((1 << shift) - 1))) * ROWB : (int64_t)-1;
     };
-    int ids = -1;
-    auto fill = [&](int i, char* slot, bool is_k) {  // the wave's i-th tile, i within the 32 whose ids are here
-        const int key0 = k_begin + (wave + i * WAVES) * kDecTile;
+    int64_t offset = -1;
+    auto offset_of = [&](int half) {
+        return ((int64_t)__builtin_amdgcn_readlane((int)(offset >> 32), half) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)offset, half);
+    };
+    auto fill = [&](int i, char* slot, bool is_k) {  // the wave's i-th tile, i within the 32 whose offsets are here
+        const int left = k_end - k_begin - (wave + i * WAVES) * kDecTile;  // rows from its first one on
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int id = __builtin_amdgcn_readlane(ids, 2 * (i % 32) + h);
-            const int key = key0 + 16 * h;
-            const int left = (k_end - key < 16 ? k_end - key : 16) * ROWB;
-            const char* page = (is_k ? a.pages.K : a.pages.V) + (int64_t)(id < 0 ? 0 : id) * a.pages.page_bytes +
-                               (((int64_t)p.head << shift) + (key & ((1 << shift) - 1))) * ROWB;
-            const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void*)page, 0, id < 0 || left < 0 ? 0 : left, 0x00020000);
+            const int64_t off = offset_of(2 * (i % 32) + h);
+            const int bytes = off < 0 ? 0 : (left - 16 * h < 16 ? left - 16 * h : 16) * ROWB;
+            const __amdgpu_buffer_rsrc_t rs =
+                __builtin_amdgcn_make_buffer_rsrc((void*)((is_k ? a.pages.K : a.pages.V) + (off < 0 ? 0 : off)), 0, bytes, 0x00020000);
 #pragma unroll
             for (int j = 0; j < HL; ++j) {
                 const int r = lane / CH + j * RPW;
-                const int off = r * ROWB + (((lane % CH) ^ (is_k ? swz_k(r) : swz_v(r))) << 4);
+                const int at = r * ROWB + (((lane % CH) ^ (is_k ? swz_k(r) : swz_v(r))) << 4);
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(
-                    rs, (void __attribute__((address_space(3)))*)(slot + (h * HL + j) * (kWave * 16)), 16, off, 0, 0, 2);
+                    rs, (void __attribute__((address_space(3)))*)(slot + (h * HL + j) * (kWave * 16)), 16, at, 0, 0, 2);
             }
         }
     };
@@ -112,9 +115,9 @@ FEDRAG_KERNEL __launch_bounds__(kDecThreads, 2) void paged_decode_kernel(const P
     auto step = [&](int i, auto more) {
         constexpr bool MORE = decltype(more)::value;
         const int key0 = k_begin + (wave + i * WAVES) * kDecTile;
-        const int id0 = __builtin_amdgcn_readlane(ids, 2 * (i % 32)), id1 = __builtin_amdgcn_readlane(ids, 2 * (i % 32) + 1);
+        const int id0 = __builtin_amdgcn_readlane((int)(offset >> 32), 2 * (i % 32)), id1 = __builtin_amdgcn_readlane((int)(offset >> 32), 2 * (i % 32) + 1);
         const bool masked = key0 + kDecTile > (lim_min < k_end ? lim_min : k_end) || (id0 | id1) < 0;
-        if (MORE && i % 32 == 31) ids = load_ids(i + 1);
+        if (MORE && i % 32 == 31) offset = offsets(i + 1);
         wait_loads(std::integral_constant<int, KL>{});  // K's (V's are younger)
         f32x4_t s[2];
 #pragma unroll
@@ -226,7 +229,7 @@ FEDRAG_KERNEL __launch_bounds__(kDecThreads, 2) void paged_decode_kernel(const P
         }
     };
     if (n_mine > 0) {
-        ids = load_ids(0);
+        offset = offsets(0);
         fill(0, kslot, true);
         fill(0, vslot, false);
         __builtin_amdgcn_sched_barrier(0);
@@ -274,34 +277,29 @@ FEDRAG_KERNEL __launch_bounds__(kDecThreads, 2) void paged_decode_kernel(const P
         for (int e = 0; e < 4; ++e) num[e] = any ? num[e] / den : 0.f;
         const float lse = any ? (M + fast_log2(den)) * kLn2 : -INFINITY;
         const uint32_t t = FastDiv::div_by(z.by_g.m, z.by_g.s, (uint32_t)(row0 + n)), g = (uint32_t)(row0 + n) - t * z.by_g.d;
-        const int64_t at = part ? slot * z.cut.tile + n : ((int64_t)p.head * z.G + g) * z.T + q.begin + t;
+        const int64_t at = part ? (slot << z.cut.tile_shift) + n : ((int64_t)p.head * z.G + g) * z.T + q.begin + t;
         *(f32x4_t*)((part ? z.part_O : z.O) + at * D + c) = num;
         if (c == 0) (part ? z.part_lse : z.lse)[at] = lse;
     }
     };
-    // Where the next share begins, where this one does, then its spans; one search in the code for all of them.
-    uint32_t pos = (blockIdx.x + 1) * shares.share, end = 0;
-    for (int stage = 0;;) {
-        PagedArgsLate& z = late_args();
-        const PagedSpan p = shares.find(z, pos);
-        if (stage < 2) {
-            // a share begins behind the few units that it lies among
-            const uint32_t begin = p.b < 0 ? shares.total : pos == p.begin || p.n > shares.whole ? pos : p.begin + p.n;
-            pos = begin;
-            if (stage++ == 0) {
-                end = begin;
-                pos = blockIdx.x * shares.share;
-                continue;
-            }
-            if (pos >= end) return;
-            if (p.b < 0 || pos >= p.begin + p.n) continue;
-        }
+    uint32_t pos = blockIdx.x * shares.share;
+    const uint32_t end = pos + shares.share;
+    for (bool first = true;; first = false) {
+        const PagedSpan p = shares.find(late_args(), pos);
         if (p.b < 0) return;
-        const uint32_t u0 = pos - p.begin, take = end - pos < p.n - u0 ? end - pos : p.n - u0;
-        span(p, u0, take);
-        pos += take;
+        uint32_t take = p.begin + p.n - pos;
+        if (p.n <= shares.whole) {
+            // not cut: the share before has it, if it began there
+            if (first && pos != p.begin) take |= 0x80000000u;
+        } else if (end - pos < take) {
+            take = end - pos;
+        }
+        if (!(take >> 31)) {
+            if (!first) __syncthreads();  // the slots have been read by all, and are filled again
+            span(p, pos - p.begin, take);
+        }
+        pos += take & 0x7fffffff;
         if (pos >= end) return;
-        __syncthreads();  // the slots have been read by all, and are filled again
     }
 }
 

@@ -209,7 +209,7 @@ FEDRAG_KERNEL __launch_bounds__(256, 2) void paged_f32_kernel(const PagedArgs a)
 #pragma unroll
         for (int e = 0; e < 4; ++e) num[e] = any ? num[e] * inv : 0.f;
         const uint32_t t = a.by_g.div((uint32_t)(row0 + n)), g = (uint32_t)(row0 + n) - t * a.by_g.d;
-        const int64_t at = p.runs > 1 ? (int64_t)p.slot * a.cut.tile + n : ((int64_t)p.head * a.G + g) * a.T + rq.begin + t;
+        const int64_t at = p.runs > 1 ? ((int64_t)p.slot << a.cut.tile_shift) + n : ((int64_t)p.head * a.G + g) * a.T + rq.begin + t;
         *(f32x4_t*)((p.runs > 1 ? a.part_O : a.O) + at * D + c) = num;
         if (c == 0) (p.runs > 1 ? a.part_lse : a.lse)[at] = any ? M + logf(den) : -INFINITY;
     }
@@ -217,7 +217,7 @@ FEDRAG_KERNEL __launch_bounds__(256, 2) void paged_f32_kernel(const PagedArgs a)
 
 hipError_t launch_paged_f32(const PagedArgs& a, int D, int, int64_t grid, hipStream_t stream) {
     if (!grid_fits(grid, 256)) return hipErrorInvalidValue;
-    const bool wide = a.cut.tile == 32;
+    const bool wide = a.cut.tile_shift == 5;
     const auto kernel = D == 128 ? (wide ? paged_f32_kernel<128, 2> : paged_f32_kernel<128, 1>)
                                  : (wide ? paged_f32_kernel<64, 2> : paged_f32_kernel<64, 1>);
     hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(256), 0, stream, a);

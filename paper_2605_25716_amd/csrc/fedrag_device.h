@@ -15,6 +15,8 @@ typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x4_t __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2_vec_t __attribute__((ext_vector_type(2)));
 typedef float f32x2_t __attribute__((ext_vector_type(2)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
@@ -42,6 +44,12 @@ struct BF16 {
     }
     static __device__ __forceinline__ elem from_float(float x) { return static_cast<__bf16>(x); }
     static __device__ __forceinline__ float to_float(elem x) { return static_cast<float>(x); }
+    // Two values in a word, each rounded to nearest even, and each of them again.
+    static __device__ __forceinline__ uint32_t pack(float x, float y) {
+        return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{x, y}), bf16x2_t));
+    }
+    static __device__ __forceinline__ float low(uint32_t w) { return __builtin_bit_cast(float, w << 16); }
+    static __device__ __forceinline__ float high(uint32_t w) { return __builtin_bit_cast(float, w & 0xffff0000u); }
 };
 
 struct F16 {
@@ -56,6 +64,11 @@ struct F16 {
     }
     static __device__ __forceinline__ elem from_float(float x) { return static_cast<_Float16>(x); }
     static __device__ __forceinline__ float to_float(elem x) { return static_cast<float>(x); }
+    static __device__ __forceinline__ uint32_t pack(float x, float y) {
+        return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{x, y}), f16x2_vec_t));
+    }
+    static __device__ __forceinline__ float low(uint32_t w) { return (float)__builtin_bit_cast(f16x2_vec_t, w)[0]; }
+    static __device__ __forceinline__ float high(uint32_t w) { return (float)__builtin_bit_cast(f16x2_vec_t, w)[1]; }
 };
 
 template <class V>
@@ -211,6 +224,11 @@ typedef short s16x4_t __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ u32x2_t lds_read_tr16(const char* p) {
     const s16x4_t v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4_t __attribute__((address_space(3)))*)p);
     return __builtin_bit_cast(u32x2_t, v);
+}
+
+// 16 bytes a lane from its own address to `to` + 16 * lane, `to` the same in all lanes.
+__device__ __forceinline__ void copy_to_lds(const char* from, char* to) {
+    __builtin_amdgcn_global_load_lds((void __attribute__((address_space(1)))*)from, (void __attribute__((address_space(3)))*)to, 16, 0, 0);
 }
 
 // exp2(a - b) with the convention that a == -inf gives 0 even when b == -inf.

@@ -235,6 +235,7 @@ SETS = {
     "chunk_128": ([127, 129], [300, 129]),
     "chunk_long": ([40], [2100]),
     "more_rows_than_keys": ([20, 3, 70], [7, 0, 65]),
+    "rows_that_see_nothing_of_runs": ([500, 2], [300, 700]),
     "mixed": ([1, 50, 0, 1, 5], [300, 50, 12, 17, 400]),
 }
 
