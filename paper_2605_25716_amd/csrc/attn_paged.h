@@ -11,10 +11,11 @@ namespace fedrag {
 // KV head (row r = token r / G, head r % G of the group), in tiles of 2^tile_shift rows, and n = ceil(keys / unit) units of keys (at least
 // one: a row without keys has an output all the same) for each of them.  All units together are below 2^31, which the host sees
 // to by way of `unit_shift`.  There are two ways to cut:
-//   runs    a tile's keys in equal runs of at most `per` = max(least, ceil(units of all / target)); a workgroup takes one.
+//   runs    a tile's keys in equal runs of about `per` = max(least, ceil(units of all / target)), as many as n / per rounds to; a
+//           workgroup takes one.
 //             runs         <= target + tiles of all requests and heads   (the grid),
-//             split runs   <= 2 target                                   (a tile in two or more has n > per: their partials),
-//             split tiles  <= target                                     (what the aggregation has to visit);
+//             split runs   <= 4 / 3 target                               (a tile in two or more has n >= 1.5 per: their partials),
+//             split tiles  <= 2 / 3 target                               (what the aggregation has to visit);
 //   shares  the units of all tiles in a row, and an even share of them to each workgroup, wherever in a tile it begins and ends:
 //           all workgroups end together, whatever the lengths.  For kernels whose partials are small.
 // `target` is a power of two.
@@ -38,11 +39,12 @@ struct PagedArgs {
     PagedCut cut;
 };
 
-// The arguments (of a kernel whose first they are), read again from memory from here on: what is needed between inner loops would
+// Arguments number N of a kernel, all of this type, read again from memory from here on: what is needed between inner loops would
 // otherwise sit in scalar registers throughout, and those that do not fit in lanes of vector registers or in scratch memory.
 typedef const __attribute__((address_space(4))) PagedArgs PagedArgsLate;
+template <int N>
 __device__ __forceinline__ PagedArgsLate& late_args() {
-    PagedArgsLate* p = (PagedArgsLate*)__builtin_amdgcn_kernarg_segment_ptr();
+    PagedArgsLate* p = (PagedArgsLate*)__builtin_amdgcn_kernarg_segment_ptr() + N;
     asm volatile("" : "+s"(p));
     return *p;
 }
@@ -141,8 +143,9 @@ struct PagedPiece {
 
 // Piece `index` of the launch, or (SPLIT) of its split tiles; each wave finds it by itself.  The pieces of a request: tile by
 // tile, the last one first (with a mask the longest), run by run, the heads innermost: workgroups are dealt to the XCDs in turn, so
-// with 8 KV heads the pieces that read the same keys share an L2.  Up to 64 requests go side by side, all their last tiles, then all
-// those before, so that long pieces start early (4 x 1000 tokens of 32 heads of 128 88 -> 83 us).
+// with 8 KV heads the pieces that read the same keys share an L2.  Up to 64 requests go side by side, so that long pieces start
+// early: the order is that of the pieces' lengths, which with a mask fall from tile to tile (4 x 1000 tokens of 32 heads of 128 one
+// request after the other 88 us, 80).
 template <bool SPLIT, class Args>
 __device__ __forceinline__ PagedPiece paged_piece(Args& a, uint32_t index) {
     PagedRequest one{};
@@ -156,7 +159,7 @@ __device__ __forceinline__ PagedPiece paged_piece(Args& a, uint32_t index) {
     per = per > (uint32_t)a.cut.least ? per : (uint32_t)a.cut.least;
     auto runs_of = [&](const PagedRequest& r) {
         const uint32_t n = paged_units(a, r);
-        return n <= per ? 1 : (n + per - 1) / per;
+        return 2 * n < 3 * per ? 1 : (n + per / 2) / per;
     };
     auto pieces_of = [&](const PagedRequest& r) {
         const uint32_t runs = runs_of(r), n = paged_tiles(a, r) * (uint32_t)a.Hkv;
@@ -181,21 +184,30 @@ __device__ __forceinline__ PagedPiece paged_piece(Args& a, uint32_t index) {
     p.head = (int)(index - group * a.by_hkv.d);
     if (!SPLIT && k == 1) {
         const uint32_t tiles = (int)threadIdx.x % kWave < a.B ? paged_tiles(a, one) : 0, runs = runs_of(one);
-        auto below = [&](uint32_t level) { return lane_value(wave_scan((tiles < level ? tiles : level) * runs), kWave - 1); };
+        // a piece's place in the order: its length behind the longest's in key units, as tiles, and with a mask also its tile
+        const uint32_t len = tiles ? (paged_units(a, one) + runs - 1) / runs : 0;
+        const uint32_t ahead = (uint32_t)((uint64_t)(wave_max(len) - len) * (uint32_t)a.G << a.cut.unit_shift >> a.cut.tile_shift);
+        auto before_level = [&](uint32_t level) {  // groups of this lane's request before it
+            const uint32_t v = level > ahead ? level - ahead : 0;
+            return (!a.causal && v > 0) || v > tiles ? tiles * runs : v * runs;
+        };
+        auto below = [&](uint32_t level) { return lane_value(wave_scan(before_level(level)), kWave - 1); };
         uint32_t level = 0;  // the most whose groups all lie before this one
-        for (uint32_t bit = (uint32_t)1 << (31 - __builtin_clz(((uint32_t)a.T * (uint32_t)a.G >> a.cut.tile_shift) + 1)); bit; bit >>= 1)
+        for (uint32_t bit = (uint32_t)1 << (31 - __builtin_clz(wave_max(tiles ? tiles + ahead : 0) | 1)); bit; bit >>= 1)
             if (below(level + bit) <= group) level += bit;
-        const uint32_t here = wave_scan(tiles > level ? runs : 0);
+        const uint32_t here = wave_scan(before_level(level + 1) - before_level(level));
         group -= below(level);
         p.b = __builtin_popcountll(__builtin_amdgcn_ballot_w64(here <= group));
         if (p.b >= kWave) {  // (only by a q_start that decreases)
             p.b = -1;
             return p;
         }
-        p.run = (int)(group - (p.b ? lane_value(here, p.b - 1) : 0));
+        group -= p.b ? lane_value(here, p.b - 1) : 0;
         p.req = lane_request(one, p.b);
         slot = p.b ? lane_value(split_to, p.b - 1) : 0;
-        before = level;
+        const uint32_t n_runs = runs_of(p.req);
+        before = a.causal ? level - lane_value(ahead, p.b) : group / n_runs;
+        p.run = (int)(a.causal ? group : group - before * n_runs);
     } else {
         const int at = __builtin_popcountll(__builtin_amdgcn_ballot_w64(to <= group * (uint32_t)a.Hkv));
         uint32_t base;
@@ -282,8 +294,8 @@ __device__ __forceinline__ int paged_limit(const PagedArgs& a, const PagedReques
     return own < 0 ? 0 : (own < q.keys ? (int)own : q.keys);
 }
 
-hipError_t launch_paged_decode(const PagedArgs& a, int D, int dtype, int64_t grid, hipStream_t stream);
-hipError_t launch_paged_f32(const PagedArgs& a, int D, int dtype, int64_t grid, hipStream_t stream);
-hipError_t launch_paged_chunk(const PagedArgs& a, int D, int dtype, int64_t grid, hipStream_t stream);
+// 16-bit storage: workgroups for requests of many rows (a, unless `chunks` is 0) and for those of few (d, unless `decodes` is 0).
+hipError_t launch_paged_16(const PagedArgs& a, int64_t chunks, const PagedArgs& d, int64_t decodes, int D, int dtype, hipStream_t stream);
+hipError_t launch_paged_f32(const PagedArgs& a, int64_t grid, int D, hipStream_t stream);
 
 }  // namespace fedrag

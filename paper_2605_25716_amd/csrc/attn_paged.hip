@@ -5,11 +5,11 @@ namespace fedrag {
 
 // The aggregation (Section 4.1) of the tiles whose keys are in several partials: a workgroup takes 8 or 16 rows of one of them, a
 // thread 4 columns of a row.  The lanes of a row share out the weights, 16 partials at a time.
-// Which tile: SHARES: the one that workgroup blockIdx.x + 1's share begins inside of, if no share before does; else the
-// blockIdx.x-th of those in several runs.
+// Which tile: SHARES: the one that workgroup index + 1's share begins inside of, if no share before does; else the index-th of
+// those in several runs.
 constexpr int kPagedMergeThreads = 256;
 template <int D, bool SHARES>
-FEDRAG_KERNEL __launch_bounds__(kPagedMergeThreads) void paged_merge_kernel(const PagedArgs a) {
+__device__ __forceinline__ void paged_merge(const PagedArgs& a, uint32_t index, int part) {
     constexpr int TPR = D / 4;
     PagedRequest req;
     int tile, head, S = 0;
@@ -17,7 +17,7 @@ FEDRAG_KERNEL __launch_bounds__(kPagedMergeThreads) void paged_merge_kernel(cons
     if constexpr (SHARES) {
         __shared__ PagedLanes lanes;
         const PagedShares<const PagedArgs> shares(a, lanes);
-        const uint32_t w = blockIdx.x + 1, pos = w * shares.share;
+        const uint32_t w = index + 1, pos = w * shares.share;
         const PagedSpan p = shares.find(a, pos);
         if (p.b < 0 || pos == p.begin || p.n <= shares.whole) return;
         const uint32_t w0 = p.begin / shares.share;
@@ -31,7 +31,7 @@ FEDRAG_KERNEL __launch_bounds__(kPagedMergeThreads) void paged_merge_kernel(cons
         step = 2;
         first = slot + 1;
     } else {
-        const PagedPiece p = paged_piece<true>(a, blockIdx.x);
+        const PagedPiece p = paged_piece<true>(a, index);
         if (p.b < 0 || p.slot + (uint32_t)(p.runs - 1) * (uint32_t)a.Hkv >= a.slots) return;  // (the latter where q_start decreases)
         req = p.req;
         tile = p.tile;
@@ -40,7 +40,7 @@ FEDRAG_KERNEL __launch_bounds__(kPagedMergeThreads) void paged_merge_kernel(cons
         step = a.Hkv;
         S = p.per;  // units of a run, for now
     }
-    const int row0 = tile << a.cut.tile_shift, n = blockIdx.y * (kPagedMergeThreads / TPR) + threadIdx.x / TPR;
+    const int row0 = tile << a.cut.tile_shift, n = part * (kPagedMergeThreads / TPR) + threadIdx.x / TPR;
     const int c = threadIdx.x % TPR, k = c % 16, group = threadIdx.x % kWave & 48;
     const int last = (row0 + (1 << a.cut.tile_shift) < req.R ? row0 + (1 << a.cut.tile_shift) : req.R) - 1;
     if (row0 + n > last) return;
@@ -82,14 +82,31 @@ FEDRAG_KERNEL __launch_bounds__(kPagedMergeThreads) void paged_merge_kernel(cons
     if (c == 0) a.lse[at] = any ? M + logf(den) : -INFINITY;
 }
 
+// Tiles in runs (a), then tiles cut by shares (d), each in several workgroups: first every tile's first rows, and so on, so that
+// with 8 KV heads a workgroup runs on the XCD that wrote its partials (the tiles' own order has the heads innermost, too).
+// KIND: 1 shares, 2 runs, 3 both (which of the two comes first is another trip to the arguments: 0.7 us of a short call).
+template <int D, int KIND>
+FEDRAG_KERNEL __launch_bounds__(kPagedMergeThreads) void paged_merge_kernel(const PagedArgs a, const PagedArgs d, uint32_t a_wgs, FastDiv tiles_a,
+                                                                            FastDiv tiles_d) {
+    const uint32_t i = blockIdx.x;
+    if (KIND == 2 || (KIND == 3 && i < a_wgs)) {
+        const uint32_t part = tiles_a.div(i);
+        paged_merge<D, false>(a, i - part * tiles_a.d, (int)part);
+    } else {
+        const uint32_t part = tiles_d.div(i - a_wgs);
+        paged_merge<D, true>(d, i - a_wgs - part * tiles_d.d, (int)part);
+    }
+}
+
 // ------------------------------------------------------------------------------------------------ the launches
-// What a launch may need, from the sizes the host knows.
+// What a form of the work may need, from the sizes the host knows.
 struct PagedLaunch {
     PagedCut cut;
-    int64_t grid;    // at least the pieces
-    int64_t slots;   // at least the split pieces
-    int64_t merges;  // at least the split tiles
-    bool shares;
+    int64_t grid;    // at least the pieces; 0: this form is not launched
+    int64_t slots;   // at least the partials
+    int64_t merges;  // at least the tiles in several partials
+    size_t bytes(int D) const { return (((size_t)slots << cut.tile_shift) * (D + 1) * 4 + 15) / 16 * 16; }
+    int64_t merge_groups(int D) const { return ((D / 4 << cut.tile_shift) + kPagedMergeThreads - 1) / kPagedMergeThreads; }
 };
 constexpr int kPagedDecodeRows = 16;  // a tile of the kernel for few rows
 
@@ -104,57 +121,49 @@ static int64_t paged_units_of(PagedCut& cut, int64_t tiles, int64_t keys) {
 static PagedLaunch paged_runs(PagedCut cut, int64_t tiles, int64_t keys) {
     const int64_t target = (int64_t)1 << cut.target_shift;
     const int64_t units = paged_units_of(cut, tiles, keys);
-    const int64_t most_runs = units > cut.least ? (units + cut.least - 1) / cut.least : 1;
-    PagedLaunch l;
+    const int64_t most_runs = (units + cut.least / 2) / cut.least > 1 ? (units + cut.least / 2) / cut.least : 1;
+    PagedLaunch l{};
     l.cut = cut;
     l.grid = target + tiles < tiles * most_runs ? target + tiles : tiles * most_runs;
     l.slots = most_runs == 1 ? 0 : (l.grid < 2 * target ? l.grid : 2 * target);
     l.merges = most_runs == 1 ? 0 : (tiles < target ? tiles : target);
-    l.shares = false;
     return l;
 }
 static PagedLaunch paged_shares(PagedCut cut, int64_t tiles, int64_t keys) {
     const int64_t target = (int64_t)1 << cut.target_shift;
     const int64_t units = paged_units_of(cut, tiles, keys);
     const int64_t total = tiles * units;
-    PagedLaunch l;
+    PagedLaunch l{};
     l.cut = cut;
     l.grid = (total + cut.least - 1) / cut.least < target ? (total + cut.least - 1) / cut.least : target;
     l.slots = units <= cut.least ? 0 : 2 * l.grid;
     l.merges = units <= cut.least ? 0 : l.grid - 1;
-    l.shares = true;
     return l;
 }
-static size_t paged_bytes(const PagedLaunch& l, int D) { return (((size_t)l.slots << l.cut.tile_shift) * (D + 1) * 4 + 15) / 16 * 16; }
 
-// The launches of a call.  16-bit storage: requests of few rows, of many, or both, where the host cannot know that there are
-// none; fp32: one form for all, of 16 or 32 rows.
+// The forms of a call.  16-bit storage: requests of many rows (in runs), of few (in shares), or both, where the host cannot know that
+// there are none; fp32: one form for all, of 16 or 32 rows, in runs.
 struct PagedPlan {
-    int n;
-    PagedLaunch l[2];
-    hipError_t (*kernel[2])(const PagedArgs&, int, int, int64_t, hipStream_t);
-    size_t bytes(int D) const { return (n > 0 ? paged_bytes(l[0], D) : 0) + (n > 1 ? paged_bytes(l[1], D) : 0); }
+    PagedLaunch runs, shares;
+    size_t bytes(int D) const { return runs.bytes(D) + shares.bytes(D); }
 };
 static PagedPlan paged_plan(int B, int Hq, int Hkv, int dtype, int64_t T, int64_t keys, int64_t max_q_len) {
     const int64_t G = Hq / Hkv, some = B < T ? B : T;
     // at least the tiles that T rows of B requests come to
     auto tiles = [&](int tile_shift) { return ((T * G >> tile_shift) + some) * Hkv; };
     const int64_t most = max_q_len > 0 && max_q_len < T ? max_q_len : T;
-    const int shift = 63 - __builtin_clzll(2 * (uint64_t)attn_target_wgs());  // two workgroups to a compute unit, rounded down
+    const int cus = 63 - __builtin_clzll((uint64_t)attn_target_wgs());  // compute units, rounded down to a power of two
     const bool many = most * G > kPagedDecodeRows, few = !many || B > 1;
     PagedPlan p{};
-    auto add = [&](auto kernel, auto how, int tile_shift, int unit_shift, int least, int from, int to, int64_t most_tiles) {
-        p.l[p.n] = how(PagedCut{tile_shift, unit_shift, least, shift, from, to}, most_tiles, keys);
-        p.kernel[p.n++] = kernel;
-    };
     if (dtype == FEDRAG_F32) {
         const int tile = many ? 5 : 4;
-        add(launch_paged_f32, paged_runs, tile, 6, 4, 1, INT32_MAX, tiles(tile));
+        p.runs = paged_runs(PagedCut{tile, 6, 4, cus + 1, 1, INT32_MAX}, tiles(tile), keys);
         return p;
     }
-    if (many) add(launch_paged_chunk, paged_runs, 7, 6, 4, few ? kPagedDecodeRows + 1 : 1, INT32_MAX, tiles(7));
+    if (many) p.runs = paged_runs(PagedCut{7, 6, 4, cus + 1, few ? kPagedDecodeRows + 1 : 1, INT32_MAX}, tiles(7), keys);
+    // beside requests of many rows: one workgroup to a compute unit, for as long as the others take
     if (few)
-        add(launch_paged_decode, paged_shares, 4, 8, 1, 1, many ? kPagedDecodeRows : INT32_MAX, many ? some * Hkv : tiles(4));
+        p.shares = paged_shares(PagedCut{4, 8, 1, many ? cus : cus + 1, 1, many ? kPagedDecodeRows : INT32_MAX}, many ? some * Hkv : tiles(4), keys);
     return p;
 }
 
@@ -162,16 +171,6 @@ size_t paged_attn_workspace_bytes(int B, int Hq, int Hkv, int D, int dtype, int6
                                   int64_t max_q_len) {
     if (T == 0 || B == 0) return 0;
     return paged_plan(B, Hq, Hkv, dtype, T, max_pages * page_tokens, max_q_len).bytes(D);
-}
-
-static hipError_t launch_paged_merge(const PagedArgs& a, const PagedLaunch& l, int D, hipStream_t stream) {
-    const int64_t groups = ((D / 4 << l.cut.tile_shift) + kPagedMergeThreads - 1) / kPagedMergeThreads;
-    if (!grid_fits(l.merges * groups, kPagedMergeThreads)) return hipErrorInvalidValue;
-    const auto kernel = l.shares ? (D == 128 ? paged_merge_kernel<128, true> : paged_merge_kernel<64, true>)
-                                 : (D == 128 ? paged_merge_kernel<128, false> : paged_merge_kernel<64, false>);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)l.merges, (unsigned)groups),
-                       dim3(kPagedMergeThreads), 0, stream, a);
-    return hipGetLastError();
 }
 
 hipError_t launch_paged_attn(const PagedAttnProblem& p, hipStream_t stream) {
@@ -197,19 +196,27 @@ hipError_t launch_paged_attn(const PagedAttnProblem& p, hipStream_t stream) {
     a.O = p.O;
     a.lse = p.lse;
     const PagedPlan plan = paged_plan(p.B, p.Hq, p.Hkv, p.dtype, p.T, p.max_pages << p.pages.shift, p.max_q_len);
-    char* scratch = (char*)p.workspace;
-    for (int i = 0; i < plan.n; ++i) {
-        const PagedLaunch& l = plan.l[i];
-        a.cut = l.cut;
-        a.slots = (uint32_t)l.slots;
-        a.part_O = (float*)scratch;
-        a.part_lse = a.part_O + (l.slots << l.cut.tile_shift) * p.D;
-        scratch += paged_bytes(l, p.D);
-        hipError_t e = plan.kernel[i](a, p.D, p.dtype, l.grid, stream);
-        if (e == hipSuccess && l.merges > 0) e = launch_paged_merge(a, l, p.D, stream);
-        if (e != hipSuccess) return e;
-    }
-    return hipSuccess;
+    auto with = [&](const PagedLaunch& l, char* scratch) {
+        PagedArgs x = a;
+        x.cut = l.cut;
+        x.slots = (uint32_t)l.slots;
+        x.part_O = (float*)scratch;
+        x.part_lse = x.part_O + (l.slots << l.cut.tile_shift) * p.D;
+        return x;
+    };
+    const PagedArgs runs = with(plan.runs, (char*)p.workspace), shares = with(plan.shares, (char*)p.workspace + plan.runs.bytes(p.D));
+    const int64_t wgs_r = plan.runs.merges * plan.runs.merge_groups(p.D), wgs_s = plan.shares.merges * plan.shares.merge_groups(p.D);
+    if (wgs_r + wgs_s > 0 && !grid_fits(wgs_r + wgs_s, kPagedMergeThreads)) return hipErrorInvalidValue;
+    const hipError_t e = p.dtype == FEDRAG_F32 ? launch_paged_f32(runs, plan.runs.grid, p.D, stream)
+                                               : launch_paged_16(runs, plan.runs.grid, shares, plan.shares.grid, p.D, p.dtype, stream);
+    if (e != hipSuccess || wgs_r + wgs_s == 0) return e;
+#define FEDRAG_MERGE(KIND) (p.D == 128 ? paged_merge_kernel<128, KIND> : paged_merge_kernel<64, KIND>)
+    const auto merge = wgs_r == 0 ? FEDRAG_MERGE(1) : wgs_s == 0 ? FEDRAG_MERGE(2) : FEDRAG_MERGE(3);
+#undef FEDRAG_MERGE
+    hipLaunchKernelGGL(merge, dim3((unsigned)(wgs_r + wgs_s)), dim3(kPagedMergeThreads), 0,
+                       stream, runs, shares, (uint32_t)wgs_r, FastDiv(plan.runs.merges > 0 ? plan.runs.merges : 1),
+                       FastDiv(plan.shares.merges > 0 ? plan.shares.merges : 1));
+    return hipGetLastError();
 }
 
 }  // namespace fedrag

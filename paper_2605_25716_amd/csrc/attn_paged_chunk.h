@@ -14,14 +14,16 @@
 //       C(t-1): O^T += V(t-1)^T P^T     with B1(t):   maximum, rescale factor and probabilities of keys 0..31 of tile t.
 //   * Tiles are visited from the last to the first: those that some row does not see whole (the diagonal, the end of the request)
 //     come first and are finished one by one, up to the last of them, with which the pipeline starts.
+#pragma once
 #include "attn_paged.h"
 
 namespace fedrag {
 
-constexpr int kAheadK = 4, kAheadV = 3;  // operands are read from LDS so many before they are used
-
-template <class T, int D, int NW>
-FEDRAG_KERNEL __launch_bounds__(NW * kWave, 2) void paged_chunk_kernel(const PagedArgs a, float scale_log2) {
+// ks0 .. vs1: an array each per tile slot, so that the compiler sees that the loads filling one do not alias the reads of another.
+// AHEAD: V operands are read from LDS so many before they are used; K operands four.  (Three of V take the registers that are left
+// at 128 columns; the other form beside it takes two more for its scalars.)
+template <class T, int D, int NW, int ARGS, int AHEAD>
+__device__ __forceinline__ void paged_chunk_body(const PagedArgs& a, uint32_t index, char* ks0, char* ks1, char* vs0, char* vs1, int& sm_odd) {
     typedef typename T::elem elem;
     typedef typename T::vec8 vec8;
     constexpr int kThreads = NW * kWave;
@@ -33,14 +35,12 @@ FEDRAG_KERNEL __launch_bounds__(NW * kWave, 2) void paged_chunk_kernel(const Pag
     constexpr int RPW = kWave / CH;         // rows per load of a wave
     constexpr int LPT = kPreK / (NW * RPW); // loads per wave and tile
     constexpr int IDT = kWave / LPT;        // tiles whose page ids a wave holds
-    __shared__ __attribute__((aligned(16))) char ks0[SLOT], ks1[SLOT], vs0[SLOT], vs1[SLOT];
-    __shared__ int sm_odd;
-
+    const float scale_log2 = a.scale * kLog2e;
     const int tid = threadIdx.x;
     const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int lane = tid % kWave;
     const int li = lane % 32, lh = lane / 32;
-    const PagedPiece p = paged_piece<false>(a, blockIdx.x);
+    const PagedPiece p = paged_piece<false>(a, index);
     if (p.b < 0) return;
     const PagedRequest& rq = p.req;
     const int row0 = p.tile * (NW * kPreQ);
@@ -218,15 +218,15 @@ FEDRAG_KERNEL __launch_bounds__(NW * kWave, 2) void paged_chunk_kernel(const Pag
 #pragma unroll
             for (int i = 0; i < KS; ++i) k_off[i] = kb ^ (32 * i);
 #pragma unroll
-            for (int j = 0; j < kAheadK; ++j) kop[j] = *(const vec8*)(kt + (j % 2) * 32 * ROWB + k_off[j / 2]);
+            for (int j = 0; j < 4; ++j) kop[j] = *(const vec8*)(kt + (j % 2) * 32 * ROWB + k_off[j / 2]);
             S0 = zero_vec<f32x16_t>();
             S1[c] = zero_vec<f32x16_t>();
             float psum = 0.f;
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int j = 0; j < NA; ++j) {
-                if (j + kAheadK < NA)
-                    kop[j + kAheadK] = *(const vec8*)(kt + ((j + kAheadK) % 2) * 32 * ROWB + k_off[(j + kAheadK) / 2]);
+                if (j + 4 < NA)
+                    kop[j + 4] = *(const vec8*)(kt + ((j + 4) % 2) * 32 * ROWB + k_off[(j + 4) / 2]);
                 if (j % 2 == 0) S0 = T::mfma32(kop[j], qop[j / 2], S0);
                 else S1[c] = T::mfma32(kop[j], qop[j / 2], S1[c]);
                 if constexpr (doC) {
@@ -293,7 +293,7 @@ FEDRAG_KERNEL __launch_bounds__(NW * kWave, 2) void paged_chunk_kernel(const Pag
             vec8 vop[NM];
             if constexpr (doC) {
 #pragma unroll
-                for (int j = 0; j < kAheadV; ++j) vop[j] = read_vop(vt, j / MT, j % MT);
+                for (int j = 0; j < AHEAD; ++j) vop[j] = read_vop(vt, j / MT, j % MT);
             }
             float mx = -INFINITY;
             float m_new = 0.f, psum = 0.f;
@@ -330,7 +330,7 @@ FEDRAG_KERNEL __launch_bounds__(NW * kWave, 2) void paged_chunk_kernel(const Pag
                 if constexpr (doC) {
                     // of each four: tiles i, i + 1 with the first terms, then with the second
                     const int at = j / 4 * 2 + j % 2, kk = at / MT, i = at % MT;
-                    if (j % 4 < 2 && at + kAheadV < NM) vop[at + kAheadV] = read_vop(vt, (at + kAheadV) / MT, (at + kAheadV) % MT);
+                    if (j % 4 < 2 && at + AHEAD < NM) vop[at + AHEAD] = read_vop(vt, (at + AHEAD) / MT, (at + AHEAD) % MT);
                     acc_o[i] = T::mfma32(vop[at], operand(j % 4 < 2 ? P[o][kk] : Plo[o][kk]), acc_o[i]);
                 }
 #pragma unroll
@@ -449,7 +449,7 @@ FEDRAG_KERNEL __launch_bounds__(NW * kWave, 2) void paged_chunk_kernel(const Pag
         const int li = lane % 32, lh = lane / 32;
         const int slot_w = wave * 4 / NW;
         char* mine = (slot_w == 0 ? ks0 : slot_w == 1 ? ks1 : slot_w == 2 ? vs0 : vs1) + (wave % (NW / 4)) * WB;
-        const PagedArgsLate& z = late_args();
+        const PagedArgsLate& z = late_args<ARGS>();
         const int r_in = row_w - row0 + li;  // this lane's row in the tile
         const bool real = row_w + li < rq.R;
         // its partial's place, or its own in O and lse: row t / G of head t % G
@@ -478,15 +478,6 @@ FEDRAG_KERNEL __launch_bounds__(NW * kWave, 2) void paged_chunk_kernel(const Pag
         }
     };
     finish(l);
-}
-
-hipError_t launch_paged_chunk(const PagedArgs& a, int D, int dtype, int64_t grid, hipStream_t stream) {
-    constexpr int NW = 4;
-    if (!grid_fits(grid, NW * kWave)) return hipErrorInvalidValue;
-    const auto kernel = dtype == FEDRAG_BF16 ? (D == 128 ? paged_chunk_kernel<BF16, 128, NW> : paged_chunk_kernel<BF16, 64, NW>)
-                                             : (D == 128 ? paged_chunk_kernel<F16, 128, NW> : paged_chunk_kernel<F16, 64, NW>);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(NW * kWave), 0, stream, a, a.scale * kLog2e);
-    return hipGetLastError();
 }
 
 }  // namespace fedrag

@@ -13,31 +13,37 @@
 //   which are also its contraction slice of O^T (d x 16) += V^T (d x 32) . P^T (32 x 16), whose V^T operands come through
 //   the transposing LDS read.
 // Probabilities enter the second product as two storage-type terms (about 16 significant bits): outputs are fp32.
+#pragma once
 #include "attn_paged.h"
 
 namespace fedrag {
 
-template <class T, int D>
-FEDRAG_KERNEL __launch_bounds__(kDecThreads, 2) void paged_decode_kernel(const PagedArgs a, float scale_log2) {
+// The LDS of a workgroup, shared with the other form (attn_paged_chunk.h): tiles of K and of V, an array for every two waves.
+template <int D>
+struct PagedSmall {
+    float m[kDecWaves][16], l[kDecWaves][16];
+    PagedLanes lanes;
+};
+// Wave w's slot of two arrays (by value: a choice between variables that a lambda holds puts them in scratch memory).
+__device__ __forceinline__ char* paged_slot(char* first, char* second, int w, int bytes) { return (w < 2 ? first : second) + w % 2 * bytes; }
+// ARGS: which of the kernel's arguments `a` is.
+template <class T, int D, int ARGS>
+__device__ __forceinline__ void paged_decode_body(const PagedArgs& a, uint32_t index, char* ks0, char* ks1, char* vs0, char* vs1, PagedSmall<D>& sm) {
     typedef typename T::elem elem;
     typedef typename T::vec8 vec8;
     constexpr int KS = D / 32;   // contraction steps of the first product
     constexpr int DCH = D / 16;  // 16-row tiles of O^T
     constexpr int ROWB = D * 2;
-    constexpr int TILEB = kDecTile * ROWB;
+    constexpr int SLOT = kDecTile * ROWB;
     constexpr int WAVES = kDecWaves;
     constexpr int OROW = (D + 4) * 4;
-    constexpr int SLOT = TILEB > 8 * OROW ? TILEB : 8 * OROW;
-    __shared__ __attribute__((aligned(16))) char ks[WAVES][SLOT], vs[WAVES][SLOT];
-    __shared__ float sm_m[WAVES][16], sm_l[WAVES][16];
-    auto out_row = [&](int w, int n) { return (float*)((n < 8 ? ks[w] : vs[w]) + n % 8 * OROW); };
-
+    static_assert(SLOT >= 8 * OROW, "eight rows of outputs fit a slot");
+    const float scale_log2 = a.scale * kLog2e;
     const int tid = threadIdx.x;
     const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int lane = tid % kWave;
     const int lr = lane % 16, lq = lane / 16;
-    __shared__ PagedLanes lanes;
-    const PagedShares<PagedArgsLate> shares(late_args(), lanes);
+    const PagedShares<PagedArgsLate> shares(late_args<ARGS>(), sm.lanes);
     // `p`: the tile; units u0 .. u0 + take of its n
     auto span = [&](const PagedSpan& p, uint32_t u0, uint32_t take) {
     const PagedRequest& q = p.req;
@@ -109,7 +115,7 @@ FEDRAG_KERNEL __launch_bounds__(kDecThreads, 2) void paged_decode_kernel(const P
         __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | ((N >> 4) << 14));
         __builtin_amdgcn_sched_barrier(0);
     };
-    char *const kslot = ks[wave], *const vslot = vs[wave];
+    char *const kslot = paged_slot(ks0, ks1, wave, SLOT), *const vslot = paged_slot(vs0, vs1, wave, SLOT);
 
     // One tile; MORE: the next one's loads are asked for as its slots come free.
     auto step = [&](int i, auto more) {
@@ -246,31 +252,31 @@ FEDRAG_KERNEL __launch_bounds__(kDecThreads, 2) void paged_decode_kernel(const P
     // fold the waves (Section 4.1 aggregation, in base 2); a thread finishes 4 columns of a row
     const float l_tot = xor32_sum(xor16_sum(l_run));
     if (lq == 0) {
-        sm_m[wave][lr] = m_run;
-        sm_l[wave][lr] = l_tot;
+        sm.m[wave][lr] = m_run;
+        sm.l[wave][lr] = l_tot;
     }
     if (lr < R) {
 #pragma unroll
-        for (int t = 0; t < DCH; ++t) *(f32x4_t*)(out_row(wave, lr) + 16 * t + 4 * lq) = acc[t];
+        for (int t = 0; t < DCH; ++t) *(f32x4_t*)((lr < 8 ? kslot : vslot) + lr % 8 * OROW + (16 * t + 4 * lq) * 4) = acc[t];
     }
     __syncthreads();
-    const PagedArgsLate& z = late_args();
+    const PagedArgsLate& z = late_args<ARGS>();
     const bool part = take < p.n;
-    const int64_t slot = 2 * (int64_t)blockIdx.x + (u0 == 0 ? 1 : 0);
+    const int64_t slot = 2 * (int64_t)index + (u0 == 0 ? 1 : 0);
     for (int idx = tid; idx < R * (D / 4); idx += kDecThreads) {
         const int n = idx / (D / 4), c = idx % (D / 4) * 4;
-        float M = sm_m[0][n];
+        float M = sm.m[0][n];
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) M = fmaxf(M, sm_m[w][n]);
+        for (int w = 1; w < WAVES; ++w) M = fmaxf(M, sm.m[w][n]);
         f32x4_t num = zero_vec<f32x4_t>();
         float den = 0.f;
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) {
-            const float f = fast_exp2(sm_m[w][n] - M);
-            const f32x4_t o = *(const f32x4_t*)(out_row(w, n) + c);
+            const float f = fast_exp2(sm.m[w][n] - M);
+            const f32x4_t o = *(const f32x4_t*)((n < 8 ? paged_slot(ks0, ks1, w, SLOT) : paged_slot(vs0, vs1, w, SLOT)) + n % 8 * OROW + c * 4);
 #pragma unroll
             for (int e = 0; e < 4; ++e) num[e] = __builtin_fmaf(f, o[e], num[e]);
-            den = __builtin_fmaf(f, sm_l[w][n], den);
+            den = __builtin_fmaf(f, sm.l[w][n], den);
         }
         const bool any = den != 0.f;  // (not a number where a score was not)
 #pragma unroll
@@ -282,10 +288,10 @@ FEDRAG_KERNEL __launch_bounds__(kDecThreads, 2) void paged_decode_kernel(const P
         if (c == 0) (part ? z.part_lse : z.lse)[at] = lse;
     }
     };
-    uint32_t pos = blockIdx.x * shares.share;
+    uint32_t pos = index * shares.share;
     const uint32_t end = pos + shares.share;
     for (bool first = true;; first = false) {
-        const PagedSpan p = shares.find(late_args(), pos);
+        const PagedSpan p = shares.find(late_args<ARGS>(), pos);
         if (p.b < 0) return;
         uint32_t take = p.begin + p.n - pos;
         if (p.n <= shares.whole) {
@@ -301,14 +307,6 @@ FEDRAG_KERNEL __launch_bounds__(kDecThreads, 2) void paged_decode_kernel(const P
         pos += take & 0x7fffffff;
         if (pos >= end) return;
     }
-}
-
-hipError_t launch_paged_decode(const PagedArgs& a, int D, int dtype, int64_t grid, hipStream_t stream) {
-    if (!grid_fits(grid, kDecThreads)) return hipErrorInvalidValue;
-    const auto kernel = dtype == FEDRAG_BF16 ? (D == 128 ? paged_decode_kernel<BF16, 128> : paged_decode_kernel<BF16, 64>)
-                                             : (D == 128 ? paged_decode_kernel<F16, 128> : paged_decode_kernel<F16, 64>);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(kDecThreads), 0, stream, a, a.scale * kLog2e);
-    return hipGetLastError();
 }
 
 }  // namespace fedrag

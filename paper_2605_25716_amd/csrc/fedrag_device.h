@@ -151,6 +151,18 @@ __device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
     return x;
 }
 
+// The largest over the wave's lanes, the same way (numbers without a sign: what a move leaves out is 0).
+__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
+    auto step = [&](uint32_t y) { x = x > y ? x : y; };
+    step(dpp_or_zero<0x111, 0xf>(x));
+    step(dpp_or_zero<0x112, 0xf>(x));
+    step(dpp_or_zero<0x114, 0xf>(x));
+    step(dpp_or_zero<0x118, 0xf>(x));
+    step(dpp_or_zero<0x142, 0xa>(x));
+    step(dpp_or_zero<0x143, 0xc>(x));
+    return (uint32_t)__builtin_amdgcn_readlane((int)x, kWave - 1);
+}
+
 // The same reduction of a minimum and a maximum at once, one instruction per step and value: the data-parallel move is
 // folded into the minimum / maximum (the compiler emits a move, a canonicalising maximum and the operation itself).  A
 // register has to be two instructions old before a data-parallel read, which the other value's step and a nop give it.
