@@ -3,13 +3,13 @@
 
 namespace fedrag {
 
-// The aggregation (Section 4.1) of the tiles whose keys are in several partials: a workgroup takes 8 or 16 rows of one of them, a
-// thread 4 columns of a row.  The lanes of a row share out the weights, 16 partials at a time.
+// The aggregation (Section 4.1) of the tiles whose keys are in several partials: a workgroup takes `rows` rows of one of them, part
+// `part`, a thread 4 columns of a row at a time.  Beyond four partials the lanes of a row share out the weights, 16 at a time.
 // Which tile: SHARES: the one that workgroup index + 1's share begins inside of, if no share before does; else the index-th of
 // those in several runs.
 constexpr int kPagedMergeThreads = 256;
 template <int D, bool SHARES>
-__device__ __forceinline__ void paged_merge(const PagedArgs& a, uint32_t index, int part) {
+__device__ __forceinline__ void paged_merge(const PagedArgs& a, uint32_t index, int part, int rows) {
     constexpr int TPR = D / 4;
     PagedRequest req;
     int tile, head, S = 0;
@@ -40,46 +40,77 @@ __device__ __forceinline__ void paged_merge(const PagedArgs& a, uint32_t index, 
         step = a.Hkv;
         S = p.per;  // units of a run, for now
     }
-    const int row0 = tile << a.cut.tile_shift, n = part * (kPagedMergeThreads / TPR) + threadIdx.x / TPR;
-    const int c = threadIdx.x % TPR, k = c % 16, group = threadIdx.x % kWave & 48;
-    const int last = (row0 + (1 << a.cut.tile_shift) < req.R ? row0 + (1 << a.cut.tile_shift) : req.R) - 1;
-    if (row0 + n > last) return;
+    const int row0 = tile << a.cut.tile_shift, last = (row0 + (1 << a.cut.tile_shift) < req.R ? row0 + (1 << a.cut.tile_shift) : req.R) - 1;
     if constexpr (!SHARES) {  // runs that hold keys which some row of the tile sees
         const int64_t run_keys = (int64_t)S << a.cut.unit_shift, seen = paged_limit(a, req, last);
         S = seen > 0 ? (int)((seen + run_keys - 1) / run_keys) : 1;
     }
-    auto place = [&](int i) { return ((i == 0 ? first : slot + i * step) << a.cut.tile_shift) + n; };
-    constexpr int NB = 16;
-    f32x4_t o[NB];
-    auto load_o = [&](int i0) {
+    const int c = threadIdx.x % TPR, k = c % 16, group = threadIdx.x % kWave & 48;
+    auto place = [&](int i, int n) { return ((i == 0 ? first : slot + i * step) << a.cut.tile_shift) + n; };
+    auto put = [&](int n, f32x4_t acc, float den, float M) {
+        const bool any = den != 0.f;
 #pragma unroll
-        for (int u = 0; u < NB; ++u) o[u] = *(const f32x4_t*)(a.part_O + place(i0 + u < S ? i0 + u : S - 1) * D + c * 4);
+        for (int e = 0; e < 4; ++e) acc[e] = any ? acc[e] / den : 0.f;
+        const uint32_t t = a.by_g.div((uint32_t)(row0 + n)), g = (uint32_t)(row0 + n) - t * a.by_g.d;
+        const int64_t at = ((int64_t)head * a.G + g) * a.T + req.begin + t;
+        *(f32x4_t*)(a.O + at * D + c * 4) = acc;
+        if (c == 0) a.lse[at] = any ? M + logf(den) : -INFINITY;
     };
-    load_o(0);
-    float M = -INFINITY;
-    for (int i = k; i < S; i += 16) M = fmaxf(M, a.part_lse[place(i)]);
-    M = group_max<16>(M);
-    f32x4_t acc = zero_vec<f32x4_t>();
-    float den = 0.f;
-    for (int i0 = 0; i0 < S; i0 += NB) {
-        if (i0) load_o(i0);
-        const float l = i0 + k < S ? a.part_lse[place(i0 + k)] : -INFINITY;
-        const float mine = l == -INFINITY ? 0.f : expf(l - M);
+    auto add = [&](float w, f32x4_t o, f32x4_t& acc, float& den) {  // (a partial of no weight takes no part, whatever it holds)
+        den += w;
 #pragma unroll
-        for (int u = 0; u < NB; ++u) {
-            const float w = __shfl(mine, group + u);
-            den += w;
+        for (int e = 0; e < 4; ++e) acc[e] = __builtin_fmaf(w, w != 0.f ? o[e] : 0.f, acc[e]);
+    };
+    for (int n0 = part * rows + threadIdx.x / TPR; n0 < (part + 1) * rows && row0 + n0 <= last; n0 += 2 * (kPagedMergeThreads / TPR)) {
+        // two rows at a time; the second may not be there
+        const int n1 = n0 + kPagedMergeThreads / TPR, n[2] = {n0, n1 < (part + 1) * rows && row0 + n1 <= last ? n1 : n0};
+        if (S <= 4) {  // a row's threads read its log-sum-exps all of them, and everything is in flight at once
+            float l[2][4];
+            f32x4_t o[2][4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[e] = __builtin_fmaf(w, w != 0.f ? o[u][e] : 0.f, acc[e]);
+            for (int r = 0; r < 2; ++r)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int64_t at = place(i < S ? i : S - 1, n[r]);
+                    l[r][i] = a.part_lse[at];
+                    o[r][i] = *(const f32x4_t*)(a.part_O + at * D + c * 4);
+                }
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                float M = -INFINITY, den = 0.f;
+                f32x4_t acc = zero_vec<f32x4_t>();
+#pragma unroll
+                for (int i = 0; i < 4; ++i) M = fmaxf(M, i < S ? l[r][i] : -INFINITY);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) add(i < S && l[r][i] != -INFINITY ? expf(l[r][i] - M) : 0.f, o[r][i], acc, den);
+                if (r == 0 || n[1] != n0) put(n[r], acc, den, M);
+            }
+            continue;
+        }
+#pragma unroll 1
+        for (int row = n0; row <= n[1]; row += kPagedMergeThreads / TPR) {
+            constexpr int NB = 16;
+            f32x4_t o[NB];
+            auto load_o = [&](int i0) {
+#pragma unroll
+                for (int u = 0; u < NB; ++u) o[u] = *(const f32x4_t*)(a.part_O + place(i0 + u < S ? i0 + u : S - 1, row) * D + c * 4);
+            };
+            load_o(0);
+            float M = -INFINITY;
+            for (int i = k; i < S; i += 16) M = fmaxf(M, a.part_lse[place(i, row)]);
+            M = group_max<16>(M);
+            f32x4_t acc = zero_vec<f32x4_t>();
+            float den = 0.f;
+            for (int i0 = 0; i0 < S; i0 += NB) {
+                if (i0) load_o(i0);
+                const float l = i0 + k < S ? a.part_lse[place(i0 + k, row)] : -INFINITY;
+                const float mine = l == -INFINITY ? 0.f : expf(l - M);
+#pragma unroll
+                for (int u = 0; u < NB; ++u) add(__shfl(mine, group + u), o[u], acc, den);
+            }
+            put(row, acc, den, M);
         }
     }
-    const bool any = den != 0.f;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) acc[e] = any ? acc[e] / den : 0.f;
-    const uint32_t t = a.by_g.div((uint32_t)(row0 + n)), g = (uint32_t)(row0 + n) - t * a.by_g.d;
-    const int64_t at = ((int64_t)head * a.G + g) * a.T + req.begin + t;
-    *(f32x4_t*)(a.O + at * D + c * 4) = acc;
-    if (c == 0) a.lse[at] = any ? M + logf(den) : -INFINITY;
 }
 
 // Tiles in runs (a), then tiles cut by shares (d), each in several workgroups: first every tile's first rows, and so on, so that
@@ -87,14 +118,14 @@ __device__ __forceinline__ void paged_merge(const PagedArgs& a, uint32_t index, 
 // KIND: 1 shares, 2 runs, 3 both (which of the two comes first is another trip to the arguments: 0.7 us of a short call).
 template <int D, int KIND>
 FEDRAG_KERNEL __launch_bounds__(kPagedMergeThreads) void paged_merge_kernel(const PagedArgs a, const PagedArgs d, uint32_t a_wgs, FastDiv tiles_a,
-                                                                            FastDiv tiles_d) {
+                                                                            FastDiv tiles_d, int rows_a, int rows_d) {
     const uint32_t i = blockIdx.x;
     if (KIND == 2 || (KIND == 3 && i < a_wgs)) {
         const uint32_t part = tiles_a.div(i);
-        paged_merge<D, false>(a, i - part * tiles_a.d, (int)part);
+        paged_merge<D, false>(a, i - part * tiles_a.d, (int)part, rows_a);
     } else {
         const uint32_t part = tiles_d.div(i - a_wgs);
-        paged_merge<D, true>(d, i - a_wgs - part * tiles_d.d, (int)part);
+        paged_merge<D, true>(d, i - a_wgs - part * tiles_d.d, (int)part, rows_d);
     }
 }
 
@@ -106,7 +137,16 @@ struct PagedLaunch {
     int64_t slots;   // at least the partials
     int64_t merges;  // at least the tiles in several partials
     size_t bytes(int D) const { return (((size_t)slots << cut.tile_shift) * (D + 1) * 4 + 15) / 16 * 16; }
-    int64_t merge_groups(int D) const { return ((D / 4 << cut.tile_shift) + kPagedMergeThreads - 1) / kPagedMergeThreads; }
+    // Rows of a tile that a workgroup of the aggregation takes: those that its threads hold at once, while there are few workgroups
+    // (117 rows over 4001 keys in 16 runs, 512 of them: 30.5 us, 36.6 with four times the rows each); else twice or four times that,
+    // as most of them, for tiles that might be in several partials, only search (1024 over 16384 keys 366 us and 358).
+    int merge_rows(int D) const {
+        int rows = kPagedMergeThreads / (D / 4);
+        const int most = cut.tile_shift >= 7 ? 4 * rows : 2 * rows;
+        while (rows < most && 2 * rows <= 1 << cut.tile_shift && (merges << cut.tile_shift) / rows > (cut.tile_shift >= 7 ? 1024 : 512)) rows *= 2;
+        return rows < 1 << cut.tile_shift ? rows : 1 << cut.tile_shift;
+    }
+    int64_t merge_groups(int D) const { return ((int64_t)1 << cut.tile_shift) / merge_rows(D); }
 };
 constexpr int kPagedDecodeRows = 16;  // a tile of the kernel for few rows
 
@@ -215,7 +255,7 @@ hipError_t launch_paged_attn(const PagedAttnProblem& p, hipStream_t stream) {
 #undef FEDRAG_MERGE
     hipLaunchKernelGGL(merge, dim3((unsigned)(wgs_r + wgs_s)), dim3(kPagedMergeThreads), 0,
                        stream, runs, shares, (uint32_t)wgs_r, FastDiv(plan.runs.merges > 0 ? plan.runs.merges : 1),
-                       FastDiv(plan.shares.merges > 0 ? plan.shares.merges : 1));
+                       FastDiv(plan.shares.merges > 0 ? plan.shares.merges : 1), plan.runs.merge_rows(p.D), plan.shares.merge_rows(p.D));
     return hipGetLastError();
 }
 
