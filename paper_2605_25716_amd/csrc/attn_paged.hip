@@ -200,7 +200,13 @@ static PagedPlan paged_plan(int B, int Hq, int Hkv, int dtype, int64_t T, int64_
         p.runs = paged_runs(PagedCut{tile, 6, 4, cus + 1, 1, INT32_MAX}, tiles(tile), keys);
         return p;
     }
-    if (many) p.runs = paged_runs(PagedCut{7, 6, 4, cus + 1, few ? kPagedDecodeRows + 1 : 1, INT32_MAX}, tiles(7), keys);
+    if (many) {
+        // Runs have four tiles of keys at least, but twice or four times that where the tiles alone occupy much of the device, as then
+        // the aggregation costs more than shorter runs save (32 heads of 128, least 4 and by this rule: 512 rows over 512 keys 27.2 and
+        // 22.8 us, 1000 over 1000 44.0 and 34.1; with few tiles the other way round: 64 over 1000 21.4, and 26.8 with 8).
+        const int64_t t = tiles(7), full = (int64_t)3 << cus >> 2;
+        p.runs = paged_runs(PagedCut{7, 6, 2 * t < full ? 4 : t < full ? 8 : 16, cus + 1, few ? kPagedDecodeRows + 1 : 1, INT32_MAX}, t, keys);
+    }
     // beside requests of many rows: one workgroup to a compute unit, for as long as the others take
     if (few)
         p.shares = paged_shares(PagedCut{4, 8, 1, many ? cus : cus + 1, 1, many ? kPagedDecodeRows : INT32_MAX}, many ? some * Hkv : tiles(4), keys);
