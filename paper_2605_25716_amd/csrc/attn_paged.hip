@@ -196,8 +196,12 @@ static PagedPlan paged_plan(int B, int Hq, int Hkv, int dtype, int64_t T, int64_
     const bool many = most * G > kPagedDecodeRows, few = !many || B > 1;
     PagedPlan p{};
     if (dtype == FEDRAG_F32) {
+        // A unit of keys is a step of each wave: as for 16 bits below, runs have one at least, two from a quarter of the compute units
+        // on, four from half of them (least 1, 2, 4, of 32 heads: 33, 1 and 70 rows of 8 heads over 500, 1025 and 70 keys 18.1, 19.2,
+        // 24.0 us; 64 over 512 23.6, 19.6, 24.6; 300 over 300 41.8, 41.5, 26.1).
         const int tile = many ? 5 : 4;
-        p.runs = paged_runs(PagedCut{tile, 6, 4, cus + 1, 1, INT32_MAX}, tiles(tile), keys);
+        const int64_t t = tiles(tile), full = (int64_t)1 << cus;
+        p.runs = paged_runs(PagedCut{tile, 6, 4 * t < full ? 1 : 2 * t < full ? 2 : 4, cus + 1, 1, INT32_MAX}, t, keys);
         return p;
     }
     if (many) {
