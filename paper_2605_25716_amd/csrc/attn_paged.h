@@ -11,14 +11,17 @@ namespace fedrag {
 // KV head (row r = token r / G, head r % G of the group), in tiles of 2^tile_shift rows, and n = ceil(keys / unit) units of keys (at least
 // one: a row without keys has an output all the same) for each of them.  All units together are below 2^31, which the host sees
 // to by way of `unit_shift`.  There are two ways to cut:
-//   runs    a tile's keys in equal runs of about `per` = max(least, ceil(units of all / target)), as many as n / per rounds to; a
-//           workgroup takes one.
+//   runs    a tile's keys in equal runs of about `per` = ceil(units of all / target) units, as many as n / per rounds to; a
+//           workgroup takes one.  The target is two workgroups to a compute unit, but one while that makes runs of up to eight units
+//           (two that share it work at half the rate, and write twice the partials: 64 rows of 28 heads of 64 over 6000 keys 24.1 us
+//           with two, 20.5 with one; 128 of 32 heads of 128 over 16384, 16 units, 67.1 and 68.8), and `least` is the least.
 //             runs         <= target + tiles of all requests and heads   (the grid),
 //             split runs   <= 4 / 3 target                               (a tile in two or more has n >= 1.5 per: their partials),
 //             split tiles  <= 2 / 3 target                               (what the aggregation has to visit);
 //   shares  the units of all tiles in a row, and an even share of them to each workgroup, wherever in a tile it begins and ends:
 //           all workgroups end together, whatever the lengths.  For kernels whose partials are small.
 // `target` is a power of two.
+constexpr uint32_t kPagedShortRun = 8;
 struct PagedCut {
     int tile_shift, unit_shift, least, target_shift;
     int few, many;  // only requests with few <= R <= many are this launch's
@@ -155,7 +158,10 @@ __device__ __forceinline__ PagedPiece paged_piece(Args& a, uint32_t index) {
         cost += is ? paged_tiles(a, r) * (uint32_t)a.Hkv * paged_units(a, r) : 0;
     });
     const uint32_t sum = lane_value(wave_scan(cost), kWave - 1);
-    uint32_t per = (uint32_t)(((uint64_t)sum + ((uint64_t)1 << a.cut.target_shift) - 1) >> a.cut.target_shift);
+    auto evenly = [&](uint64_t units) { return (uint32_t)((units + ((uint64_t)1 << a.cut.target_shift) - 1) >> a.cut.target_shift); };
+    uint32_t per = evenly((uint64_t)sum * 2);
+    per = per < kPagedShortRun ? per : kPagedShortRun;
+    per = per > evenly(sum) ? per : evenly(sum);
     per = per > (uint32_t)a.cut.least ? per : (uint32_t)a.cut.least;
     auto runs_of = [&](const PagedRequest& r) {
         const uint32_t n = paged_units(a, r);
