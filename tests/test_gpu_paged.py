@@ -273,6 +273,12 @@ def test_attn_many_requests(B):
         _check(_attn_case(list(q), list(kv), 2, 1, 64, 16, dt), True, "many")
 
 
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("q,kv,H", [([1100], [1100], 32), ([300], [300], 32), ([700, 500], [700, 900], 24), ([130], [140], 257), ([65], [65], 100)])
+def test_attn_as_many_pieces_as_workgroups_fit(dt, q, kv, H):
+    _check(_attn_case(q, kv, H, H, 64, 64, dt), True, dt)
+
+
 @pytest.mark.parametrize("form", ["tokens", "fused", "broadcast"])
 def test_attn_strided_queries(form):
     for dt in ("bf16", "f16", "f32"):
