@@ -158,6 +158,9 @@ __device__ __forceinline__ PagedPiece paged_piece(Args& a, uint32_t index) {
         cost += is ? paged_tiles(a, r) * (uint32_t)a.Hkv * paged_units(a, r) : 0;
     });
     const uint32_t sum = lane_value(wave_scan(cost), kWave - 1);
+    PagedPiece p{};
+    p.b = -1;
+    if (sum == 0) return p;  // (no requests of this form: the grid was for those that there might be)
     auto evenly = [&](uint64_t units) { return (uint32_t)((units + ((uint64_t)1 << a.cut.target_shift) - 1) >> a.cut.target_shift); };
     uint32_t per = evenly((uint64_t)sum * 2);
     per = per < kPagedShortRun ? per : kPagedShortRun;
@@ -181,8 +184,6 @@ __device__ __forceinline__ PagedPiece paged_piece(Args& a, uint32_t index) {
         split += is ? split_of(r) : 0;
     });
     const uint32_t to = wave_scan(pieces), split_to = wave_scan(split);
-    PagedPiece p{};
-    p.b = -1;
     if (lane_value(to, kWave - 1) <= index) return p;
     const int k = (a.B + kWave - 1) / kWave;
     uint32_t group = FastDiv::div_by(a.by_hkv.m, a.by_hkv.s, index);  // a tile and run of a request
@@ -235,7 +236,8 @@ __device__ __forceinline__ PagedPiece paged_piece(Args& a, uint32_t index) {
     p.runs = (int)runs;
     p.per = (int)((n + runs - 1) / runs);
     p.slot = slot + (before * runs + (uint32_t)p.run) * (uint32_t)a.Hkv + (uint32_t)p.head;  // SPLIT: run 0's; run r's is r * Hkv further
-    if (before >= tiles) p.b = -1;  // (only sums beyond 32 bits, by a q_start that decreases, lead here)
+    // (only sums beyond 32 bits, by a q_start that decreases, lead here)
+    if (before >= tiles || p.b >= a.B || (!SPLIT && runs > 1 && p.slot >= a.slots)) p.b = -1;
     return p;
 }
 
@@ -294,7 +296,7 @@ struct PagedShares {
         s.head = (int)(i - tile * a.by_hkv.d);
         const uint32_t tiles = paged_tiles(a, s.req);
         s.tile = (int)(tiles - 1 - tile);
-        if (tile >= tiles) s.b = -1;  // (only sums beyond 32 bits, by a q_start that decreases, lead here)
+        if (tile >= tiles || s.b >= a.B) s.b = -1;  // (only sums beyond 32 bits, by a q_start that decreases, lead here)
         return s;
     }
 };

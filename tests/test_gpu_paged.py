@@ -365,6 +365,20 @@ def test_attn_lengths_beyond_the_tensors():
         R.check_attn(O, lse, ref, FILL, "beyond")
 
 
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("columns,n_pages", [(0, 3), (4, 0), (0, 0)])
+def test_attn_without_columns_or_pages(dt, columns, n_pages):
+    """Lengths, but no table to say where, or no pool to point into: rows that see nothing."""
+    for q, max_q in (([1, 1], 1), ([40, 0, 1], 0), ([200], 200)):
+        T, B = sum(q), len(q)
+        Q = torch.ones((8, T, 64), dtype=dt, device=DEV)
+        pool = torch.empty((n_pages, 2, 16, 64), dtype=dt, device=DEV).fill_(float("nan"))
+        O, lse = fb.fedrag_paged_attn(Q, pool, pool.clone(), i32(np.zeros((B, columns))), i32(np.concatenate([[0], np.cumsum(q)])),
+                                      i32([500] * B), max_q, causal=max_q != 200, O_part=torch.full((1, 8, T, 64), 7.0, device=DEV),
+                                      lse=torch.full((1, 8, T), 7.0, device=DEV))
+        assert torch.all(O == 0) and torch.all(lse == -float("inf"))
+
+
 @pytest.mark.parametrize("dt,d", [("bf16", 128), ("f16", 128), ("bf16", 64), ("f32", 64)])
 def test_attn_outliers(dt, d):
     """Logits of some hundreds and channels of 20 times the others."""
