@@ -138,8 +138,8 @@ struct PagedLaunch {
     int64_t merges;  // at least the tiles in several partials
     size_t bytes(int D) const { return (((size_t)slots << cut.tile_shift) * (D + 1) * 4 + 15) / 16 * 16; }
     // Rows of a tile that a workgroup of the aggregation takes: those that its threads hold at once, while there are few workgroups
-    // (117 rows over 4001 keys in 16 runs, 512 of them: 30.5 us, 36.6 with four times the rows each); else twice or four times that,
-    // as most of them, for tiles that might be in several partials, only search (1024 over 16384 keys 366 us and 358).
+    // (117 rows over 4001 keys: 30.2 us, 35.7 with four times the rows each); else twice or four times that, as most of them, for
+    // tiles that might be in several partials, only search (1024 over 16384 keys 387 us without and 378, 512 over 2048 46 and 43).
     int merge_rows(int D) const {
         int rows = kPagedMergeThreads / (D / 4);
         const int most = cut.tile_shift >= 7 ? 4 * rows : 2 * rows;

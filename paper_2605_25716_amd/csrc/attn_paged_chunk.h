@@ -1,5 +1,7 @@
 // Attention over a paged cache for requests of many rows (a chunk of a prompt), 16-bit storage.  Bound by the matrix pipe, which
-// the two-term probabilities give half as much again to do, and by the vector work that does not hide behind it.
+// the two-term probabilities give half as much again to do, and by the vector work that does not hide behind it: 1024 rows of 32 heads
+// of 128 over 16384 keys take 357 to 377 us from one card to the next, 0.71 to 0.75 PFLOP/s of the visible pairs and half as much again
+// issued (a library product of bf16 reaches 1.39); 268 us with the matrix instructions alone, 199 with the vector ones.
 //
 // One workgroup = 4 waves x 32 flattened rows (token r / G, head r % G: all heads of a KV head's group share its keys, and a
 // tile spans few tokens, so that little of it lies above the diagonal) of one request and KV head x one run of keys.

@@ -12,7 +12,7 @@ namespace fedrag {
 // associative as + is) and of the pages they take, carried from one thousand to the next.  Each new page is then a thread's,
 // which finds its request in the prefix sums, and so is each row, up to kMapRows of them; beyond, the rows are a launch of
 // their own over the whole chip, which reads what this one has written.  Bound by the chain of its steps: a launch that reads
-// and writes a few KB.  One workgroup reads all lengths before it writes any, which is what lets a step advance in place.
+// and writes a few KB (5.0 us for 4 decoding requests, 6 for 256; 32 prompts of 4000 tokens 8.3 and 3.8).  One workgroup reads all lengths before it writes any, which is what lets a step advance in place.
 constexpr int kMapThreads = 1024;
 
 struct MapPrefix {
@@ -188,7 +188,9 @@ FEDRAG_KERNEL __launch_bounds__(256) void paged_map_rows_kernel(PagedMapJob j, i
     if (j.positions) j.positions[t] = pos;
 }
 
-constexpr int64_t kMapRows = 8192;  // rows that the one workgroup maps itself
+// Rows that the one workgroup maps itself: a launch less, but a chip less too (one launch and two: 4 requests of 1000 rows 6.3 and
+// 7.5 us, 1 of 4096 6.1 and 6.9, 8 of 1000 8.8 and 7.6, 256 of 32 11.2 and 8.3, 32 of 1000 26 and 8.5).
+constexpr int64_t kMapRows = 4096;
 
 hipError_t launch_paged_map(const PagedMapJob& job, hipStream_t stream) {
     const int shift = __builtin_ctz((unsigned)job.page_tokens);
@@ -203,7 +205,8 @@ hipError_t launch_paged_map(const PagedMapJob& job, hipStream_t stream) {
 // ------------------------------------------------------------------------------------------------ write
 // A copy: a thread moves 16 bytes of one row of one head, K's or V's.  A workgroup takes rows that follow each other in the
 // step, whose places in a page mostly follow each other too: whole runs of a page are written at once, and of a projection's
-// output whole rows of a head are read.
+// output whole rows of a head are read.  Bound by HBM: 32768 rows of 8 heads of 128 48.4 us, 5.55 TB/s of bytes read and written (a
+// library copy of 1 GiB 5.1); a single row 2.5 us, most of it the slot's trip and then the row's.
 constexpr int kWriteThreads = 256;
 
 template <int CH>  // 16-byte chunks per row
