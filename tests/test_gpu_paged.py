@@ -379,6 +379,35 @@ def test_attn_without_columns_or_pages(dt, columns, n_pages):
         assert torch.all(O == 0) and torch.all(lse == -float("inf"))
 
 
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_attn_far_pages(dt):
+    """Pages more than 2^32 bytes into a pool, K's and V's taking turns in it."""
+    q, kv, page, d = [1, 50, 300], [700, 400, 300], 256, 64
+    Q, Kp, Vp, table, q_start, lens = _attn_case(q, kv, 2, 1, d, page, dt)
+    n = 2 ** 32 // (2 * page * d * Kp.element_size()) + 100
+    pool = torch.empty((n, 2, 1, page, d), dtype=DT[dt], device=DEV)
+    far = n - 1 - np.arange(Kp.shape[0])
+    pool[far, 0], pool[far, 1] = Kp.to(DEV), Vp.to(DEV)
+    ref = R.attn_ref(Q, Kp, Vp, table, q_start, lens, True, d ** -0.5)
+    there = np.where(table >= 0, far[np.clip(table, 0, len(far) - 1)], -1)
+    O, lse = fb.fedrag_paged_attn(Q.to(DEV), pool[:, 0], pool[:, 1], i32(there), i32(q_start), i32(lens), 300)
+    R.check_attn(O[:, :, :sum(q)], lse[:, :, :sum(q)], tuple(x[:, :sum(q)] for x in ref[:4]) + (ref[4][:sum(q)],), FILL, "far")
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
+def test_attn_outputs_beyond_four_gib(dt):
+    """As many rows as make O pass 2^32 bytes, all with the same query: all of a head's rows are the first one's."""
+    Hq, T, d = 64, 2 ** 32 // (64 * 64 * 4) + 7, 64
+    g = torch.Generator().manual_seed(0)
+    Q = torch.randn((Hq, 1, d), generator=g).to(dt).to(DEV).expand(Hq, T, d)
+    pool = torch.randn((2, 3, 1, 16, d), generator=g).to(dt).to(DEV)
+    O, lse = fb.fedrag_paged_attn(Q, pool[0], pool[1], i32([[2, 0]]), i32([0, T]), i32([21]), T, causal=False)
+    first = slice(0, 1)
+    ref = R.attn_ref(Q[:, first].cpu(), pool[0].cpu(), pool[1].cpu(), np.array([[2, 0]]), [0, 1], [21], False, d ** -0.5)
+    R.check_attn(O[:, :, first], lse[:, :, first], ref, FILL, "first row")
+    assert torch.equal(O, O[:, :, :1].expand_as(O)) and torch.equal(lse, lse[:, :, :1].expand_as(lse))
+
+
 @pytest.mark.parametrize("dt,d", [("bf16", 128), ("f16", 128), ("bf16", 64), ("f32", 64)])
 def test_attn_outliers(dt, d):
     """Logits of some hundreds and channels of 20 times the others."""
