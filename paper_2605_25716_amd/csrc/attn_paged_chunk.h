@@ -1,6 +1,6 @@
 // Attention over a paged cache for requests of many rows (a chunk of a prompt), 16-bit storage.  Bound by the matrix pipe, which
 // the two-term probabilities give half as much again to do, and by the vector work that does not hide behind it: 1024 rows of 32 heads
-// of 128 over 16384 keys take 357 to 377 us from one card to the next, 0.71 to 0.75 PFLOP/s of the visible pairs and half as much again
+// of 128 over 16384 keys take 354 to 361 us with the fold, 0.74 to 0.75 PFLOP/s of the visible pairs and half as much again
 // issued (a library product of bf16 reaches 1.39); 268 us with the matrix instructions alone, 199 with the vector ones.
 //
 // One workgroup = 4 waves x 32 flattened rows (token r / G, head r % G: all heads of a KV head's group share its keys, and a
@@ -14,6 +14,9 @@
 //   * A wave works on two tiles at a time, so that vector work has matrix instructions to hide behind: iteration t issues
 //       A(t):   S^T(t) = K(t) Q^T       with B2(t-1): probabilities of keys 32..63 of tile t-1, whose maximum is known;
 //       C(t-1): O^T += V(t-1)^T P^T     with B1(t):   maximum, rescale factor and probabilities of keys 0..31 of tile t.
+//     The further a wave is in its iteration, the higher its priority over the one that it shares its SIMD with, which belongs to
+//     another workgroup: the two stay apart by half an iteration, and a barrier's last waves are not kept (without: 1024 rows over
+//     16384 keys 372 us, 361 so; 4096 over 4096 212 and 201; one step in place of three 365 and 203, the other way round 370 and 210).
 //   * Tiles are visited from the last to the first: those that some row does not see whole (the diagonal, the end of the request)
 //     come first and are finished one by one, up to the last of them, with which the pipeline starts.
 #pragma once
@@ -225,10 +228,12 @@ __device__ __forceinline__ void paged_chunk_body(const PagedArgs& a, uint32_t in
             S1[c] = zero_vec<f32x16_t>();
             float psum = 0.f;
             __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_setprio(0);
 #pragma unroll
             for (int j = 0; j < NA; ++j) {
                 if (j + 4 < NA)
                     kop[j + 4] = *(const vec8*)(kt + ((j + 4) % 2) * 32 * ROWB + k_off[(j + 4) / 2]);
+                if (j == NA / 2) __builtin_amdgcn_s_setprio(1);
                 if (j % 2 == 0) S0 = T::mfma32(kop[j], qop[j / 2], S0);
                 else S1[c] = T::mfma32(kop[j], qop[j / 2], S1[c]);
                 if constexpr (doC) {
@@ -297,6 +302,7 @@ __device__ __forceinline__ void paged_chunk_body(const PagedArgs& a, uint32_t in
 #pragma unroll
                 for (int j = 0; j < AHEAD; ++j) vop[j] = read_vop(vt, j / MT, j % MT);
             }
+            __builtin_amdgcn_s_setprio(2);
             float mx = -INFINITY;
             float m_new = 0.f, psum = 0.f;
             auto step = [&](int s) {
