@@ -18,14 +18,14 @@ FEDRAG_KERNEL __launch_bounds__(kPaged16Waves * kWave, 2) void paged_16_kernel(c
     if constexpr (KIND == 1) {
         paged_decode_body<T, D, 1>(d, blockIdx.x, ks0, ks1, vs0, vs1, sm);
     } else if constexpr (KIND == 2) {
-        paged_chunk_body<T, D, kPaged16Waves, 0, 3>(a, blockIdx.x, ks0, ks1, vs0, vs1, *(int*)&sm);
+        paged_chunk_body<T, D, kPaged16Waves, 0, 3>(a, blockIdx.x, ks0, ks1, vs0, vs1, (int*)&sm);
     } else {
         // `first` workgroups of many rows, one to a compute unit; then all of few rows; then the rest
         const int i = (int)blockIdx.x, decodes = (int)gridDim.x - chunks;
         if (i >= first && i < first + decodes)
             paged_decode_body<T, D, 1>(d, (uint32_t)(i - first), ks0, ks1, vs0, vs1, sm);
         else
-            paged_chunk_body<T, D, kPaged16Waves, 0, 2>(a, (uint32_t)(i < first ? i : i - decodes), ks0, ks1, vs0, vs1, *(int*)&sm);
+            paged_chunk_body<T, D, kPaged16Waves, 0, 2>(a, (uint32_t)(i < first ? i : i - decodes), ks0, ks1, vs0, vs1, (int*)&sm);
     }
 }
 

@@ -28,7 +28,7 @@ namespace fedrag {
 // AHEAD: V operands are read from LDS so many before they are used; K operands four.  (Three of V take the registers that are left
 // at 128 columns; the other form beside it takes two more for its scalars.)
 template <class T, int D, int NW, int ARGS, int AHEAD>
-__device__ __forceinline__ void paged_chunk_body(const PagedArgs& a, uint32_t index, char* ks0, char* ks1, char* vs0, char* vs1, int& sm_odd) {
+__device__ __forceinline__ void paged_chunk_body(const PagedArgs& a, uint32_t index, char* ks0, char* ks1, char* vs0, char* vs1, int* flags) {
     typedef typename T::elem elem;
     typedef typename T::vec8 vec8;
     constexpr int kThreads = NW * kWave;
@@ -74,6 +74,11 @@ __device__ __forceinline__ void paged_chunk_body(const PagedArgs& a, uint32_t in
     const int own = paged_limit(a, rq, row) - k_begin;
     const int key_lim = own < L ? own : L;                            // this lane's row sees keys < key_lim
 
+    vec8 qop[KS];  // Q^T operands: column li, channels 16 i + 8 lh
+    const char* Qr = a.Q + ((int64_t)p.head * a.G + hg) * a.q_head_stride + ((int64_t)rq.begin + tok) * a.q_token_stride;
+#pragma unroll
+    for (int i = 0; i < KS; ++i) qop[i] = *(const vec8*)(Qr + (i * 16 + lh * 8) * 2);
+
     // ---- where this wave's loads begin, lane l: load l % LPT of the tile l / LPT below `top`
     const int64_t table0 = (int64_t)p.b * a.max_pages;
     const int shift = a.pages.shift;
@@ -98,11 +103,6 @@ __device__ __forceinline__ void paged_chunk_body(const PagedArgs& a, uint32_t in
     int top = n_tiles - 1;  // `offset` is of this tile and the IDT - 1 below
     const int ids = ask_ids(top);
     int ids_next = ask_ids(top - IDT);
-    if (tid == 0) sm_odd = 0;
-    __syncthreads();
-    if (__builtin_amdgcn_ballot_w64(hole) != 0 && lane == 0) sm_odd = 1;
-    __syncthreads();
-    if (sm_odd != 0) t_mask0 = -1;
     int64_t offset = offset_of(ids, top);
 
     f32x16_t acc_o[MT];
@@ -117,7 +117,7 @@ __device__ __forceinline__ void paged_chunk_body(const PagedArgs& a, uint32_t in
     static_assert((NW * RPW) % 16 == 0, "swizzle must not depend on the load index");
     const int ld_k = ld_r * ROWB + ((ld_p ^ (tile_r % CH)) << 4);
     const int ld_v = ld_r * ROWB + ((ld_p ^ ((4 * (tile_r % 4)) % CH)) << 4);
-    const int full_tiles = t_mask0 < 0 ? 0 : L / kPreK;  // (pages are missing: none)
+    int full_tiles = 0;  // tiles whose rows are all there, once it is known that no pages are missing (before, the first tile is asked for)
     auto load_rows = [&](const char* base, char* slot, int tile, int voff) {
         auto begin = [&](int j) {
             const int at = (top - tile) * LPT + j;
@@ -162,11 +162,11 @@ __device__ __forceinline__ void paged_chunk_body(const PagedArgs& a, uint32_t in
 
     int tile = n_tiles - 1;
     load_k(tile, ks0);
-    vec8 qop[KS];  // Q^T operands: column li, channels 16 i + 8 lh
-    const char* Qr = a.Q + ((int64_t)p.head * a.G + hg) * a.q_head_stride + ((int64_t)rq.begin + tok) * a.q_token_stride;
-#pragma unroll
-    for (int i = 0; i < KS; ++i) qop[i] = *(const vec8*)(Qr + (i * 16 + lh * 8) * 2);
-
+    load_v(tile, vs0);
+    // flags: a wave's `hole` each, and whether `mend` has found something
+    const bool wave_hole = __builtin_amdgcn_ballot_w64(hole) != 0;
+    if (lane == 0) flags[wave] = wave_hole;
+    if (tid == 0) flags[NW] = 0;
     f32x16_t S0;                // S^T of the current tile, keys 0..31
     f32x16_t S1[2];             // S1[t & 1]: keys 32..63 of tile t, kept one iteration longer; then their probabilities
     uint32_t P[2][4][4];        // [t & 1]: P^T operands of tile t, one per 16 keys, in words of two,
@@ -202,14 +202,14 @@ __device__ __forceinline__ void paged_chunk_body(const PagedArgs& a, uint32_t in
     // par: t & 1 as a constant, so that the double sets are addressed statically.  kFirst: A and B1 of a tile (masked if need be);
     // kLast: B2 and C of the one before; kSteady: all, on tiles that every row sees whole.
     enum { kFirst, kSteady, kLast };
-    auto iteration = [&](int tile, int next, auto par, auto stage, bool ld_next) {
+    auto iteration = [&](int tile, int next, auto par, auto stage, bool ld_next, bool ld_v = true) {
         constexpr int c = decltype(par)::value;
         constexpr int o = 1 - c;
         constexpr int kind = decltype(stage)::value;
         constexpr bool doC = kind != kFirst;
         constexpr bool doAB = kind != kLast;
         constexpr int NM = 4 * MT;
-        if constexpr (doAB) load_v(tile, c ? vs1 : vs0);   // slot last read by C(t-2)
+        if (doAB && ld_v) load_v(tile, c ? vs1 : vs0);     // slot last read by C(t-2)
         if (ld_next) load_k(next, o ? ks1 : ks0);          // slot last read by A(t-1)
 
         // lane: row li and, per 32-key half, keys 8 (r / 4) + 4 lh + r % 4, r = 0..15
@@ -381,9 +381,9 @@ __device__ __forceinline__ void paged_chunk_body(const PagedArgs& a, uint32_t in
                 bad |= lo || up;
             }
         }
-        if (__builtin_amdgcn_ballot_w64(bad) != 0 && lane == 0) sm_odd = 1;
+        if (__builtin_amdgcn_ballot_w64(bad) != 0 && lane == 0) flags[NW] = 1;
         __syncthreads();
-        if (sm_odd == 0) return;  // workgroup-uniform
+        if (flags[NW] == 0) return;  // workgroup-uniform
 #pragma unroll
         for (int i = 0; i < MT; ++i) acc_o[i] *= alph[0];
         alph[0] = 1.0f;
@@ -414,17 +414,20 @@ __device__ __forceinline__ void paged_chunk_body(const PagedArgs& a, uint32_t in
             }
             *at = v;
         }
-        if (tid == 0) sm_odd = 0;
+        if (tid == 0) flags[NW] = 0;
         __syncthreads();
     };
     const bool differ = lim_min != lim_max;
 
     alph[0] = alph[1] = 1.0f;
     tile_barrier();
-    if (tid == 0) sm_odd = 0;
-    __syncthreads();
+    int holes = 0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) holes |= flags[w];
+    if (__builtin_amdgcn_readfirstlane(holes) != 0) t_mask0 = -1;
+    else full_tiles = L / kPreK;
     while (tile >= 0 && (tile > t_mask0 || (tile & 1))) {
-        iteration(tile, 0, even, first, false);
+        iteration(tile, 0, even, first, false, tile != n_tiles - 1);
         tile_barrier();
         if (differ && tile >= t_mask0) mend(tile);
         --tile;
@@ -433,7 +436,7 @@ __device__ __forceinline__ void paged_chunk_body(const PagedArgs& a, uint32_t in
         tile_barrier();
     }
     if (tile >= 0) {
-        iteration(tile, tile - 1, even, first, true);
+        iteration(tile, tile - 1, even, first, true, tile != n_tiles - 1);
         tile_barrier();
         if (differ && tile >= t_mask0) mend(tile);
         for (; tile > 0; tile -= 2) {
@@ -477,7 +480,7 @@ __device__ __forceinline__ void paged_chunk_body(const PagedArgs& a, uint32_t in
         if (lh == 0 && real) (p.runs > 1 ? z.part_lse : z.lse)[at] = l_tot != 0.f ? (m_run + fast_log2(l_tot)) * kLn2 : -INFINITY;
         wave_lds_fence();
         // a store covers whole rows; where a row goes is with the lane of its number
-#pragma unroll 4
+#pragma unroll
         for (int u = 0; u < kPreQ * PCH / kWave; ++u) {
             const int r = (u * kWave + lane) / PCH, chunk = lane % PCH;
             const f32x4_t o = *(const f32x4_t*)(mine + r * (D * 4) + ((chunk ^ (r % PCH)) << 4));
