@@ -15,6 +15,9 @@ namespace fedrag {
 //           workgroup takes one.  The target is two workgroups to a compute unit, but one while that makes runs of up to eight units
 //           (two that share it work at half the rate, and write twice the partials: 64 rows of 28 heads of 64 over 6000 keys 24.1 us
 //           with two, 20.5 with one; 128 of 32 heads of 128 over 16384, 16 units, 67.1 and 68.8), and `least` is the least.
+//           With a least of 1 a run has c sqrt(n) units, c = 2 / 5 for tiles of 128 rows and 1 / 5 for less: of few tiles of many keys the time to
+//           fold n / per partials grows as the time of a run falls (20 rows of 4 heads over 30000 keys, 117 runs 31.8 us, so 59 31.9,
+//           469 47.6; 3 of 14 over 6856 27, 27, 108 runs 18.0, 18.9, 25.3; one fp32 row over 30000 40.1, 31.3 by c = 1 / 5).
 //             runs         <= target + tiles of all requests and heads   (the grid),
 //             split runs   <= 4 / 3 target                               (a tile in two or more has n >= 1.5 per: their partials),
 //             split tiles  <= 2 / 3 target                               (what the aggregation has to visit);
@@ -168,7 +171,12 @@ __device__ __forceinline__ PagedPiece paged_piece(Args& a, uint32_t index) {
     per = per > (uint32_t)a.cut.least ? per : (uint32_t)a.cut.least;
     auto runs_of = [&](const PagedRequest& r) {
         const uint32_t n = paged_units(a, r);
-        return 2 * n < 3 * per ? 1 : (n + per / 2) / per;
+        uint32_t len = per;
+        if (a.cut.least == 1) {
+            const uint32_t fold = (uint32_t)(__builtin_amdgcn_sqrtf((float)n) * (a.cut.tile_shift >= 7 ? 0.4f : 0.2f));
+            len = len > fold ? len : fold;
+        }
+        return 2 * n < 3 * len ? 1 : (n + len / 2) / len;
     };
     auto pieces_of = [&](const PagedRequest& r) {
         const uint32_t runs = runs_of(r), n = paged_tiles(a, r) * (uint32_t)a.Hkv;

@@ -207,11 +207,12 @@ static PagedPlan paged_plan(int B, int Hq, int Hkv, int dtype, int64_t T, int64_
     if (many) {
         // Runs have four tiles of keys at least, but twice or four times that where the tiles alone occupy much of the device, as then
         // the aggregation costs more than shorter runs save (32 heads of 128, least 4 and by this rule: 512 rows over 512 keys 27.2 and
-        // 22.8 us, 1000 over 1000 44.0 and 34.1; with few tiles the other way round: 64 over 1000 21.4, and 26.8 with 8).
+        // 22.8 us, 1000 over 1000 44.0 and 34.1; 64 over 1000 21.1, and 26.3 with 8), and one where there are hardly any (64 over 1000
+        // 19.0, 20 over 500 19.2 and 15.6, 569 and 57 of 2 heads over as many 20.6 and 16.7; with 32 tiles 117 over 4001 30.1 and 31.2).
         // (beside the other form a request of this one has more than its rows)
         const int64_t by_rows = T * G / (kPagedDecodeRows + 1) * Hkv;
         const int64_t t = few && by_rows < tiles(7) ? by_rows : tiles(7), full = (int64_t)3 << cus >> 2;
-        p.runs = paged_runs(PagedCut{7, 6, 2 * t < full ? 4 : t < full ? 8 : 16, cus + 1, few ? kPagedDecodeRows + 1 : 1, INT32_MAX}, t, keys);
+        p.runs = paged_runs(PagedCut{7, 6, 8 * t <= full ? 1 : 2 * t < full ? 4 : t < full ? 8 : 16, cus + 1, few ? kPagedDecodeRows + 1 : 1, INT32_MAX}, t, keys);
     }
     // beside requests of many rows: one workgroup to a compute unit, for as long as the others take
     if (few)
