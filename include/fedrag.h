@@ -452,7 +452,8 @@ fedrag_status fedrag_paged_attn(const fedrag_shape* shape, int64_t n_rows, const
                                 void* workspace, size_t workspace_bytes, void* stream);
 
 /* Bytes of workspace fedrag_paged_attn needs for these sizes; 0 for arguments it would reject.  Like the other size it
- * depends on the compute units of the device that is current in the calling thread. */
+ * depends on the compute units of the device that is current in the calling thread.  More rows can need less (they are
+ * cut into fewer runs); whatever the sizes, 69 MiB are enough on a device of 256 compute units. */
 size_t fedrag_paged_attn_workspace_bytes(const fedrag_shape* shape, int64_t n_rows, int64_t max_pages,
                                          int32_t page_tokens, int64_t max_q_len);
 

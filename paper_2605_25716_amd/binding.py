@@ -651,6 +651,7 @@ def fedrag_paged_write(K, V, slots, K_pages, V_pages):
 
 
 def fedrag_paged_attn_workspace_bytes(batch, n_q_heads, n_kv_heads, d_head, dtype, n_rows, max_pages, page_tokens, max_q_len) -> int:
+    """Bytes for one call of these sizes (more rows can need less); 69 MiB are enough for any on 256 compute units."""
     shape = _shape_ref_of_numbers(batch, n_q_heads, n_kv_heads, d_head, dtype)
     return int(load().fedrag_paged_attn_workspace_bytes(shape, n_rows, max_pages, page_tokens, max_q_len))
 

@@ -113,6 +113,18 @@ def test_attn_workspace(lib):
         assert lib.fedrag_paged_attn_workspace_bytes(*bad) == 0
 
 
+def test_attn_workspace_has_a_bound(lib):
+    """What a caller may set aside once for all its calls."""
+    sizes = [(B, T) for B in (1, 7, 64, 1000) for T in (1, 3, 17, 64, 300, 1000, 5000, 70000)]
+    for B, T in sizes:
+        for Hkv, G in ((1, 1), (1, 16), (8, 4), (33, 2)):
+            for d, dtype in ((64, fb.F32), (128, fb.F32), (128, fb.BF16)):
+                for columns in (1, 9, 100, 3000, 40000):
+                    for max_q in (0, 1, 5, T):
+                        need = lib.fedrag_paged_attn_workspace_bytes(shape(B=B, Hq=G * Hkv, Hkv=Hkv, d=d, dt=dtype), T, columns, 16, max_q)
+                        assert need <= 69 * 2 ** 20, (B, T, Hkv, G, d, dtype, columns, max_q)
+
+
 WRITE = dict(shape=None, n_rows=40, K=A, V=2 * A, hs=128, ts=1024, slots=3 * A, Kp=4 * A, Vp=5 * A, n_pages=10, ps=0, page=16)
 
 
