@@ -15,6 +15,10 @@ namespace fedrag {
 //           workgroup takes one.  The target is two workgroups to a compute unit, but one while that makes runs of up to eight units
 //           (two that share it work at half the rate, and write twice the partials: 64 rows of 28 heads of 64 over 6000 keys 24.1 us
 //           with two, 20.5 with one; 128 of 32 heads of 128 over 16384, 16 units, 67.1 and 68.8), and `least` is the least.
+//           A tile is not cut where that saves less than `gain` units, or if it has at most 48 units and no more than a compute unit's
+//           part of the work and a third (1200 rows of 32 heads over 1800 keys cut 82.8 us, whole 62.4, 1000 over 1500 53.0 and 48.9;
+//           700 over 1500, one and a half times the part, 41.3 and 44.3; 1024 over 16384, 256 units, 346 and 372, as two workgroups that
+//           share a compute unit get 8 % more out of it); not so tiles of fewer rows (377 fp32 rows beside twelve single ones 42 and 56).
 //           With a least of 1 a run has c sqrt(n) units, c = 2 / 5 for tiles of 128 rows and 1 / 5 for less: of few tiles of many keys the time to
 //           fold n / per partials grows as the time of a run falls (20 rows of 4 heads over 30000 keys, 117 runs 31.8 us, so 59 31.9,
 //           469 47.6; 3 of 14 over 6856 27, 27, 108 runs 18.0, 18.9, 25.3; one fp32 row over 30000 40.1, 31.3 by c = 1 / 5).
@@ -24,9 +28,10 @@ namespace fedrag {
 //   shares  the units of all tiles in a row, and an even share of them to each workgroup, wherever in a tile it begins and ends:
 //           all workgroups end together, whatever the lengths.  For kernels whose partials are small.
 // `target` is a power of two.
-constexpr uint32_t kPagedShortRun = 8;
+constexpr uint32_t kPagedShortRun = 8, kPagedWhole = 48;
 struct PagedCut {
     int tile_shift, unit_shift, least, target_shift;
+    int gain;       // runs: a tile is cut only if they are shorter than the whole by so many units
     int few, many;  // only requests with few <= R <= many are this launch's
 };
 
@@ -165,8 +170,9 @@ __device__ __forceinline__ PagedPiece paged_piece(Args& a, uint32_t index) {
     p.b = -1;
     if (sum == 0) return p;  // (no requests of this form: the grid was for those that there might be)
     auto evenly = [&](uint64_t units) { return (uint32_t)((units + ((uint64_t)1 << a.cut.target_shift) - 1) >> a.cut.target_shift); };
-    uint32_t per = evenly((uint64_t)sum * 2);
-    per = per < kPagedShortRun ? per : kPagedShortRun;
+    const uint32_t unit = evenly((uint64_t)sum * 2);  // of a compute unit
+    const uint32_t whole = unit + unit / 3 < kPagedWhole ? unit + unit / 3 : kPagedWhole;
+    uint32_t per = unit < kPagedShortRun ? unit : kPagedShortRun;
     per = per > evenly(sum) ? per : evenly(sum);
     per = per > (uint32_t)a.cut.least ? per : (uint32_t)a.cut.least;
     auto runs_of = [&](const PagedRequest& r) {
@@ -176,7 +182,7 @@ __device__ __forceinline__ PagedPiece paged_piece(Args& a, uint32_t index) {
             const uint32_t fold = (uint32_t)(__builtin_amdgcn_sqrtf((float)n) * (a.cut.tile_shift >= 7 ? 0.4f : 0.2f));
             len = len > fold ? len : fold;
         }
-        return 2 * n < 3 * len ? 1 : (n + len / 2) / len;
+        return 2 * n < 3 * len || n < len + (uint32_t)a.cut.gain || (a.cut.tile_shift >= 7 && n <= whole) ? 1 : (n + len / 2) / len;
     };
     auto pieces_of = [&](const PagedRequest& r) {
         const uint32_t runs = runs_of(r), n = paged_tiles(a, r) * (uint32_t)a.Hkv;

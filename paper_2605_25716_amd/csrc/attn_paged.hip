@@ -161,7 +161,7 @@ static int64_t paged_units_of(PagedCut& cut, int64_t tiles, int64_t keys) {
 static PagedLaunch paged_runs(PagedCut cut, int64_t tiles, int64_t keys) {
     const int64_t target = (int64_t)1 << cut.target_shift;
     const int64_t units = paged_units_of(cut, tiles, keys);
-    const int64_t most_runs = (units + cut.least / 2) / cut.least > 1 ? (units + cut.least / 2) / cut.least : 1;
+    const int64_t most_runs = units >= cut.least + cut.gain && (units + cut.least / 2) / cut.least > 1 ? (units + cut.least / 2) / cut.least : 1;
     PagedLaunch l{};
     l.cut = cut;
     l.grid = target + tiles < tiles * most_runs ? target + tiles : tiles * most_runs;
@@ -201,7 +201,7 @@ static PagedPlan paged_plan(int B, int Hq, int Hkv, int dtype, int64_t T, int64_
         // 24.0 us; 64 over 512 23.6, 19.6, 24.6; 300 over 300 41.8, 41.5, 26.1).
         const int tile = many ? 5 : 4;
         const int64_t t = tiles(tile), full = (int64_t)1 << cus;
-        p.runs = paged_runs(PagedCut{tile, 6, 4 * t < full ? 1 : 2 * t < full ? 2 : 4, cus + 1, 1, INT32_MAX}, t, keys);
+        p.runs = paged_runs(PagedCut{tile, 6, 4 * t < full ? 1 : 2 * t < full ? 2 : 4, cus + 1, 0, 1, INT32_MAX}, t, keys);
         return p;
     }
     if (many) {
@@ -209,14 +209,16 @@ static PagedPlan paged_plan(int B, int Hq, int Hkv, int dtype, int64_t T, int64_
         // the aggregation costs more than shorter runs save (32 heads of 128, least 4 and by this rule: 512 rows over 512 keys 27.2 and
         // 22.8 us, 1000 over 1000 44.0 and 34.1; 64 over 1000 21.1, and 26.3 with 8), and one where there are hardly any (64 over 1000
         // 19.0, 20 over 500 19.2 and 15.6, 569 and 57 of 2 heads over as many 20.6 and 16.7; with 32 tiles 117 over 4001 30.1 and 31.2).
-        // (beside the other form a request of this one has more than its rows)
+        // A cut has to save 6 units, 4 of few tiles (300 over 500 24.2 us without, 22.4 so; 64 over 300 17.1, and 18.3 with 6).
+        // (t: beside the other form a request of this one has more than its rows)
         const int64_t by_rows = T * G / (kPagedDecodeRows + 1) * Hkv;
         const int64_t t = few && by_rows < tiles(7) ? by_rows : tiles(7), full = (int64_t)3 << cus >> 2;
-        p.runs = paged_runs(PagedCut{7, 6, 8 * t <= full ? 1 : 2 * t < full ? 4 : t < full ? 8 : 16, cus + 1, few ? kPagedDecodeRows + 1 : 1, INT32_MAX}, t, keys);
+        const int least = 8 * t <= full ? 1 : 2 * t < full ? 4 : t < full ? 8 : 16, gain = least == 1 ? 4 : 6;
+        p.runs = paged_runs(PagedCut{7, 6, least, cus + 1, gain, few ? kPagedDecodeRows + 1 : 1, INT32_MAX}, t, keys);
     }
     // beside requests of many rows: one workgroup to a compute unit, for as long as the others take
     if (few)
-        p.shares = paged_shares(PagedCut{4, 8, 1, many ? cus : cus + 1, 1, many ? kPagedDecodeRows : INT32_MAX}, many ? some * Hkv : tiles(4), keys);
+        p.shares = paged_shares(PagedCut{4, 8, 1, many ? cus : cus + 1, 0, 1, many ? kPagedDecodeRows : INT32_MAX}, many ? some * Hkv : tiles(4), keys);
     return p;
 }
 
