@@ -279,6 +279,12 @@ def test_attn_as_many_pieces_as_workgroups_fit(dt, q, kv, H):
     _check(_attn_case(q, kv, H, H, 64, 64, dt), True, dt)
 
 
+@pytest.mark.parametrize("causal", [True, False], ids=["causal", "all"])
+def test_attn_whole_tiles_beside_cut_ones(causal):
+    """Tiles that fit a compute unit's part of the work stay whole; those of a long request are cut, and folded by the same launch."""
+    _check(_attn_case([1000, 40, 3], [1500, 5000, 700], 24, 24, 64, 64, "bf16"), causal, "whole and cut")
+
+
 @pytest.mark.parametrize("form", ["tokens", "fused", "broadcast"])
 def test_attn_strided_queries(form):
     for dt in ("bf16", "f16", "f32"):
