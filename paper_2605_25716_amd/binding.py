@@ -591,6 +591,8 @@ def _page_stride(shape, stride) -> int:
     n, H, P, d = shape
     if any(size > 1 and have != want for have, size, want in ((stride[1], H, P * d), (stride[2], P, d), (stride[3], d, 1))):
         raise ValueError("a page has to be dense: [Hkv, page_tokens, d] without gaps")
+    if n > 1 and stride[0] == 0:  # (which to the library means that the pages lie side by side)
+        raise ValueError("K_pages, V_pages: every page has memory of its own, not one that is expanded")
     return stride[0] if n > 1 else 0
 
 

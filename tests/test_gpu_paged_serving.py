@@ -219,3 +219,13 @@ def test_binding_refusals_on_the_device():
         fb.fedrag_paged_write(rows, rows, torch.zeros(3, dtype=torch.int64, device=DEV), Kp, Kp)
     with pytest.raises(TypeError):
         fb.fedrag_paged_attn(**ok, max_q_len=1.5)
+
+
+def test_expanded_pools_are_refused():
+    """One page under many ids: there is no memory behind the others."""
+    Q, rows, page = torch.zeros((4, 3, 64), device=DEV), torch.zeros((2, 3, 64), device=DEV), torch.zeros((1, 2, 16, 64), device=DEV)
+    K, V = page.expand(5, 2, 16, 64), page.clone().expand(5, 2, 16, 64)
+    with pytest.raises(ValueError):
+        fb.fedrag_paged_attn(Q, K, V, i32([[0, 1]]), i32([0, 3]), i32([9]))
+    with pytest.raises(ValueError):
+        fb.fedrag_paged_write(rows, rows, torch.zeros(3, dtype=torch.int64, device=DEV), K, V)

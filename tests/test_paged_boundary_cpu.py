@@ -168,6 +168,16 @@ def test_binding_refuses_host_tensors():
                              z(1, dtype=torch.int32))
 
 
+def test_pages_have_memory_of_their_own():
+    """A stride of 0 between pages is the struct's word for pages side by side, which those of an expanded tensor are not."""
+    for pool in (torch.zeros((1, 2, 16, 64)).expand(4, 2, 16, 64), torch.zeros((2, 16, 64), dtype=torch.bfloat16).expand(4, 2, 16, 64)):
+        with pytest.raises(ValueError):
+            fb._page_stride(pool.shape, pool.stride())
+    both = torch.zeros((4, 2, 2, 16, 64))
+    for pool, want in ((both[0, 0][None].expand(1, 2, 16, 64), 0), (both[:, 0], 4096), (both[:, 0].contiguous(), 2048), (both[:0, 0], 0)):
+        assert fb._page_stride(pool.shape, pool.stride()) == want
+
+
 def test_structs_match_the_header(tmp_path):
     """The binding's structs have the header's sizes and offsets."""
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
