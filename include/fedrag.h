@@ -397,8 +397,8 @@ typedef struct {
  *     8  a length below zero (taken as 0), tokens beyond INT32_MAX (cached_lens is cut), or *free_count outside
  *        [0, n_free] (taken as the nearer of the two).
  * To release a request's pages, put their ids back on the stack and add their number to the count.
- * One launch up to some thousand rows, two beyond.  batch, n_rows, max_pages, n_free : 0 .. INT32_MAX; n_free may be 0
- * with free_pages NULL, and tensors of no elements may be NULL.
+ * One launch up to some thousand rows, two beyond.  batch : 0 .. INT32_MAX - 255;  n_rows, max_pages, n_free : 0 ..
+ * INT32_MAX; n_free may be 0 with free_pages NULL, and tensors of no elements may be NULL.
  */
 #define FEDRAG_MAP_NO_PAGES 1
 #define FEDRAG_MAP_NO_COLUMNS 2
@@ -425,7 +425,7 @@ fedrag_status fedrag_paged_write(const fedrag_shape* shape, int64_t n_rows, cons
 
 /*
  * Attention of a step's rows over the paged cache, in which the step's own rows are already.  shape->batch = number of
- * requests.  Row i of request b, i = 0 .. n-1 with n = q_start[b+1] - q_start[b], sees the first
+ * requests, at most INT32_MAX - 255.  Row i of request b, i = 0 .. n-1 with n = q_start[b+1] - q_start[b], sees the first
  *     kv_lens[b] tokens of the request (causal = 0: a Compute Node's part, Section 4.1), or of them the first
  *     kv_lens[b] - n + i + 1 (causal = 1: the new rows are the last tokens, and a token sees itself and what comes
  *     before; the Inquirer's own part, Section 5.3),

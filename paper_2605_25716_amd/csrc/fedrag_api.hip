@@ -82,6 +82,8 @@ fedrag_status check_rows(const fedrag_rows* r, int64_t n_rows, int32_t heads, co
 
 constexpr int64_t kMostTokens = INT32_MAX - 255;  // of a request: a tile's end is still an int32
 
+constexpr int32_t kMostRequests = INT32_MAX - 255;  // rounded up to some for each of a wave's lanes they are still an int32
+
 bool page_tokens_ok(int32_t n) { return n == 16 || n == 32 || n == 64 || n == 128 || n == 256; }
 
 // The cache's numbers; its pointers are looked at only if it has pages.
@@ -118,8 +120,8 @@ bool pages_overlap(const Pages& p, size_t extent, size_t block) {
     return d < block || (size_t)p.page_bytes - d < block;
 }
 
-fedrag_status check_paged_sizes(int64_t n_rows, int64_t max_pages, int64_t max_q_len) {
-    return n_rows < 0 || n_rows > INT32_MAX || max_pages < 0 || max_pages > INT32_MAX || max_q_len < 0 ? FEDRAG_ERR_SHAPE
+fedrag_status check_paged_sizes(int32_t batch, int64_t n_rows, int64_t max_pages, int64_t max_q_len) {
+    return batch > kMostRequests || n_rows < 0 || n_rows > INT32_MAX || max_pages < 0 || max_pages > INT32_MAX || max_q_len < 0 ? FEDRAG_ERR_SHAPE
                                                                                                         : FEDRAG_OK;
 }
 
@@ -776,7 +778,7 @@ fedrag_status fedrag_paged_map(int32_t batch, int64_t n_rows, int32_t page_token
                                const int32_t* free_count, int32_t* block_table, int32_t* q_start, int32_t* kv_lens, int64_t* slots,
                                int32_t* positions, int32_t* free_left, int32_t* flags, void* stream) {
     if (batch < 0 || n_free < 0 || n_free > INT32_MAX) return FEDRAG_ERR_SHAPE;
-    fedrag_status st = check_paged_sizes(n_rows, max_pages, 0);
+    fedrag_status st = check_paged_sizes(batch, n_rows, max_pages, 0);
     if (st != FEDRAG_OK) return st;
     if (!page_tokens_ok(page_tokens)) return FEDRAG_ERR_UNSUPPORTED;
     if (!free_count || !q_start || !free_left || !flags || (batch > 0 && (!cached_lens || !new_lens || !kv_lens)) ||
@@ -809,7 +811,7 @@ fedrag_status fedrag_paged_map(int32_t batch, int64_t n_rows, int32_t page_token
 fedrag_status fedrag_paged_write(const fedrag_shape* shape, int64_t n_rows, const fedrag_rows* K_rows, const fedrag_rows* V_rows,
                                  const int64_t* slots, const fedrag_paged_cache* cache, void* stream) {
     fedrag_status st = check_shape(shape, true);
-    if (st == FEDRAG_OK) st = check_paged_sizes(n_rows, 0, 0);
+    if (st == FEDRAG_OK) st = check_paged_sizes(0, n_rows, 0, 0);
     if (st != FEDRAG_OK) return st;
     PagedWriteJob j{};
     size_t extent, block, kb, vb;
@@ -843,7 +845,7 @@ fedrag_status fedrag_paged_write(const fedrag_shape* shape, int64_t n_rows, cons
 
 size_t fedrag_paged_attn_workspace_bytes(const fedrag_shape* shape, int64_t n_rows, int64_t max_pages, int32_t page_tokens,
                                          int64_t max_q_len) {
-    if (check_shape(shape, true) != FEDRAG_OK || check_paged_sizes(n_rows, max_pages, max_q_len) != FEDRAG_OK ||
+    if (check_shape(shape, true) != FEDRAG_OK || check_paged_sizes(shape->batch, n_rows, max_pages, max_q_len) != FEDRAG_OK ||
         !page_tokens_ok(page_tokens) || max_pages * page_tokens > kMostTokens)
         return 0;
     return paged_attn_workspace_bytes(shape->batch, shape->n_q_heads, shape->n_kv_heads, shape->d_head, shape->dtype, n_rows, max_pages,
@@ -855,7 +857,7 @@ fedrag_status fedrag_paged_attn(const fedrag_shape* shape, int64_t n_rows, const
                                 int64_t max_q_len, int32_t causal, float softmax_scale, float* O, float* lse, void* workspace,
                                 size_t workspace_bytes, void* stream) {
     fedrag_status st = check_shape(shape, true);
-    if (st == FEDRAG_OK) st = check_paged_sizes(n_rows, max_pages, max_q_len);
+    if (st == FEDRAG_OK) st = check_paged_sizes(shape->batch, n_rows, max_pages, max_q_len);
     if (st != FEDRAG_OK) return st;
     PagedAttnProblem p{};
     size_t extent, block, qb;

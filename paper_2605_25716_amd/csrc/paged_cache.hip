@@ -173,7 +173,7 @@ FEDRAG_KERNEL __launch_bounds__(256) void paged_map_rows_kernel(PagedMapJob j, i
         if (last >= j.q_start[lo + 1]) hi = __builtin_amdgcn_readfirstlane(request_of(j.q_start, j.batch, last));
         if (t < rows) {
             while (lo < hi) {  // the last request that starts at or before t
-                const int mid = (lo + hi + 1) / 2;
+                const int mid = hi - (hi - lo) / 2;
                 if (j.q_start[mid] <= t) lo = mid;
                 else hi = mid - 1;
             }

@@ -178,6 +178,19 @@ def test_pages_have_memory_of_their_own():
         assert fb._page_stride(pool.shape, pool.stride()) == want
 
 
+def test_most_requests(lib):
+    """What is reckoned with requests a lane, rounded up, stays in 32 bits."""
+    most, far = 2 ** 31 - 1 - 255, 1 << 40  # (their arrays pass the distance of the others)
+    addresses = {k: far * (i + 1) for i, k in enumerate(("cached", "new", "free", "count", "table", "q_start", "kv", "slots", "positions", "left", "flags"))}
+    for batch in (most + 1, 2 ** 31 - 1):
+        assert map_call(lib, **addresses, batch=batch) == fb.ERR_SHAPE
+        assert attn_call(lib, shape=shape(B=batch), q_start=far, kv=2 * far, table=3 * far) == fb.ERR_SHAPE
+        assert lib.fedrag_paged_attn_workspace_bytes(shape(B=batch), 40, 400, 16, 8) == 0
+    # one less goes on to what comes behind: that the tables overlap, or the scratch is missing
+    assert map_call(lib, **{**addresses, "new": addresses["kv"]}, batch=most) == fb.ERR_ALIAS
+    assert attn_call(lib, shape=shape(B=most), q_start=far, kv=2 * far, table=3 * far, columns=400, ws=None) == fb.ERR_WORKSPACE
+
+
 def test_structs_match_the_header(tmp_path):
     """The binding's structs have the header's sizes and offsets."""
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
