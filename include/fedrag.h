@@ -418,6 +418,7 @@ fedrag_status fedrag_paged_map(int32_t batch, int64_t n_rows, int32_t page_token
  * and n_q_heads are not used, but must be valid).  K_rows, V_rows : n_rows rows of n_kv_heads heads, 16-byte aligned,
  * each with strides of its own (views of a projection's output, or what fedrag_scramble_kv returned).  The pages must
  * not overlap the rows, nor K's pages V's (FEDRAG_ERR_ALIAS; pages that take turns in one tensor are fine).
+ * What a launch holds: n_kv_heads <= 65535, and rows of some less than 32 GiB of K (n_rows * n_kv_heads * d elements).
  */
 fedrag_status fedrag_paged_write(const fedrag_shape* shape, int64_t n_rows, const fedrag_rows* K_rows,
                                  const fedrag_rows* V_rows, const int64_t* slots, const fedrag_paged_cache* cache,
@@ -440,6 +441,9 @@ fedrag_status fedrag_paged_write(const fedrag_shape* shape, int64_t n_rows, cons
  * Values of q_start outside [0, n_rows] are taken as the nearer bound, kv_lens below 0 as 0.
  * max_q_len : the most rows that a request is expected to have, 0 = not known.  It decides which kernels are launched,
  * never the result: requests with more rows are attended to all the same, only more slowly.
+ * Else FEDRAG_ERR_SHAPE: n_rows * (n_q_heads / n_kv_heads) <= INT32_MAX, and a launch's workgroups are fewer than 2^24
+ * (two to a compute unit, and one for every 128 rows of a KV head and its group, 16 or 32 in fp32 storage, of which a
+ * request's last may have fewer).
  * 16-bit storage: probabilities enter the second product as two storage-type terms, so that a sum keeps about 16
  * significant bits of each; everything else is fp32.
  * workspace : at least fedrag_paged_attn_workspace_bytes(...) bytes for the same arguments, 16-byte aligned.  The longest

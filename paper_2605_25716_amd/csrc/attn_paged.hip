@@ -222,15 +222,18 @@ static PagedPlan paged_plan(int B, int Hq, int Hkv, int dtype, int64_t T, int64_
     return p;
 }
 
-size_t paged_attn_workspace_bytes(int B, int Hq, int Hkv, int D, int dtype, int64_t T, int64_t max_pages, int page_tokens,
-                                  int64_t max_q_len) {
-    if (T == 0 || B == 0) return 0;
-    return paged_plan(B, Hq, Hkv, dtype, T, max_pages * page_tokens, max_q_len).bytes(D);
+bool paged_attn_fits(int B, int Hq, int Hkv, int D, int dtype, int64_t T, int64_t max_pages, int page_tokens, int64_t max_q_len, size_t* bytes) {
+    *bytes = 0;
+    if (T == 0 || B == 0) return true;
+    if (T * (Hq / Hkv) > INT32_MAX) return false;
+    const PagedPlan plan = paged_plan(B, Hq, Hkv, dtype, T, max_pages * page_tokens, max_q_len);
+    if (!grid_fits(plan.runs.grid + plan.shares.grid, 256)) return false;  // (the aggregation's is below 2^14)
+    *bytes = plan.bytes(D);
+    return true;
 }
 
 hipError_t launch_paged_attn(const PagedAttnProblem& p, hipStream_t stream) {
     const int G = p.Hq / p.Hkv;
-    if (p.T * G > INT32_MAX) return hipErrorInvalidValue;
     PagedArgs a{};
     a.Q = p.Q;
     a.q_head_stride = p.q_head_stride;
@@ -261,7 +264,6 @@ hipError_t launch_paged_attn(const PagedAttnProblem& p, hipStream_t stream) {
     };
     const PagedArgs runs = with(plan.runs, (char*)p.workspace), shares = with(plan.shares, (char*)p.workspace + plan.runs.bytes(p.D));
     const int64_t wgs_r = plan.runs.merges * plan.runs.merge_groups(p.D), wgs_s = plan.shares.merges * plan.shares.merge_groups(p.D);
-    if (wgs_r + wgs_s > 0 && !grid_fits(wgs_r + wgs_s, kPagedMergeThreads)) return hipErrorInvalidValue;
     const hipError_t e = p.dtype == FEDRAG_F32 ? launch_paged_f32(runs, plan.runs.grid, p.D, stream)
                                                : launch_paged_16(runs, plan.runs.grid, shares, plan.shares.grid, p.D, p.dtype, stream);
     if (e != hipSuccess || wgs_r + wgs_s == 0) return e;

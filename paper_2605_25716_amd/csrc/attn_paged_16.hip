@@ -31,7 +31,6 @@ FEDRAG_KERNEL __launch_bounds__(kPaged16Waves * kWave, 2) void paged_16_kernel(c
 
 template <class T, int D>
 static hipError_t launch_paged_16_t(const PagedArgs& a, int64_t chunks, const PagedArgs& d, int64_t decodes, hipStream_t stream) {
-    if (!grid_fits(chunks + decodes, kPaged16Waves * kWave)) return hipErrorInvalidValue;
     const int64_t cus = attn_target_wgs();
     const auto kernel = chunks == 0 ? paged_16_kernel<T, D, 1> : decodes == 0 ? paged_16_kernel<T, D, 2> : paged_16_kernel<T, D, 3>;
     hipLaunchKernelGGL(kernel, dim3((unsigned)(chunks + decodes)), dim3(kPaged16Waves * kWave), 0, stream, a, d, (int)chunks,

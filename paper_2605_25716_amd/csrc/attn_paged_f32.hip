@@ -217,7 +217,6 @@ FEDRAG_KERNEL __launch_bounds__(256, 2) void paged_f32_kernel(const PagedArgs a)
 }
 
 hipError_t launch_paged_f32(const PagedArgs& a, int64_t grid, int D, hipStream_t stream) {
-    if (!grid_fits(grid, 256)) return hipErrorInvalidValue;
     const bool wide = a.cut.tile_shift == 5;
     const auto kernel = D == 128 ? (wide ? paged_f32_kernel<128, 2> : paged_f32_kernel<128, 1>)
                                  : (wide ? paged_f32_kernel<64, 2> : paged_f32_kernel<64, 1>);

@@ -840,6 +840,7 @@ fedrag_status fedrag_paged_write(const fedrag_shape* shape, int64_t n_rows, cons
     j.H = shape->n_kv_heads;
     j.D = shape->d_head;
     j.elem_bytes = (int)e;
+    if (!paged_write_fits(j)) return FEDRAG_ERR_SHAPE;
     return dev(launch_paged_write(j, (hipStream_t)stream));
 }
 
@@ -848,8 +849,10 @@ size_t fedrag_paged_attn_workspace_bytes(const fedrag_shape* shape, int64_t n_ro
     if (check_shape(shape, true) != FEDRAG_OK || check_paged_sizes(shape->batch, n_rows, max_pages, max_q_len) != FEDRAG_OK ||
         !page_tokens_ok(page_tokens) || max_pages * page_tokens > kMostTokens)
         return 0;
-    return paged_attn_workspace_bytes(shape->batch, shape->n_q_heads, shape->n_kv_heads, shape->d_head, shape->dtype, n_rows, max_pages,
-                                      page_tokens, max_q_len);
+    size_t need;
+    paged_attn_fits(shape->batch, shape->n_q_heads, shape->n_kv_heads, shape->d_head, shape->dtype, n_rows, max_pages, page_tokens,
+                    max_q_len, &need);
+    return need;
 }
 
 fedrag_status fedrag_paged_attn(const fedrag_shape* shape, int64_t n_rows, const fedrag_rows* Q, const fedrag_paged_cache* cache,
@@ -876,8 +879,10 @@ fedrag_status fedrag_paged_attn(const fedrag_shape* shape, int64_t n_rows, const
     const uintptr_t words = reinterpret_cast<uintptr_t>(block_table) | reinterpret_cast<uintptr_t>(q_start) |
                             reinterpret_cast<uintptr_t>(kv_lens) | reinterpret_cast<uintptr_t>(lse);
     if (!aligned16(O) || (words & 3u) || !aligned16(workspace)) return FEDRAG_ERR_ALIAS;
-    const size_t need = paged_attn_workspace_bytes(shape->batch, shape->n_q_heads, shape->n_kv_heads, shape->d_head, shape->dtype, n_rows,
-                                                   max_pages, cache->page_tokens, max_q_len);
+    size_t need;
+    if (!paged_attn_fits(shape->batch, shape->n_q_heads, shape->n_kv_heads, shape->d_head, shape->dtype, n_rows, max_pages,
+                         cache->page_tokens, max_q_len, &need))
+        return FEDRAG_ERR_SHAPE;
     if (need > 0 && (!workspace || workspace_bytes < need)) return FEDRAG_ERR_WORKSPACE;
     const struct { const void* p; size_t n; } in[] = {{Q->data, qb}, {p.pages.K, extent}, {p.pages.V, extent}, {block_table, (size_t)table},
                                                       {q_start, ((size_t)shape->batch + 1) * 4}, {kv_lens, (size_t)shape->batch * 4}},

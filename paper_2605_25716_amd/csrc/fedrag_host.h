@@ -253,6 +253,7 @@ struct PagedWriteJob {
     int64_t n_rows;
     int H, D, elem_bytes;
 };
+bool paged_write_fits(const PagedWriteJob& job);  // whether its workgroups fit a launch
 hipError_t launch_paged_write(const PagedWriteJob& job, hipStream_t stream);
 
 // Attention of a ragged step over the pages (fedrag_paged_attn).
@@ -272,7 +273,7 @@ struct PagedAttnProblem {
     void* workspace;
 };
 hipError_t launch_paged_attn(const PagedAttnProblem& p, hipStream_t stream);
-size_t paged_attn_workspace_bytes(int B, int Hq, int Hkv, int D, int dtype, int64_t T, int64_t max_pages, int page_tokens,
-                                  int64_t max_q_len);
+// Whether a problem of these sizes fits a launch, and the workspace it needs.
+bool paged_attn_fits(int B, int Hq, int Hkv, int D, int dtype, int64_t T, int64_t max_pages, int page_tokens, int64_t max_q_len, size_t* bytes);
 
 }  // namespace fedrag

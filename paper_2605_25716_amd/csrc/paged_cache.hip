@@ -224,10 +224,15 @@ FEDRAG_KERNEL __launch_bounds__(kWriteThreads) void paged_write_kernel(PagedWrit
     *(u32x4_t*)to = *(const u32x4_t*)from;
 }
 
+static int64_t write_groups(const PagedWriteJob& job) {  // workgroups for the rows of a head
+    const int64_t rows = kWriteThreads / (job.D * job.elem_bytes / 16);
+    return (job.n_rows + rows - 1) / rows;
+}
+bool paged_write_fits(const PagedWriteJob& job) { return job.H <= 65535 && grid_fits(write_groups(job) * job.H * 2, kWriteThreads); }
+
 hipError_t launch_paged_write(const PagedWriteJob& job, hipStream_t stream) {
     const int chunks = job.D * job.elem_bytes / 16;
-    const int64_t rows = kWriteThreads / chunks, groups = (job.n_rows + rows - 1) / rows;
-    if (job.H > 65535 || !grid_fits(groups * job.H * 2, kWriteThreads)) return hipErrorInvalidValue;
+    const int64_t groups = write_groups(job);
     const auto kernel = chunks == 8 ? paged_write_kernel<8> : chunks == 16 ? paged_write_kernel<16> : paged_write_kernel<32>;
     hipLaunchKernelGGL(kernel, dim3((unsigned)groups, (unsigned)job.H, 2), dim3(kWriteThreads), 0, stream, job);
     return hipGetLastError();

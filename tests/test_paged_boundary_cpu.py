@@ -191,6 +191,23 @@ def test_most_requests(lib):
     assert attn_call(lib, shape=shape(B=most), q_start=far, kv=2 * far, table=3 * far, columns=400, ws=None) == fb.ERR_WORKSPACE
 
 
+def test_what_a_launch_holds(lib):
+    """Sizes that no launch holds are refused as sizes, and need no scratch."""
+    far = 1 << 44
+    at = dict(Q=far, O=2 * far, lse=3 * far, ws=4 * far, q_start=5 * far, kv=6 * far, table=7 * far)
+    for sizes, n_rows, max_q in ((dict(B=2, Hq=64, Hkv=1, d=64), 1 << 26, 0), (dict(B=2, Hq=64, Hkv=1, d=64), 1 << 25, 7),
+                                 (dict(B=1 << 21, Hq=8, Hkv=8, d=64, dt=fb.F32), 1 << 21, 1)):
+        kw = dict(at, shape=shape(**sizes), n_rows=n_rows, max_q=max_q, hs=0, ts=64, columns=400)
+        assert attn_call(lib, **kw) == fb.ERR_SHAPE, sizes
+        assert lib.fedrag_paged_attn_workspace_bytes(shape(**sizes), n_rows, 400, 16, max_q) == 0
+        fewer = n_rows // 4
+        assert attn_call(lib, **dict(kw, n_rows=fewer, ws=None)) == fb.ERR_WORKSPACE, sizes
+        assert lib.fedrag_paged_attn_workspace_bytes(shape(**sizes), fewer, 400, 16, max_q) > 0
+    at = dict(K=far, V=2 * far, slots=3 * far, Kp=4 * far, Vp=5 * far)
+    assert write_call(lib, **at, shape=shape(Hq=8, Hkv=8, d=128), n_rows=1 << 24) == fb.ERR_SHAPE
+    assert write_call(lib, **at, shape=shape(Hq=65536, Hkv=65536, d=128), n_rows=1) == fb.ERR_SHAPE
+
+
 def test_structs_match_the_header(tmp_path):
     """The binding's structs have the header's sizes and offsets."""
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
