@@ -445,7 +445,7 @@ fedrag_status fedrag_paged_write(const fedrag_shape* shape, int64_t n_rows, cons
  * (two to a compute unit, and one for every 128 rows of a KV head and its group, 16 or 32 in fp32 storage, of which a
  * request's last may have fewer).
  * 16-bit storage: probabilities enter the second product as two storage-type terms, so that a sum keeps about 16
- * significant bits of each; everything else is fp32.
+ * significant bits of each in bf16, and 22 in fp16, but what is below 2^-40 of the largest; everything else is fp32.
  * workspace : at least fedrag_paged_attn_workspace_bytes(...) bytes for the same arguments, 16-byte aligned.  The longest
  * requests' keys are cut into runs that are attended to side by side, and their partials land there.
  */

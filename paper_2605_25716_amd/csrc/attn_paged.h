@@ -322,6 +322,24 @@ __device__ __forceinline__ int paged_limit(const PagedArgs& a, const PagedReques
     return own < 0 ? 0 : (own < q.keys ? (int)own : q.keys);
 }
 
+// What a row's scores (in units of a factor of two) are taken relative to, from their maximum: probabilities are 2^(x - reference), in
+// the products and in the sum that they are divided by alike.  bf16: the maximum, probabilities of 1 and less.  fp16: 15 less, up to
+// 2^15, as its second term ends at 2^-24.  Relative to a largest probability of 1 tens of thousands of small ones would lose bits, or
+// all of them (131072 keys 17.5 below another came to nothing); so it ends at 2^-40 of the largest.  (The bits cost clock, and no instruction that
+// could be measured: 1024 rows of 32 heads of 128 over 16384 keys 373 us without, 387.)  A maximum of 2^20 and more is taken as it is:
+// its last place, by which an exponent may be off, has to stay far below the factor of 2 that fp16 has above 2^15.
+template <class T>
+__device__ __forceinline__ float paged_reference(float x) {
+    if constexpr (std::is_same<T, F16>::value) return x - (__builtin_fabsf(x) < 1048576.0f ? 15.0f : 0.0f);
+    return x;
+}
+// The log-sum-exp in those units, from the reference and the sum.
+template <class T>
+__device__ __forceinline__ float paged_log2_sum(float reference, float sum) {
+    if constexpr (std::is_same<T, F16>::value) return (reference + 15.0f) + fast_log2(sum * 0x1p-15f);  // (the sum of either as small as may be)
+    return reference + fast_log2(sum);
+}
+
 // 16-bit storage: workgroups for requests of many rows (a, unless `chunks` is 0) and for those of few (d, unless `decodes` is 0).
 hipError_t launch_paged_16(const PagedArgs& a, int64_t chunks, const PagedArgs& d, int64_t decodes, int D, int dtype, hipStream_t stream);
 hipError_t launch_paged_f32(const PagedArgs& a, int64_t grid, int D, hipStream_t stream);

@@ -315,7 +315,7 @@ __device__ __forceinline__ void paged_chunk_body(const PagedArgs& a, uint32_t in
                 } else if (s == 4) {
                     if constexpr (doAB) {
                         mx = xor32_max(mx);
-                        m_new = fmaxf(m_run, mx * scale_log2);
+                        m_new = fmaxf(m_run, paged_reference<T>(mx * scale_log2));
                         alph[c] = fast_exp2(m_run - m_new);
                     }
                 } else {
@@ -477,7 +477,7 @@ __device__ __forceinline__ void paged_chunk_body(const PagedArgs& a, uint32_t in
                 for (int r = 0; r < 4; ++r) o[r] = l_tot != 0.f ? acc_o[i][4 * r4 + r] * inv : 0.f;
                 *(f32x4_t*)(mine + li * (D * 4) + (((8 * i + 2 * r4 + lh) ^ (li % PCH)) << 4)) = o;
             }
-        if (lh == 0 && real) (p.runs > 1 ? z.part_lse : z.lse)[at] = l_tot != 0.f ? (m_run + fast_log2(l_tot)) * kLn2 : -INFINITY;
+        if (lh == 0 && real) (p.runs > 1 ? z.part_lse : z.lse)[at] = l_tot != 0.f ? paged_log2_sum<T>(m_run, l_tot) * kLn2 : -INFINITY;
         wave_lds_fence();
         // a store covers whole rows; where a row goes is with the lane of its number
 #pragma unroll

@@ -154,9 +154,9 @@ __device__ __forceinline__ void paged_decode_body(const PagedArgs& a, uint32_t i
 #pragma unroll
         for (int e = 0; e < 8; ++e) mx = fmaxf(mx, x[e]);
         mx = xor32_max(xor16_max(mx));
-        const float m_new = fmaxf(m_run, mx);
+        const float m_new = fmaxf(m_run, paged_reference<T>(mx));
         const float alpha = fast_exp2(m_run - m_new);
-        if (masked) {  // a key alone has the probability 1
+        if (masked) {  // a key alone has a power of two
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] -= m_new;
         } else {  // one rounding of the exponent's argument
@@ -282,7 +282,7 @@ __device__ __forceinline__ void paged_decode_body(const PagedArgs& a, uint32_t i
         const bool any = den != 0.f;  // (not a number where a score was not)
 #pragma unroll
         for (int e = 0; e < 4; ++e) num[e] = any ? num[e] / den : 0.f;
-        const float lse = any ? (M + fast_log2(den)) * kLn2 : -INFINITY;
+        const float lse = any ? paged_log2_sum<T>(M, den) * kLn2 : -INFINITY;
         const uint32_t t = FastDiv::div_by(z.by_g.m, z.by_g.s, (uint32_t)(row0 + n)), g = (uint32_t)(row0 + n) - t * z.by_g.d;
         const int64_t at = part ? (slot << z.cut.tile_shift) + n : ((int64_t)p.head * z.G + g) * z.T + q.begin + t;
         *(f32x4_t*)((part ? z.part_O : z.O) + at * D + c) = num;
