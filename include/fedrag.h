@@ -433,7 +433,9 @@ fedrag_status fedrag_paged_write(const fedrag_shape* shape, int64_t n_rows, cons
  * as far as block_table[b][..] names pages for them.  A token that a row does not see does not touch it, whatever its
  * K and V hold (NaN and infinities among it).
  *     O[h,t,:] = softmax(<Q[h,t], K> * softmax_scale) . V,   lse[h,t] = ln sum exp(<Q[h,t], K> * softmax_scale)
- * with n_q_heads / n_kv_heads query heads to a KV head; a row that sees nothing has O = 0, lse = -inf.
+ * with n_q_heads / n_kv_heads query heads to a KV head; a row that sees nothing has O = 0, lse = -inf.  Where the V of
+ * tokens that a row sees is not finite, that channel of the row's O is the sum of those values, an infinity or not a
+ * number, however small their probabilities; a score that is not a number makes all of its row's O and lse that.
  * Q : n_rows rows of n_q_heads heads with strides;  O : fp32 [n_q_heads, n_rows, d], lse : fp32 [n_q_heads, n_rows],
  * dense; padding rows of both keep what they held.
  * block_table : int32 [batch, max_pages], max_pages * page_tokens <= INT32_MAX - 255;  q_start : int32 [batch + 1], not

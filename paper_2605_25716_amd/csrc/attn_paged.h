@@ -316,10 +316,65 @@ struct PagedShares {
 };
 
 // Keys that a flattened row sees: row r of the request is token r / G, and rows / G the last.
-__device__ __forceinline__ int paged_limit(const PagedArgs& a, const PagedRequest& q, int r) {
+template <class Args>
+__device__ __forceinline__ int paged_limit(Args& a, const PagedRequest& q, int r) {
     if (!a.causal) return q.keys;
-    const int64_t own = (int64_t)q.kv - (int)a.by_g.div((uint32_t)q.R) + (int)a.by_g.div((uint32_t)r) + 1;
+    auto token = [&](int row) { return (int)FastDiv::div_by(a.by_g.m, a.by_g.s, (uint32_t)row); };
+    const int64_t own = (int64_t)q.kv - token(q.R) + token(r) + 1;
     return own < 0 ? 0 : (own < q.keys ? (int)own : q.keys);
+}
+
+// V that is not finite, of a token that a row sees: that channel of the row's output is the sum of such values, an infinity or not a
+// number, however small their probabilities.  The products do not keep to that: an infinity times a probability, factor or second
+// term that is 0 or negative comes out as not a number.  But they never lose that there was something: where a row's output is not
+// finite and its sum is a number, the kernels take the values of these channels (c .. c + 3, keys first .. last - 1 of a KV head)
+// once more and by themselves.  It costs a look at the output (calls got 0 to 1.4 % longer), and a pass over V only then.
+template <class E>
+__device__ __forceinline__ f32x4_t paged_four(const char* at) {
+    if constexpr (std::is_same<E, float>::value) return *(const f32x4_t*)at;
+    else {
+        typedef E vec4 __attribute__((ext_vector_type(4)));
+        return __builtin_convertvector(*(const vec4*)at, f32x4_t);
+    }
+}
+__device__ __forceinline__ bool all_finite(f32x4_t v) {
+    return __builtin_isfinite(v[0]) && __builtin_isfinite(v[1]) && __builtin_isfinite(v[2]) && __builtin_isfinite(v[3]);
+}
+// The sums of those values; 0 where there are none.  E: the storage type's elements.
+template <class E, int D, class Args>
+__device__ __forceinline__ f32x4_t paged_odd_values(Args& a, int b, int head, int first, int last, int c) {
+    constexpr int ROWB = D * (int)sizeof(E);
+    const int shift = a.pages.shift;
+    const uint32_t n_pages = a.pages.n_pages;
+    const int64_t page_bytes = a.pages.page_bytes;
+    const char* const V = a.pages.V + ((int64_t)head << shift) * ROWB + c * (int)sizeof(E);
+    const int32_t* const table = a.table + (int64_t)b * a.max_pages;
+    f32x4_t sum = zero_vec<f32x4_t>();
+#pragma unroll 1
+    for (int key = first; key < last;) {
+        const int in_page = key & ((1 << shift) - 1), left = last - key, to_end = (1 << shift) - in_page;
+        const int n = left < to_end ? left : to_end;  // keys of this page
+        const uint32_t id = (uint32_t)table[key >> shift];
+        key += n;
+        if (id >= n_pages) continue;
+        const char* const page = V + (int64_t)id * page_bytes + in_page * ROWB;
+        for (int i = 0; i < n; i += 8) {
+            f32x4_t v[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) v[u] = paged_four<E>(page + (i + u < n ? i + u : n - 1) * ROWB);  // (twice the last changes no sum)
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum[e] += __builtin_isfinite(v[u][e]) ? 0.f : v[u][e];
+        }
+    }
+    return sum;
+}
+// An output with its channels that hold such values.
+__device__ __forceinline__ f32x4_t paged_with_odd(f32x4_t o, f32x4_t odd) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = __builtin_isfinite(odd[e]) ? o[e] : odd[e];
+    return o;
 }
 
 // What a row's scores (in units of a factor of two) are taken relative to, from their maximum: probabilities are 2^(x - reference), in

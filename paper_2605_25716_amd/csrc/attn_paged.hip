@@ -56,6 +56,8 @@ __device__ __forceinline__ void paged_merge(const PagedArgs& a, uint32_t index, 
         *(f32x4_t*)(a.O + at * D + c * 4) = acc;
         if (c == 0) a.lse[at] = any ? M + logf(den) : -INFINITY;
     };
+    // a partial's weight: never 0 where it has any, so that what of its outputs is not finite stays (elsewhere the term is rounded off)
+    auto weight = [](float l, float M) { return l == -INFINITY ? 0.f : expf(l - M) + __FLT_DENORM_MIN__; };
     auto add = [&](float w, f32x4_t o, f32x4_t& acc, float& den) {  // (a partial of no weight takes no part, whatever it holds)
         den += w;
 #pragma unroll
@@ -82,7 +84,7 @@ __device__ __forceinline__ void paged_merge(const PagedArgs& a, uint32_t index, 
 #pragma unroll
                 for (int i = 0; i < 4; ++i) M = fmaxf(M, i < S ? l[r][i] : -INFINITY);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) add(i < S && l[r][i] != -INFINITY ? expf(l[r][i] - M) : 0.f, o[r][i], acc, den);
+                for (int i = 0; i < 4; ++i) add(i < S ? weight(l[r][i], M) : 0.f, o[r][i], acc, den);
                 if (r == 0 || n[1] != n0) put(n[r], acc, den, M);
             }
             continue;
@@ -104,7 +106,7 @@ __device__ __forceinline__ void paged_merge(const PagedArgs& a, uint32_t index, 
             for (int i0 = 0; i0 < S; i0 += NB) {
                 if (i0) load_o(i0);
                 const float l = i0 + k < S ? a.part_lse[place(i0 + k, row)] : -INFINITY;
-                const float mine = l == -INFINITY ? 0.f : expf(l - M);
+                const float mine = weight(l, M);
 #pragma unroll
                 for (int u = 0; u < NB; ++u) add(__shfl(mine, group + u), o[u], acc, den);
             }

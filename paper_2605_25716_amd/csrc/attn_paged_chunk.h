@@ -480,12 +480,29 @@ __device__ __forceinline__ void paged_chunk_body(const PagedArgs& a, uint32_t in
         if (lh == 0 && real) (p.runs > 1 ? z.part_lse : z.lse)[at] = l_tot != 0.f ? paged_log2_sum<T>(m_run, l_tot) * kLn2 : -INFINITY;
         wave_lds_fence();
         // a store covers whole rows; where a row goes is with the lane of its number
+        bool odd = false;
 #pragma unroll
         for (int u = 0; u < kPreQ * PCH / kWave; ++u) {
             const int r = (u * kWave + lane) / PCH, chunk = lane % PCH;
             const f32x4_t o = *(const f32x4_t*)(mine + r * (D * 4) + ((chunk ^ (r % PCH)) << 4));
             const int64_t to = ((int64_t)__shfl((int)(at >> 32), r) << 32) | (uint32_t)__shfl((int)at, r);
             if (row_w + r < rq.R) *(f32x4_t*)(O + to * D + chunk * 4) = o;
+            odd |= !all_finite(o);
+        }
+        if (__builtin_amdgcn_ballot_w64(odd) == 0) return;
+        // What all rows see of this lane's channels once, and for each row what it sees beyond.
+        const int chunk = lane % PCH, shared = lim_min < k_begin + L ? lim_min : k_begin + L;
+        const f32x4_t all = paged_odd_values<elem, D>(z, p.b, p.head, k_begin, shared, chunk * 4);
+#pragma unroll 1
+        for (int u = 0; u < kPreQ * PCH / kWave; ++u) {
+            const int r = (u * kWave + lane) / PCH;
+            const f32x4_t o = *(const f32x4_t*)(mine + r * (D * 4) + ((chunk ^ (r % PCH)) << 4));
+            const int64_t to = ((int64_t)__shfl((int)(at >> 32), r) << 32) | (uint32_t)__shfl((int)at, r);
+            const float sum = __shfl(l_tot, r);
+            if (row_w + r >= rq.R || all_finite(o) || !__builtin_isfinite(sum)) continue;
+            const int own = paged_limit(z, rq, row_w + r), end = own < k_begin + L ? own : k_begin + L;
+            const f32x4_t more = paged_odd_values<elem, D>(z, p.b, p.head, shared > k_begin ? shared : k_begin, end, chunk * 4);
+            *(f32x4_t*)(O + to * D + chunk * 4) = paged_with_odd(o, all + more);
         }
     };
     finish(l);

@@ -23,6 +23,7 @@ namespace fedrag {
 template <int D>
 struct PagedSmall {
     float m[kDecWaves][16], l[kDecWaves][16];
+    int lim[16];
     PagedLanes lanes;
 };
 // Wave w's slot of two arrays (by value: a choice between variables that a lambda holds puts them in scratch memory).
@@ -255,6 +256,7 @@ __device__ __forceinline__ void paged_decode_body(const PagedArgs& a, uint32_t i
     if (lq == 0) {
         sm.m[wave][lr] = m_run;
         sm.l[wave][lr] = l_tot;
+        if (wave == 0) sm.lim[lr] = lim < k_end ? lim : k_end;
     }
     if (lr < R) {
 #pragma unroll
@@ -283,6 +285,9 @@ __device__ __forceinline__ void paged_decode_body(const PagedArgs& a, uint32_t i
 #pragma unroll
         for (int e = 0; e < 4; ++e) num[e] = any ? num[e] / den : 0.f;
         const float lse = any ? paged_log2_sum<T>(M, den) * kLn2 : -INFINITY;
+        if (!all_finite(num) && __builtin_isfinite(den)) {
+            num = paged_with_odd(num, paged_odd_values<elem, D>(z, p.b, p.head, k_begin, sm.lim[n], c));
+        }
         const uint32_t t = FastDiv::div_by(z.by_g.m, z.by_g.s, (uint32_t)(row0 + n)), g = (uint32_t)(row0 + n) - t * z.by_g.d;
         const int64_t at = part ? (slot << z.cut.tile_shift) + n : ((int64_t)p.head * z.G + g) * z.T + q.begin + t;
         *(f32x4_t*)((part ? z.part_O : z.O) + at * D + c) = num;

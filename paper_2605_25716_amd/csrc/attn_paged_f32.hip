@@ -26,6 +26,7 @@ FEDRAG_KERNEL __launch_bounds__(256, 2) void paged_f32_kernel(const PagedArgs a)
     constexpr int ROWB = D * 4;
     constexpr int LDO = D + 4;
     __shared__ float sm_m[W][NQ * 16], sm_l[W][NQ * 16];
+    __shared__ int sm_lim[NQ * 16];
     __shared__ __attribute__((aligned(16))) float sm_o[W][NQ * 16][LDO];
     const int tid = threadIdx.x;
     const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
@@ -178,6 +179,7 @@ FEDRAG_KERNEL __launch_bounds__(256, 2) void paged_f32_kernel(const PagedArgs a)
         if (lq == 0) {
             sm_m[wave][n * 16 + lr] = m_run[n];
             sm_l[wave][n * 16 + lr] = l_tot;
+            if (wave == 0) sm_lim[n * 16 + lr] = lim[n];
         }
 #pragma unroll
         for (int r = 0; r < 4; ++r)
@@ -209,6 +211,9 @@ FEDRAG_KERNEL __launch_bounds__(256, 2) void paged_f32_kernel(const PagedArgs a)
         const float inv = 1.0f / den;
 #pragma unroll
         for (int e = 0; e < 4; ++e) num[e] = any ? num[e] * inv : 0.f;
+        if (!all_finite(num) && __builtin_isfinite(den)) {
+            num = paged_with_odd(num, paged_odd_values<float, D>(late_args<0>(), p.b, p.head, k_begin, sm_lim[n], c));
+        }
         const uint32_t t = a.by_g.div((uint32_t)(row0 + n)), g = (uint32_t)(row0 + n) - t * a.by_g.d;
         const int64_t at = p.runs > 1 ? ((int64_t)p.slot << a.cut.tile_shift) + n : ((int64_t)p.head * a.G + g) * a.T + rq.begin + t;
         *(f32x4_t*)((p.runs > 1 ? a.part_O : a.O) + at * D + c) = num;

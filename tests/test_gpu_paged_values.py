@@ -1,11 +1,11 @@
-"""Paged attention where the values themselves are the difficulty: long flat tails below a peak."""
+"""Paged attention where the values themselves are the difficulty: long flat tails below a peak, and V that is not finite."""
 import numpy as np
 import pytest
 import torch
 
 import paged_ref as R
 from paper_2605_25716_amd import binding as fb
-from test_gpu_paged import DT, i32
+from test_gpu_paged import DT, FILL, _attn, _attn_case, i32
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -47,3 +47,33 @@ def test_attn_flat_tails(B, n, dt, above, N, spread):
     assert worst <= 1, f"{worst:.1f} times the tolerance"
     tol_l = off + 4 * R.U * abs(want_lse) + 2.0 ** -20
     assert np.abs(lse.double().cpu().numpy() - want_lse).max() <= tol_l
+
+
+ODD = {
+    "tokens": ([1, 1, 1], [300, 2500, 33]),
+    "few": ([3, 2], [40, 700]),
+    "chunks": ([40, 150, 17], [80, 900, 2100]),
+    "mixed": ([1, 130, 2], [900, 130, 64]),
+}
+
+
+@pytest.mark.parametrize("scale", [None, 4.0], ids=["", "far"])
+@pytest.mark.parametrize("causal", [True, False], ids=["causal", "all"])
+@pytest.mark.parametrize("dt,d", [("bf16", 128), ("bf16", 64), ("f16", 128), ("f16", 64), ("f32", 128), ("f32", 64)])
+@pytest.mark.parametrize("name", list(ODD))
+def test_attn_values_that_are_not_finite(name, dt, d, causal, scale):
+    """A row that sees a token whose V is not finite has it in those channels: an infinity, or not a number where there are two of
+    both signs, whichever tokens other rows see and however small the probability.  (far: logits some hundreds apart, with
+    probabilities that are 0 in fp32, and not in 64 bits.)"""
+    q, kv = ODD[name]
+    Q, Kp, Vp, table, q_start, lens = case = _attn_case(q, kv, 8, 2, d, 16, dt)
+    inf = float("inf")
+    for b, L in enumerate(kv):
+        for t, values in ((L // 9, {3: inf, 4: -inf, 5: inf, 40: inf}), (L * 6 // 10, {5: -inf, 6: float("nan"), 41: -inf}), (L - 1, {7: inf, d - 1: -inf})):
+            for c, x in values.items():
+                Vp[table[b, t // 16], :, t % 16, c] = x
+    O, lse = _attn(case, causal, scale=scale)
+    with np.errstate(invalid="ignore"):
+        ref = R.attn_ref(*case, causal, d ** -0.5 if scale is None else scale)
+    R.check_attn(O, lse, ref, FILL, name)
+    assert np.array_equal(np.isnan(O[0].cpu().numpy()), np.isnan(ref[0]))
