@@ -112,7 +112,9 @@ def build_host_check(c_driver: str, force: bool = False, verbose: bool = False, 
         return exe
     obj = lambda s_: os.path.join(SAN_DIR, os.path.splitext(os.path.basename(s_))[0] + ".o")
     flags = [f for f in HIPCC_FLAGS if f != "-O3"] + SAN_FLAGS
-    cmds = [[hipcc] + flags + ["-c", s_, "-o", obj(s_)] for s_ in sources()]
+    newest = max(os.path.getmtime(h) for h in _headers() + [os.path.abspath(__file__)])
+    old = lambda s_: force or not os.path.exists(obj(s_)) or os.path.getmtime(obj(s_)) < max(newest, os.path.getmtime(s_))
+    cmds = [[hipcc] + flags + ["-c", s_, "-o", obj(s_)] for s_ in sources() if old(s_)]  # (drivers share the library's objects)
     include = os.path.join(_HERE, "..", "include")
     cmds.append([clang, "-std=c99", "-g", "-fsanitize=address,undefined", "-fno-sanitize-recover=undefined",
                  "-I", include, "-c", c_driver, "-o", obj(c_driver)])

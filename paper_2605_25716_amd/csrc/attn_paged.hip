@@ -227,7 +227,8 @@ static PagedPlan paged_plan(int B, int Hq, int Hkv, int dtype, int64_t T, int64_
 bool paged_attn_fits(int B, int Hq, int Hkv, int D, int dtype, int64_t T, int64_t max_pages, int page_tokens, int64_t max_q_len, size_t* bytes) {
     *bytes = 0;
     if (T == 0 || B == 0) return true;
-    if (T * (Hq / Hkv) > INT32_MAX) return false;
+    const int64_t rows = T * (Hq / Hkv);
+    if (rows > INT32_MAX || ((rows >> 4) + (B < T ? B : T)) * Hkv > INT32_MAX) return false;  // (tiles of 16 rows, the finest)
     const PagedPlan plan = paged_plan(B, Hq, Hkv, dtype, T, max_pages * page_tokens, max_q_len);
     if (!grid_fits(plan.runs.grid + plan.shares.grid, 256)) return false;  // (the aggregation's is below 2^14)
     *bytes = plan.bytes(D);

@@ -208,6 +208,17 @@ def test_what_a_launch_holds(lib):
     assert write_call(lib, **at, shape=shape(Hq=65536, Hkv=65536, d=128), n_rows=1) == fb.ERR_SHAPE
 
 
+def test_host_paths_under_sanitizers():
+    """The host side of the paged calls with the library's host code under address and undefined-behaviour sanitizers, over 200000 random
+    sizes and those at the ends; no call reaches a launch."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    exe = fbuild.build_host_check(os.path.join(root, "tests", "c", "paged_host_paths.c"))
+    env = dict(os.environ, ASAN_OPTIONS="detect_leaks=0:abort_on_error=0", UBSAN_OPTIONS="print_stacktrace=1")
+    res = subprocess.run([exe], capture_output=True, text=True, env=env, timeout=300)
+    assert res.returncode == 0, f"{res.stdout[-3000:]}\n{res.stderr[-3000:]}"
+    assert "paged host paths ok" in res.stdout
+
+
 def test_structs_match_the_header(tmp_path):
     """The binding's structs have the header's sizes and offsets."""
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
