@@ -1,4 +1,5 @@
-"""Paged attention where the values themselves are the difficulty: long flat tails below a peak, and V that is not finite."""
+"""Paged attention where the values themselves are the difficulty: long flat tails below a peak, V that is not finite; and requests by
+themselves, and under tables of the most columns."""
 import numpy as np
 import pytest
 import torch
@@ -77,3 +78,31 @@ def test_attn_values_that_are_not_finite(name, dt, d, causal, scale):
         ref = R.attn_ref(*case, causal, d ** -0.5 if scale is None else scale)
     R.check_attn(O, lse, ref, FILL, name)
     assert np.array_equal(np.isnan(O[0].cpu().numpy()), np.isnan(ref[0]))
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("causal", [True, False], ids=["causal", "all"])
+def test_attn_of_a_request_by_itself(dt, causal):
+    """What a request comes to does not hang on those beside it, but for roundings."""
+    Q, Kp, Vp, table, q_start, lens = case = _attn_case([1, 50, 1, 5], [3000, 600, 20, 1700], 8, 2, 128, 16, dt)
+    O, lse = _attn(case, causal)
+    for b in range(4):
+        rows = slice(int(q_start[b]), int(q_start[b + 1]))
+        alone = (Q[:, rows].contiguous(), Kp, Vp, table[b:b + 1], np.array([0, rows.stop - rows.start]), lens[b:b + 1])
+        ref = R.attn_ref(*alone, causal, 128 ** -0.5)
+        R.check_attn(*_attn(alone, causal), ref, FILL, f"request {b} alone")
+        R.check_attn(O[:, :, rows], lse[:, :, rows], ref, FILL, f"request {b} among others")
+
+
+@pytest.mark.parametrize("dt,q,Hq,Hkv", [("bf16", [1, 1], 600, 300), ("bf16", [20], 256, 128), ("f16", [20, 1, 1], 256, 128), ("f32", [1, 1], 600, 300),
+                                         ("f32", [20], 128, 64)])
+def test_attn_under_the_widest_table(dt, q, Hq, Hkv):
+    """As many columns as a table may have, nearly all of no page.  With so many tiles, the units that the host counts keys in are several
+    times their usual length (all units that there might be are below 2^31), and runs and shares are made of those."""
+    page, d, kv = 16, 64, [1500, 1111, 33][:len(q)]
+    Q, Kp, Vp, table, q_start, lens = _attn_case(q, kv, Hq, Hkv, d, page, dt)
+    wide = torch.full((len(q), (2 ** 31 - 256) // page), -1, dtype=torch.int32, device=DEV)
+    wide[:, :table.shape[1]] = i32(table)
+    O, lse = (torch.full((1, Hq, sum(q)) + s, FILL, dtype=torch.float32, device=DEV) for s in ((d,), ()))
+    fb.fedrag_paged_attn(Q.to(DEV), Kp.to(DEV), Vp.to(DEV), wide, i32(q_start), i32(lens), max(q), O_part=O, lse=lse)
+    R.check_attn(O, lse, R.attn_ref(Q, Kp, Vp, table, q_start, lens, True, d ** -0.5), FILL, "wide")

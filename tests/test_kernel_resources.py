@@ -118,3 +118,11 @@ def test_residency_that_the_row_products_are_cut_for(kernels):
             assert workgroups_per_unit(k) == counted(int(m[1]), m[2] == "true", m[3] == "true"), name
             checked += 1
     assert checked == 8
+
+
+def test_residency_that_paged_attention_is_cut_for(kernels):
+    """Runs and shares are made for two workgroups to a compute unit."""
+    cut = {n: k for n, k in kernels.items() if re.match(r"paged_(16|f32)_kernel<", n)}
+    assert len(cut) == 2 * 2 * 3 + 2 * 2
+    for name, k in cut.items():
+        assert workgroups_per_unit(k) >= 2, name
