@@ -11,14 +11,15 @@ namespace fedrag {
 // KV head (row r = token r / G, head r % G of the group), in tiles of 2^tile_shift rows, and n = ceil(keys / unit) units of keys (at least
 // one: a row without keys has an output all the same) for each of them.  All units together are below 2^31, which the host sees
 // to by way of `unit_shift`.  There are two ways to cut:
-//   runs    a tile's keys in equal runs of about `per` = ceil(units of all / target) units, as many as n / per rounds to; a
-//           workgroup takes one.  The target is two workgroups to a compute unit, but one while that makes runs of up to eight units
-//           (two that share it work at half the rate, and write twice the partials: 64 rows of 28 heads of 64 over 6000 keys 24.1 us
-//           with two, 20.5 with one; 128 of 32 heads of 128 over 16384, 16 units, 67.1 and 68.8), and `least` is the least.
+//   runs    a tile's keys in equal runs of about `per` = ceil(units of all / target) units (those that the mask
+//           hides among them), as many as n / per rounds to; a workgroup takes one.  The target is one workgroup to a compute unit while that makes runs of up to eight units, and two
+//           from 16 on (two that share it work at half the rate, and write twice the partials: 64 rows of 28 heads of 64 over 6000 keys,
+//           6 units, 24.1 us with two, 20.5 with one; 128 of 32 heads of 128 over 16384, 16 units, 67.1 and 68.8).  In between runs stay
+//           at eight units, and some compute units get two and some one, which was not looked at more closely.  `least` is the least.
 //           A tile is not cut where that saves less than `gain` units, or if it has at most 48 units and no more than a compute unit's
 //           part of the work and a third (1200 rows of 32 heads over 1800 keys cut 82.8 us, whole 62.4, 1000 over 1500 53.0 and 48.9;
-//           700 over 1500, one and a half times the part, 41.3 and 44.3; 1024 over 16384, 256 units, 346 and 372, as two workgroups that
-//           share a compute unit get 8 % more out of it); not so tiles of fewer rows (377 fp32 rows beside twelve single ones 42 and 56).
+//           700 over 1500, one and a half times the part, 41.3 and 44.3; 1024 over 16384, 256 units, cut 7 % less than whole, as two workgroups
+//           that share a compute unit get 8 % more out of it); not so tiles of fewer rows (377 fp32 rows beside twelve single ones 42 and 56).
 //           With a least of 1 a run has c sqrt(n) units, c = 2 / 5 for tiles of 128 rows and 1 / 5 for less: of few tiles of many keys the time to
 //           fold n / per partials grows as the time of a run falls (20 rows of 4 heads over 30000 keys, 117 runs 31.8 us, so 59 31.9,
 //           469 47.6; 3 of 14 over 6856 27, 27, 108 runs 18.0, 18.9, 25.3; one fp32 row over 30000 40.1, 31.3 by c = 1 / 5).
@@ -328,7 +329,8 @@ __device__ __forceinline__ int paged_limit(Args& a, const PagedRequest& q, int r
 // number, however small their probabilities.  The products do not keep to that: an infinity times a probability, factor or second
 // term that is 0 or negative comes out as not a number.  But they never lose that there was something: where a row's output is not
 // finite and its sum is a number, the kernels take the values of these channels (c .. c + 3, keys first .. last - 1 of a KV head)
-// once more and by themselves.  It costs a look at the output (calls got 0 to 1.4 % longer), and a pass over V only then.
+// once more and by themselves.  It costs a look at the output (calls got 0 to 1.4 % longer), and a pass over V only then
+// (with such a value in every page 64 tokens over 1000 to 32768 keys 379 -> 4620 us, 1024 rows over 16384 388 -> 1109).
 template <class E>
 __device__ __forceinline__ f32x4_t paged_four(const char* at) {
     if constexpr (std::is_same<E, float>::value) return *(const f32x4_t*)at;
@@ -380,7 +382,7 @@ __device__ __forceinline__ f32x4_t paged_with_odd(f32x4_t o, f32x4_t odd) {
 // What a row's scores (in units of a factor of two) are taken relative to, from their maximum: probabilities are 2^(x - reference), in
 // the products and in the sum that they are divided by alike.  bf16: the maximum, probabilities of 1 and less.  fp16: 15 less, up to
 // 2^15, as its second term ends at 2^-24.  Relative to a largest probability of 1 tens of thousands of small ones would lose bits, or
-// all of them (131072 keys 17.5 below another came to nothing); so it ends at 2^-40 of the largest.  (The bits cost clock, and no instruction that
+// all of them (131072 keys 17.5 below another came to nothing); so it ends at 2^-39 of the largest.  (The bits cost clock, and no instruction that
 // could be measured: 1024 rows of 32 heads of 128 over 16384 keys 373 us without, 387.)  A maximum of 2^20 and more is taken as it is:
 // its last place, by which an exponent may be off, has to stay far below the factor of 2 that fp16 has above 2^15.
 template <class T>

@@ -1,7 +1,8 @@
 // Attention over a paged cache for requests of many rows (a chunk of a prompt), 16-bit storage.  Bound by the matrix pipe, which
 // the two-term probabilities give half as much again to do, and by the vector work that does not hide behind it: 1024 rows of 32 heads
-// of 128 over 16384 keys take 354 to 361 us with the fold, 0.74 to 0.75 PFLOP/s of the visible pairs and half as much again
-// issued (a library product of bf16 reaches 1.39); 268 us with the matrix instructions alone, 199 with the vector ones.
+// of 128 over 16384 keys take 356 to 381 us with the fold, by the card, 0.70 to 0.75 PFLOP/s of the visible pairs and half as much again
+// issued (a library product of bf16 reaches 1.39); 268 us with the matrix instructions alone, 199 with the vector ones.  In fp16, whose
+// terms have more bits set, 387.
 //
 // One workgroup = 4 waves x 32 flattened rows (token r / G, head r % G: all heads of a KV head's group share its keys, and a
 // tile spans few tokens, so that little of it lies above the diagonal) of one request and KV head x one run of keys.
@@ -15,8 +16,8 @@
 //       A(t):   S^T(t) = K(t) Q^T       with B2(t-1): probabilities of keys 32..63 of tile t-1, whose maximum is known;
 //       C(t-1): O^T += V(t-1)^T P^T     with B1(t):   maximum, rescale factor and probabilities of keys 0..31 of tile t.
 //     The further a wave is in its iteration, the higher its priority over the one that it shares its SIMD with, which belongs to
-//     another workgroup: the two stay apart by half an iteration, and a barrier's last waves are not kept (without: 1024 rows over
-//     16384 keys 372 us, 361 so; 4096 over 4096 212 and 201; one step in place of three 365 and 203, the other way round 370 and 210).
+//     another workgroup: the two stay apart by half an iteration, and a barrier's last waves are not kept (without it 1024 rows over
+//     16384 keys take 3.0 % longer and 4096 over 4096 5.5 %; one step in place of three 1.1 and 1.0, the other way round 2.5 and 4.5).
 //   * Tiles are visited from the last to the first: those that some row does not see whole (the diagonal, the end of the request)
 //     come first and are finished one by one, up to the last of them, with which the pipeline starts.
 #pragma once

@@ -1,6 +1,6 @@
 // Attention over a paged cache for requests of few rows (at most 16 to a KV head with its group's heads: a decoded token,
 // a few tokens), 16-bit storage.  Bound by HBM: every K, V byte is read once (64 tokens over 1000 to 32768 keys, 32 heads of 128, 8 KV
-// heads: 2.42 GB in 371 us, 6.5 TB/s, where a read-only stream reaches 7.1), and one request by the chain of its trips (192 keys 7.0 us).
+// heads: 2.42 GB in 371 us, 6.5 TB/s, where a read-only stream reaches 7.1), and one request by the chain of its trips (192 keys 7.3 us).
 //
 // One workgroup = an even share of all KV heads' keys of all requests (attn_paged.h), one span of a head's keys after the other; its
 // waves take 32-key tiles in turn.  A tile goes
@@ -19,7 +19,8 @@
 
 namespace fedrag {
 
-// The LDS of a workgroup, shared with the other form (attn_paged_chunk.h): tiles of K and of V, an array for every two waves.
+// What a workgroup has in LDS beside its tiles of K and of V, which are arrays of the kernel (one for every two waves' slots, shared
+// with the other form): the waves' maxima and sums of the rows, the keys that a row sees, and the requests that lanes have looked up.
 template <int D>
 struct PagedSmall {
     float m[kDecWaves][16], l[kDecWaves][16];

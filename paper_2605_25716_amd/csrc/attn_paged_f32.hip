@@ -10,7 +10,8 @@
 //   O^T (d x 16) += V^T . P^T, four keys an instruction: in instruction r lane group lq contracts key 4 lq + r, whose probability it
 //   holds; channels are assigned d = DCH i + t (tile t, row i), so that lane (i = lr) needs DCH contiguous ones of each key.
 // Bound by the matrix pipe (64 NQ instructions of 32 cycles per 16 KiB of K, V at 128 columns): 1024 rows of 32 heads over 4096 keys
-// 557 us, 108 TFLOP/s, where a library product of fp32 reaches 150; single tokens by HBM (64 over 1000 keys 95 us, 5.5 TB/s).
+// 571 to 604 us, 105 TFLOP/s, where a library product of fp32 reaches 150 (every step of 16 keys rescales all outputs, a multiplication
+// for every two matrix instructions at 128 columns); single tokens by HBM (64 over 1000 keys 93 us, 5.6 TB/s).
 #include "attn_paged.h"
 
 namespace fedrag {

@@ -12,7 +12,9 @@ namespace fedrag {
 // associative as + is) and of the pages they take, carried from one thousand to the next.  Each new page is then a thread's,
 // which finds its request in the prefix sums, and so is each row, up to kMapRows of them; beyond, the rows are a launch of
 // their own over the whole chip, which reads what this one has written.  Bound by the chain of its steps: a launch that reads
-// and writes a few KB (5.0 us for 4 decoding requests, 6 for 256; 32 prompts of 4000 tokens 8.3 and 3.8).  One workgroup reads all lengths before it writes any, which is what lets a step advance in place.
+// and writes a few KB (4.8 us for 4 decoding requests, 7.0 for 256 with some chunks of prompts; 32 prompts of 4000 tokens 8.3 and 3.6).
+// A thread reads a request's lengths before it writes them, and the second launch takes what the first has written: that is what lets
+// a step advance in place.
 constexpr int kMapThreads = 1024;
 
 struct MapPrefix {
