@@ -235,7 +235,7 @@ def prepare(case, seed):
     if c["kind"] == "tree_map":
         T = c["T"]
         return dict(case=c, parents=_dev32(g.parents(q) + [-1] * (T - sum(q))), q_start=_dev32(start), kv=_dev32(kv),
-                    mask=new((T, c["words"]), torch.int64), positions=new(T), flags=new(1))
+                    mask=new((T, c["words"]), torch.int64), positions=new(T), flags=new(len(kv)))
     P = c["page"]
     if c["kind"] == "trim":
         table, n_pages, spare = _table(g, kv, P, 40)
