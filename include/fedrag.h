@@ -7,7 +7,7 @@
  * - Every data pointer is DEVICE memory owned by the caller, 16-byte aligned, dense row-major (the rows of the paged
  *   calls have strides).  The library never allocates, frees or keeps a pointer after the call returns.  Three kinds of
  *   argument are HOST memory and say so where they are declared: the fedrag_structured_key structs, the fedrag_rows and
- *   fedrag_paged_cache structs (all of which hold device pointers) and the per-shard arrays of
+ *   fedrag_paged_cache structs and arrays (all of which hold device pointers) and the per-shard arrays of
  *   fedrag_partial_attn_shards; they are read during the call only.
  * - Tensors are laid out [batch, heads, tokens, d_head] ("[B,H,L,d]").  Query head h uses KV head
  *   h / (n_q_heads / n_kv_heads); scrambling matrices are per KV head, [n_kv_heads, d, d], row-major,
@@ -462,6 +462,124 @@ fedrag_status fedrag_paged_attn(const fedrag_shape* shape, int64_t n_rows, const
  * cut into fewer runs); whatever the sizes, 69 MiB are enough on a device of 256 compute units. */
 size_t fedrag_paged_attn_workspace_bytes(const fedrag_shape* shape, int64_t n_rows, int64_t max_pages,
                                          int32_t page_tokens, int64_t max_q_len);
+
+/*
+ * A drafted step.  A request brings its last token and drafts of what may follow it, several for one place among them: a tree.  Its
+ * rows are the tree's nodes: row 0 the token that is decided already, the others drafts, each behind its parent.  All of them are
+ * tokens of the cache for now, in the order of the rows, planned by fedrag_paged_map and written by fedrag_paged_write.
+ * fedrag_tree_map makes masks and positions of the parents, fedrag_paged_tree_attn is the attention in which a row sees what the
+ * request had before and its own ancestors (a Compute Node's part is fedrag_paged_attn without a mask, as for any rows),
+ * fedrag_tree_verify decides which rows stay and draws the next token, fedrag_paged_keep moves the K, V of those that stay to where
+ * they belong, and fedrag_paged_trim returns the pages that are no longer needed.  Decoding costs a trip between Inquirer and Compute
+ * Nodes for every token and layer (Section 5.3): several drafts in one step share it.
+ *
+ * Row t of request b, t = q_start[b] .. q_start[b+1]-1, is node i = t - q_start[b]; n = q_start[b+1] - q_start[b] is the number of its
+ * nodes.  q_start and what lies behind the last request are as in the paged calls.
+ */
+
+/*
+ * parents[t] = index of the node's parent among the request's, below its own; -1: it has none (it follows what is in the cache).
+ *     bit j % 64 of tree_mask[t][j / 64]: node j is the row's own or an ancestor, j < 64 * mask_words;
+ *     positions[t] = kv_lens[b] - n + the number of its ancestors  (what a rotary embedding turns by);
+ *     padding rows: 0 and -1.
+ * kv_lens : int32 [batch], the rows among them;  parents : int32 [n_rows];  tree_mask : uint64 [n_rows, mask_words], 8-byte aligned;
+ * positions : int32 [n_rows] or NULL;  flags : int32 [batch], receives 0 or the sum of
+ *     1  a parent outside [-1, i) (taken as -1);   2  more than 64 * mask_words nodes (the bits beyond are not there).
+ * mask_words : 1 .. FEDRAG_TREE_WORDS.  Out of place.  A mask need not come from here: any bits will do for the attention.
+ */
+#define FEDRAG_TREE_WORDS 64
+#define FEDRAG_TREE_BAD_PARENT 1
+#define FEDRAG_TREE_NO_WORDS 2
+fedrag_status fedrag_tree_map(int32_t batch, int64_t n_rows, int32_t mask_words, const int32_t* q_start, const int32_t* kv_lens,
+                              const int32_t* parents, uint64_t* tree_mask, int32_t* positions, int32_t* flags, void* stream);
+
+/*
+ * fedrag_paged_attn with a mask of its own for each row: of the request's tokens, as far as block_table names pages for them, row t
+ * sees the first kv_lens[b] - n, and token kv_lens[b] - n + j if bit j of tree_mask[t] is set, 0 <= j < n, j < 64 * mask_words.
+ * tree_mask : uint64 [n_rows, mask_words], 8-byte aligned, any bits (an ancestor is not told from another node);
+ * a row without any bit sees the tokens of before, and if there are none, it has O = 0, lse = -inf.
+ * Everything else as fedrag_paged_attn: strides, rounding, what is not finite, padding rows, max_q_len, the workspace's use.
+ */
+fedrag_status fedrag_paged_tree_attn(const fedrag_shape* shape, int64_t n_rows, const fedrag_rows* Q,
+                                     const fedrag_paged_cache* cache, const int32_t* block_table, int64_t max_pages,
+                                     const int32_t* q_start, const int32_t* kv_lens, const uint64_t* tree_mask, int32_t mask_words,
+                                     int64_t max_q_len, float softmax_scale, float* O, float* lse,
+                                     void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace fedrag_paged_tree_attn needs for these sizes, by the rules of fedrag_paged_attn_workspace_bytes. */
+size_t fedrag_paged_tree_attn_workspace_bytes(const fedrag_shape* shape, int64_t n_rows, int64_t max_pages,
+                                              int32_t page_tokens, int64_t max_q_len);
+
+/*
+ * Which drafts stay, and the token that follows them: the result is distributed as if every token had been drawn from the target's
+ * probabilities, whatever the drafts are, if each draft was drawn from the draft's probabilities of its parent, independently of its
+ * siblings, and the random numbers are uniform.
+ * The walk begins at node 0.  At a node its children are tried in the order of their index; p, q are the node's rows of target and
+ * draft, and x = tokens[child].  With C = 0, M = 1 on arrival, and r(v) = max(p(v) - C q(v), 0):
+ *     the child is accepted if u[child] * q(x) * M < r(x): the walk goes on there;
+ *     else C <- C + M, and then M <- sum_v r(v) with this C  (what remains of p as often as q was taken from it, not normalised).
+ * When no child is left, or max_kept nodes are accepted, the next token is drawn from r: the first v with sum_{w <= v} r(w) > u_next[b]
+ * * sum_w r(w).  If nothing is left of r, p takes its place; if p has nothing either, the token is -1.
+ * draft = NULL: drafts that were not drawn (looked up, say; or the likeliest ones).  Then q is 1 at the child's token and 0 elsewhere:
+ * r is p without the tokens rejected at the node, each once, M is 1 less their p.
+ * Weights of tokens are counted in whole units of 2^-43, each rounded to nearest even once, and their sums M and C are whole
+ * numbers: nothing depends on the order of sums, and a token with p below 2^-44 is not drawn.  Products and differences are formed in
+ * 64-bit floating point in the order written, each rounded by itself; a threshold is rounded down to units.
+ * Values are taken as between 0 and 1, not a number as 0; a child whose token lies outside [0, vocab) is passed by as if it were not there.
+ * target, draft : [n_rows, vocab] of storage type dtype, row t at t * target_stride (draft_stride) elements, >= vocab, the strides and
+ * addresses any multiples of an element;  tokens, parents : int32 [n_rows] (a parent that is not below its child is none);
+ * u : double [n_rows], u_next : double [batch], in [0, 1), 8-byte aligned (outside: as the nearest);
+ * kept : int32 [batch, max_kept], the nodes of the accepted path, beginning with 0, and 0 behind them;  n_kept, next_token : int32
+ * [batch];  a request of no rows has n_kept = 0, next_token = -1.  batch : 0 .. 65535;  vocab : 1 .. 2^20;  max_kept : 1 .. INT32_MAX.
+ * workspace : fedrag_tree_verify_workspace_bytes(batch, vocab) bytes, 16-byte aligned.  Out of place.
+ */
+fedrag_status fedrag_tree_verify(int32_t batch, int64_t n_rows, int64_t vocab, int32_t dtype, const int32_t* q_start,
+                                 const int32_t* parents, const int32_t* tokens, const void* target, int64_t target_stride,
+                                 const void* draft, int64_t draft_stride, const double* u, const double* u_next, int64_t max_kept,
+                                 int32_t* kept, int32_t* n_kept, int32_t* next_token,
+                                 void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace fedrag_tree_verify needs; 0 for sizes it would reject. */
+size_t fedrag_tree_verify_workspace_bytes(int32_t batch, int64_t vocab);
+
+/*
+ * The rows that stay, moved together: for j = 0 .. n_kept[b]-1
+ *     K, V of the request's token kv_lens[b] - n + j  <-  those of its token kv_lens[b] - n + kept[b][j]
+ * in place, as if all were read before any is written, in each of n_caches caches (the layers', which share lengths and table).  Bytes
+ * are moved as they are; the other tokens keep theirs.  The n tokens need not be a tree: with q_start the sums of kv_lens they are all
+ * of the request's, which thins it out.
+ * kept : int32 [batch, max_kept], rising within a request, each in [0, n) (where a list does not keep to that, the tokens from
+ * kv_lens[b] - n on hold anything afterwards, and nothing else is touched);  n_kept : int32 [batch], values outside [0, min(n, max_kept)]
+ * are taken as the nearer bound.  A token without a page is neither read nor written.
+ * shape: batch, n_kv_heads, d_head, dtype (n_q_heads is not used, but must be valid).  caches : HOST array of n_caches structs, 1 ..
+ * FEDRAG_KEEP_CACHES, all of the same page_tokens; their pages must not overlap each other, nor the arrays (FEDRAG_ERR_ALIAS).
+ * max_kept : 0 .. INT32_MAX;  max_pages * page_tokens <= INT32_MAX - 255;  batch * n_kv_heads * n_caches below 2^20, else
+ * FEDRAG_ERR_SHAPE.
+ */
+#define FEDRAG_KEEP_CACHES 64
+fedrag_status fedrag_paged_keep(const fedrag_shape* shape, int32_t n_caches, const fedrag_paged_cache* caches,
+                                const int32_t* block_table, int64_t max_pages, const int32_t* q_start, const int32_t* kv_lens,
+                                const int32_t* kept, int64_t max_kept, const int32_t* n_kept, void* stream);
+
+/*
+ * The bookkeeping behind it.  Request b goes on with
+ *     lens_out[b] = kv_lens[b] - n + n_kept[b]   (q_start = NULL: n_kept[b]; 0 releases the request)
+ * of its kv_lens[b] tokens, and the pages of its table that hold none of them are put on the stack free_pages[0 .. *free_count-1]: request
+ * by request, column by column, the last one on top; *free_left = what is on the stack then.  Entries of the table keep what they hold,
+ * and those below 0 are no pages.
+ * kv_lens, n_kept, lens_out : int32 [batch];  q_start : int32 [batch + 1] or NULL;  block_table : int32 [batch, max_pages];  free_pages :
+ * int32 [n_free], in and out;  free_count, free_left, flags : int32 [1].
+ * lens_out may be kv_lens and free_left may be free_count; otherwise nothing that is written may overlap anything.  With those two the
+ * next fedrag_paged_map takes cached_lens = lens_out.
+ * flags receives 0, or the sum of
+ *     1  the stack has no room for all of them: those that come last are lost to it;
+ *     2  a length outside [0, kv_lens[b]], kv_lens[b] below 0, or *free_count outside [0, n_free] (each taken as the nearer bound).
+ */
+#define FEDRAG_TRIM_NO_ROOM 1
+#define FEDRAG_TRIM_BAD_LENGTH 2
+fedrag_status fedrag_paged_trim(int32_t batch, int32_t page_tokens, int64_t max_pages, const int32_t* kv_lens, const int32_t* q_start,
+                                const int32_t* n_kept, const int32_t* block_table, int32_t* free_pages, int64_t n_free,
+                                const int32_t* free_count, int32_t* lens_out, int32_t* free_left, int32_t* flags, void* stream);
 
 /* inv_out[perm[j]] = j for j in [0, L): the gather array that undoes `perm`.  Device pointers. */
 fedrag_status fedrag_invert_perm(const int32_t* perm, int64_t L, int32_t* inv_out, void* stream);

@@ -29,12 +29,18 @@ EXPORTS = ("fedrag_scramble_kv", "fedrag_scramble_q", "fedrag_partial_attn", "fe
            "fedrag_local_attn", "fedrag_unpermute_lse", "fedrag_partial_attn_varlen", "fedrag_quantize_rows",
            "fedrag_dequantize_rows", "fedrag_scramble_kv_quantized", "fedrag_scramble_kv_structured_quantized",
            "fedrag_partial_attn_quantized", "fedrag_partial_attn_varlen_quantized", "fedrag_paged_map",
-           "fedrag_paged_write", "fedrag_paged_attn", "fedrag_paged_attn_workspace_bytes", "fedrag_invert_perm",
+           "fedrag_paged_write", "fedrag_paged_attn", "fedrag_paged_attn_workspace_bytes", "fedrag_tree_map",
+           "fedrag_paged_tree_attn", "fedrag_paged_tree_attn_workspace_bytes", "fedrag_tree_verify",
+           "fedrag_tree_verify_workspace_bytes", "fedrag_paged_keep", "fedrag_paged_trim", "fedrag_invert_perm",
            "fedrag_validate_perm", "fedrag_status_string",
            "fedrag_version")
 
 # what fedrag_paged_map's flags are the sum of
 MAP_NO_PAGES, MAP_NO_COLUMNS, MAP_NO_ROWS, MAP_BAD_LENGTH = 1, 2, 4, 8
+# fedrag_tree_map's flags of a request, fedrag_paged_trim's
+TREE_BAD_PARENT, TREE_NO_WORDS = 1, 2
+TRIM_NO_ROOM, TRIM_BAD_LENGTH = 1, 2
+TREE_WORDS, KEEP_CACHES = 64, 64  # FEDRAG_TREE_WORDS, FEDRAG_KEEP_CACHES
 
 
 class Shape(ctypes.Structure):
@@ -123,6 +129,17 @@ def load() -> ctypes.CDLL:
                                           ctypes.c_size_t, vp]
         lib.fedrag_paged_attn_workspace_bytes.argtypes = [sp, i64, i64, i32, i64]
         lib.fedrag_paged_attn_workspace_bytes.restype = ctypes.c_size_t
+        lib.fedrag_tree_map.argtypes = [i32, i64, i32, vp, vp, vp, vp, vp, vp, vp]
+        lib.fedrag_paged_tree_attn.argtypes = [sp, i64, rp, cp, vp, i64, vp, vp, vp, i32, i64, ctypes.c_float, f32p, f32p, vp,
+                                               ctypes.c_size_t, vp]
+        lib.fedrag_paged_tree_attn_workspace_bytes.argtypes = lib.fedrag_paged_attn_workspace_bytes.argtypes
+        lib.fedrag_paged_tree_attn_workspace_bytes.restype = ctypes.c_size_t
+        lib.fedrag_tree_verify.argtypes = [i32, i64, i64, i32, vp, vp, vp, vp, i64, vp, i64, vp, vp, i64, vp, vp, vp, vp,
+                                           ctypes.c_size_t, vp]
+        lib.fedrag_tree_verify_workspace_bytes.argtypes = [i32, i64]
+        lib.fedrag_tree_verify_workspace_bytes.restype = ctypes.c_size_t
+        lib.fedrag_paged_keep.argtypes = [sp, i32, cp, vp, i64, vp, vp, vp, i64, vp, vp]
+        lib.fedrag_paged_trim.argtypes = [i32, i32, i64, vp, vp, vp, vp, vp, i64, vp, vp, vp, vp, vp]
         lib.fedrag_invert_perm.argtypes = [vp, i64, vp, vp]
         lib.fedrag_validate_perm.argtypes = [vp, i32, i64, vp, vp, vp]
         lib.fedrag_status_string.argtypes = [ctypes.c_int]
@@ -136,7 +153,8 @@ def load() -> ctypes.CDLL:
                      "fedrag_dequantize_rows", "fedrag_scramble_kv_quantized",
                      "fedrag_scramble_kv_structured_quantized", "fedrag_partial_attn_quantized",
                      "fedrag_partial_attn_varlen_quantized", "fedrag_paged_map", "fedrag_paged_write",
-                     "fedrag_paged_attn"):
+                     "fedrag_paged_attn", "fedrag_tree_map", "fedrag_paged_tree_attn", "fedrag_tree_verify",
+                     "fedrag_paged_keep", "fedrag_paged_trim"):
             getattr(lib, name).restype = ctypes.c_int
         _lib = lib
     return _lib
@@ -697,6 +715,175 @@ def fedrag_paged_attn(Q, K_pages, V_pages, block_table, q_start, kv_lens, max_q_
     if st != OK:
         raise FedragError(st, "fedrag_paged_attn")
     return O_part, lse
+
+
+def fedrag_tree_map(parents, q_start, kv_lens, mask_words: int, tree_mask=None, positions=None, flags=None):
+    """Masks and positions of a drafted step's rows from the nodes' parents (int32 [n_rows], indices within the request, -1 for none):
+    (tree_mask int64 [n_rows, mask_words], positions int32 [n_rows], flags int32 [B]: 0 or a sum of TREE_* for each request).
+    Bit j % 64 of a row's word j / 64: node j is the row's own or an ancestor."""
+    dev, i32 = _device(parents), torch.int32
+    n_rows, B, mask_words = parents.numel(), kv_lens.numel(), index(mask_words)
+    if mask_words < 1:
+        raise ValueError("mask_words: at least one for every 64 nodes")
+    new = lambda *n, dt=i32: torch.empty(n, dtype=dt, device=parents.device)  # noqa: E731
+    tree_mask = new(n_rows, mask_words, dt=torch.int64) if tree_mask is None else tree_mask
+    positions = new(n_rows) if positions is None else positions
+    flags = new(B) if flags is None else flags
+    st = load().fedrag_tree_map(
+        B, n_rows, mask_words, _values("q_start", q_start, i32, dev, B + 1), _values("kv_lens", kv_lens, i32, dev, B),
+        _values("parents", parents, i32, dev, n_rows), _exactly("tree_mask", tree_mask, torch.int64, dev, (n_rows, mask_words)),
+        _values("positions", positions, i32, dev, n_rows), _values("flags", flags, i32, dev, B), torch._C._cuda_getCurrentRawStream(dev))
+    if st != OK:
+        raise FedragError(st, "fedrag_tree_map")
+    return tree_mask, positions, flags
+
+
+def fedrag_paged_tree_attn_workspace_bytes(batch, n_q_heads, n_kv_heads, d_head, dtype, n_rows, max_pages, page_tokens, max_q_len) -> int:
+    """Bytes for one call of these sizes."""
+    shape = _shape_ref_of_numbers(batch, n_q_heads, n_kv_heads, d_head, dtype)
+    return int(load().fedrag_paged_tree_attn_workspace_bytes(shape, n_rows, max_pages, page_tokens, max_q_len))
+
+
+@functools.lru_cache(maxsize=256)
+def _tree_need(dev, *sizes) -> int:
+    return fedrag_paged_tree_attn_workspace_bytes(*sizes)
+
+
+def fedrag_paged_tree_attn(Q, K_pages, V_pages, block_table, q_start, kv_lens, tree_mask, max_q_len: int = 0,
+                           softmax_scale: Optional[float] = None, O_part=None, lse=None, workspace=None):
+    """fedrag_paged_attn with a mask for each row: a request's rows q_start[b] .. q_start[b+1]-1 are the last of its kv_lens[b] tokens; a
+    row sees all tokens before them, and of them those whose bit is set in its words of tree_mask (int64 [T, words], as
+    fedrag_tree_map makes them)."""
+    dev, dtype, i32, f32 = _device(K_pages), K_pages.dtype, torch.int32, torch.float32
+    (_, Hkv, P, dk), cache = _pages(K_pages, V_pages, dev)
+    (Hq, T, d), rq = _rows("Q", Q, dtype, dev)
+    if d != dk:
+        raise ValueError("Q [Hq, T, d] and the pages [n_pages, Hkv, page_tokens, d] do not match")
+    if block_table.dim() != 2:
+        raise ValueError("block_table: int32 [B, max_pages]")
+    if tree_mask.dim() != 2:
+        raise ValueError("tree_mask: int64 [T, words]")
+    (B, columns), words = block_table.shape, tree_mask.shape[1]
+    max_q_len = index(max_q_len)
+    if softmax_scale is None:
+        softmax_scale = float(d) ** -0.5
+    O_part = torch.empty((1, Hq, T, d), dtype=f32, device=Q.device) if O_part is None else O_part
+    lse = torch.empty((1, Hq, T), dtype=f32, device=Q.device) if lse is None else lse
+    if workspace is None:
+        ws, ws_bytes = None, _tree_need(dev, B, Hq, Hkv, d, dtype, T, columns, P, max_q_len)
+        if ws_bytes:
+            workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=Q.device)
+            ws = workspace.data_ptr()
+    else:
+        ws, ws_bytes = _values("workspace", workspace, workspace.dtype, dev, 0), workspace.numel() * workspace.element_size()
+    st = load().fedrag_paged_tree_attn(
+        _shape_ref(B, Hq, Hkv, d, dtype), T, rq, cache, _exactly("block_table", block_table, i32, dev, (B, columns)), columns,
+        _values("q_start", q_start, i32, dev, B + 1), _exactly("kv_lens", kv_lens, i32, dev, (B,)),
+        _exactly("tree_mask", tree_mask, torch.int64, dev, (T, words)), words, max_q_len, softmax_scale,
+        _values("O_part", O_part, f32, dev, Hq * T * d), _values("lse", lse, f32, dev, Hq * T), ws, ws_bytes,
+        torch._C._cuda_getCurrentRawStream(dev))
+    if st != OK:
+        raise FedragError(st, "fedrag_paged_tree_attn")
+    return O_part, lse
+
+
+def fedrag_tree_verify_workspace_bytes(batch: int, vocab: int) -> int:
+    return int(load().fedrag_tree_verify_workspace_bytes(index(batch), index(vocab)))
+
+
+def _vocab_rows(name, X, dtype, dev, n_rows, vocab):
+    """(address, elements from a row to the next) of [n_rows, vocab] with any row stride that is not smaller."""
+    if X.get_device() != dev or X.dtype is not dtype or X.shape != (n_rows, vocab):
+        _refuse(name, X, dtype, dev, f"shape {[n_rows, vocab]}")
+    if (vocab > 1 and X.stride(1) != 1) or (n_rows > 1 and X.stride(0) < vocab):
+        raise ValueError(f"{name}: the values of a row have to lie side by side, and rows apart")
+    return X.data_ptr(), X.stride(0) if n_rows > 1 else vocab
+
+
+def fedrag_tree_verify(target, tokens, parents, q_start, u, u_next, draft=None, max_kept: int = 0, kept=None, n_kept=None,
+                       next_token=None, workspace=None):
+    """The walk over a drafted step's trees: (kept int32 [B, max_kept]: the accepted nodes of each request, node 0 first; n_kept int32
+    [B]; next_token int32 [B]).  target [n_rows, vocab]: the probabilities that follow each node; draft: those that its children were
+    drawn from, or None if they were not drawn; tokens, parents int32 [n_rows]; u float64 [n_rows], u_next float64 [B]: uniform in
+    [0, 1).  max_kept: 16 if neither it nor kept is given."""
+    dev, i32, f64 = _device(target), torch.int32, torch.float64
+    if target.dim() != 2 or target.dtype not in _DTYPES:
+        raise ValueError("target: [n_rows, vocab] in fp32, bf16 or fp16")
+    (n_rows, vocab), B = target.shape, u_next.numel()
+    new = lambda *n: torch.empty(n, dtype=i32, device=target.device)  # noqa: E731
+    kept = new(B, index(max_kept) or 16) if kept is None else kept
+    if kept.dim() != 2:
+        raise ValueError("kept: int32 [B, max_kept]")
+    columns = kept.shape[1]
+    if max_kept and index(max_kept) != columns:
+        raise ValueError("max_kept is the number of kept's columns")
+    n_kept = new(B) if n_kept is None else n_kept
+    next_token = new(B) if next_token is None else next_token
+    target_at, target_stride = _vocab_rows("target", target, target.dtype, dev, n_rows, vocab)
+    draft_at, draft_stride = (None, 0) if draft is None else _vocab_rows("draft", draft, target.dtype, dev, n_rows, vocab)
+    if workspace is None:
+        workspace = torch.empty(max(fedrag_tree_verify_workspace_bytes(B, vocab), 16), dtype=torch.uint8, device=target.device)
+    st = load().fedrag_tree_verify(
+        B, n_rows, vocab, _DTYPES[target.dtype], _values("q_start", q_start, i32, dev, B + 1), _values("parents", parents, i32, dev, n_rows),
+        _values("tokens", tokens, i32, dev, n_rows), target_at, target_stride, draft_at, draft_stride, _values("u", u, f64, dev, n_rows),
+        _values("u_next", u_next, f64, dev, B), columns, _exactly("kept", kept, i32, dev, (B, columns)),
+        _values("n_kept", n_kept, i32, dev, B), _values("next_token", next_token, i32, dev, B),
+        _values("workspace", workspace, workspace.dtype, dev, 0), workspace.numel() * workspace.element_size(),
+        torch._C._cuda_getCurrentRawStream(dev))
+    if st != OK:
+        raise FedragError(st, "fedrag_tree_verify")
+    return kept, n_kept, next_token
+
+
+def fedrag_paged_keep(caches, block_table, q_start, kv_lens, kept, n_kept):
+    """Moves the K, V of the rows that stay to the front of each request's rows, in place, in every one of the caches, a list of (K_pages,
+    V_pages) of one shape and type but for their numbers of pages.  kept int32 [B, max_kept], rising; n_kept int32 [B]."""
+    if not caches:
+        raise ValueError("caches: a list of (K_pages, V_pages)")
+    first, i32 = caches[0][0], torch.int32
+    dev, dtype = _device(first), first.dtype
+    structs = (PagedCache * len(caches))()
+    for at, (K_pages, V_pages) in zip(structs, caches):
+        shape = K_pages.shape
+        if V_pages.shape != shape or V_pages.stride() != K_pages.stride() or V_pages.dtype is not dtype or K_pages.dtype is not dtype or \
+                K_pages.get_device() != dev or V_pages.get_device() != dev or shape[1:] != first.shape[1:]:
+            raise ValueError("caches: K_pages and V_pages alike in shape, type, strides and device, and all of them but for n_pages")
+        at.K, at.V, at.n_pages, at.page_stride, at.page_tokens = (K_pages.data_ptr(), V_pages.data_ptr(), shape[0],
+                                                                   _page_stride(shape, K_pages.stride()), shape[2])
+    if block_table.dim() != 2 or kept.dim() != 2:
+        raise ValueError("block_table: int32 [B, max_pages], kept: int32 [B, max_kept]")
+    (B, columns), (_, H, _, d), most = block_table.shape, first.shape, kept.shape[1]
+    st = load().fedrag_paged_keep(
+        _shape_ref(B, H, H, d, dtype), len(caches), structs, _exactly("block_table", block_table, i32, dev, (B, columns)), columns,
+        _values("q_start", q_start, i32, dev, B + 1), _exactly("kv_lens", kv_lens, i32, dev, (B,)), _exactly("kept", kept, i32, dev, (B, most)),
+        most, _exactly("n_kept", n_kept, i32, dev, (B,)), torch._C._cuda_getCurrentRawStream(dev))
+    if st != OK:
+        raise FedragError(st, "fedrag_paged_keep")
+    return caches
+
+
+def fedrag_paged_trim(kv_lens, n_kept, block_table, free_pages, free_count, page_tokens: int, q_start=None, lens_out=None, free_left=None,
+                      flags=None):
+    """What is left of the requests: (lens_out int32 [B], free_left int32 [1], flags int32 [1]).  Request b keeps kv_lens[b] - n + n_kept[b]
+    of its tokens, n = q_start[b+1] - q_start[b] (without q_start: n_kept[b]), and its other pages go on the stack
+    free_pages[:free_count], in place.  lens_out may be kv_lens and free_left may be free_count.  flags: 0 or a sum of TRIM_*."""
+    if block_table.dim() != 2:
+        raise ValueError("block_table: int32 [B, max_pages]")
+    dev, i32 = _device(block_table), torch.int32
+    (B, columns), page_tokens = block_table.shape, index(page_tokens)
+    new = lambda n: torch.empty(n, dtype=i32, device=block_table.device)  # noqa: E731
+    lens_out = new(B) if lens_out is None else lens_out
+    free_left = new(1) if free_left is None else free_left
+    flags = new(1) if flags is None else flags
+    st = load().fedrag_paged_trim(
+        B, page_tokens, columns, _exactly("kv_lens", kv_lens, i32, dev, (B,)),
+        None if q_start is None else _values("q_start", q_start, i32, dev, B + 1), _exactly("n_kept", n_kept, i32, dev, (B,)),
+        _exactly("block_table", block_table, i32, dev, (B, columns)), _values("free_pages", free_pages, i32, dev, 0), free_pages.numel(),
+        _values("free_count", free_count, i32, dev, 1), _exactly("lens_out", lens_out, i32, dev, (B,)),
+        _values("free_left", free_left, i32, dev, 1), _values("flags", flags, i32, dev, 1), torch._C._cuda_getCurrentRawStream(dev))
+    if st != OK:
+        raise FedragError(st, "fedrag_paged_trim")
+    return lens_out, free_left, flags
 
 
 def fedrag_invert_perm(perm, inv_out=None):

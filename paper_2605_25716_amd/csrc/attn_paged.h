@@ -49,6 +49,8 @@ struct PagedArgs {
     float *part_O, *part_lse;  // [slot][rows of a tile][D], [slot][rows of a tile]
     uint32_t slots;
     PagedCut cut;
+    const uint64_t* tree;  // a mask for each row, [T][tree_words]; only for kernels made for it, with causal = 0
+    int tree_words;
 };
 
 // Arguments number N of a kernel, all of this type, read again from memory from here on: what is needed between inner loops would
@@ -325,6 +327,20 @@ __device__ __forceinline__ int paged_limit(Args& a, const PagedRequest& q, int r
     return own < 0 ? 0 : (own < q.keys ? (int)own : q.keys);
 }
 
+// Masks of rows.  A request's rows are its last tokens, the first of which is number `paged_base`; bit j of token t's mask says
+// whether it sees the j-th of them, and all see what comes before.
+__device__ __forceinline__ int paged_base(const PagedRequest& q, int tokens) { return q.kv - tokens; }  // (may be below 0: kv is not)
+// Whether the row of token t sees keys key0 .. key0 + 63, the first in bit 0.
+template <class Args>
+__device__ __forceinline__ uint64_t paged_tree_bits(Args& a, const PagedRequest& q, int base, int t, int key0) {
+    const int64_t first = (int64_t)key0 - base;
+    const int64_t w = first >> 6;
+    const uint64_t* const mask = a.tree + ((int64_t)q.begin + t) * a.tree_words;
+    const uint64_t lo = w < 0 ? ~(uint64_t)0 : (w < a.tree_words ? mask[w] : 0), hi = w < -1 ? ~(uint64_t)0 : (w + 1 < a.tree_words ? mask[w + 1] : 0);
+    const int shift = (int)(first & 63);
+    return shift ? lo >> shift | hi << (64 - shift) : lo;
+}
+
 // V that is not finite, of a token that a row sees: that channel of the row's output is the sum of such values, an infinity or not a
 // number, however small their probabilities.  The products do not keep to that: an infinity times a probability, factor or second
 // term that is 0 or negative comes out as not a number.  But they never lose that there was something: where a row's output is not
@@ -372,6 +388,16 @@ __device__ __forceinline__ f32x4_t paged_odd_values(Args& a, int b, int head, in
     }
     return sum;
 }
+// The same over what the row of token t sees by its mask of keys first .. last - 1.
+template <class E, int D, class Args>
+__device__ __forceinline__ f32x4_t paged_odd_tree_values(Args& a, const PagedRequest& q, int base, int t, int b, int head, int first, int last, int c) {
+    const int split = base < first ? first : (base < last ? base : last);
+    f32x4_t sum = paged_odd_values<E, D>(a, b, head, first, split, c);
+#pragma unroll 1
+    for (int key = split; key < last; ++key)
+        if (paged_tree_bits(a, q, base, t, key) & 1) sum += paged_odd_values<E, D>(a, b, head, key, key + 1, c);
+    return sum;
+}
 // An output with its channels that hold such values.
 __device__ __forceinline__ f32x4_t paged_with_odd(f32x4_t o, f32x4_t odd) {
 #pragma unroll
@@ -400,5 +426,8 @@ __device__ __forceinline__ float paged_log2_sum(float reference, float sum) {
 // 16-bit storage: workgroups for requests of many rows (a, unless `chunks` is 0) and for those of few (d, unless `decodes` is 0).
 hipError_t launch_paged_16(const PagedArgs& a, int64_t chunks, const PagedArgs& d, int64_t decodes, int D, int dtype, hipStream_t stream);
 hipError_t launch_paged_f32(const PagedArgs& a, int64_t grid, int D, hipStream_t stream);
+// The same for rows with masks of their own.
+hipError_t launch_tree_16(const PagedArgs& a, int64_t chunks, const PagedArgs& d, int64_t decodes, int D, int dtype, hipStream_t stream);
+hipError_t launch_tree_f32(const PagedArgs& a, int64_t grid, int D, hipStream_t stream);
 
 }  // namespace fedrag

@@ -224,7 +224,9 @@ static PagedPlan paged_plan(int B, int Hq, int Hkv, int dtype, int64_t T, int64_
     return p;
 }
 
-bool paged_attn_fits(int B, int Hq, int Hkv, int D, int dtype, int64_t T, int64_t max_pages, int page_tokens, int64_t max_q_len, size_t* bytes) {
+bool paged_attn_fits(int B, int Hq, int Hkv, int D, int dtype, int64_t T, int64_t max_pages, int page_tokens, int64_t max_q_len, bool tree,
+                     size_t* bytes) {
+    (void)tree;
     *bytes = 0;
     if (T == 0 || B == 0) return true;
     const int64_t rows = T * (Hq / Hkv);
@@ -256,6 +258,8 @@ hipError_t launch_paged_attn(const PagedAttnProblem& p, hipStream_t stream) {
     a.scale = p.scale;
     a.O = p.O;
     a.lse = p.lse;
+    a.tree = p.tree;
+    a.tree_words = p.tree_words;
     const PagedPlan plan = paged_plan(p.B, p.Hq, p.Hkv, p.dtype, p.T, p.max_pages << p.pages.shift, p.max_q_len);
     auto with = [&](const PagedLaunch& l, char* scratch) {
         PagedArgs x = a;
@@ -267,8 +271,9 @@ hipError_t launch_paged_attn(const PagedAttnProblem& p, hipStream_t stream) {
     };
     const PagedArgs runs = with(plan.runs, (char*)p.workspace), shares = with(plan.shares, (char*)p.workspace + plan.runs.bytes(p.D));
     const int64_t wgs_r = plan.runs.merges * plan.runs.merge_groups(p.D), wgs_s = plan.shares.merges * plan.shares.merge_groups(p.D);
-    const hipError_t e = p.dtype == FEDRAG_F32 ? launch_paged_f32(runs, plan.runs.grid, p.D, stream)
-                                               : launch_paged_16(runs, plan.runs.grid, shares, plan.shares.grid, p.D, p.dtype, stream);
+    hipError_t e;
+    if (p.dtype == FEDRAG_F32) e = (p.tree ? launch_tree_f32 : launch_paged_f32)(runs, plan.runs.grid, p.D, stream);
+    else e = (p.tree ? launch_tree_16 : launch_paged_16)(runs, plan.runs.grid, shares, plan.shares.grid, p.D, p.dtype, stream);
     if (e != hipSuccess || wgs_r + wgs_s == 0) return e;
 #define FEDRAG_MERGE(KIND) (p.D == 128 ? paged_merge_kernel<128, KIND> : paged_merge_kernel<64, KIND>)
     const auto merge = wgs_r == 0 ? FEDRAG_MERGE(1) : wgs_s == 0 ? FEDRAG_MERGE(2) : FEDRAG_MERGE(3);

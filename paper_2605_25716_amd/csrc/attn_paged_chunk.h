@@ -27,8 +27,8 @@ namespace fedrag {
 
 // ks0 .. vs1: an array each per tile slot, so that the compiler sees that the loads filling one do not alias the reads of another.
 // AHEAD: V operands are read from LDS so many before they are used; K operands four.  (Three of V take the registers that are left
-// at 128 columns; the other form beside it takes two more for its scalars.)
-template <class T, int D, int NW, int ARGS, int AHEAD>
+// at 128 columns; the other form beside it takes two more for its scalars.)  TREE: rows have masks of their own.
+template <class T, int D, int NW, int ARGS, int AHEAD, bool TREE = false>
 __device__ __forceinline__ void paged_chunk_body(const PagedArgs& a, uint32_t index, char* ks0, char* ks1, char* vs0, char* vs1, int* flags) {
     typedef typename T::elem elem;
     typedef typename T::vec8 vec8;
@@ -51,7 +51,9 @@ __device__ __forceinline__ void paged_chunk_body(const PagedArgs& a, uint32_t in
     const PagedRequest& rq = p.req;
     const int row0 = p.tile * (NW * kPreQ);
     const int last = (row0 + NW * kPreQ < rq.R ? row0 + NW * kPreQ : rq.R) - 1;
-    const int lim_min = paged_limit(a, rq, row0), lim_max = paged_limit(a, rq, last);
+    const int base = TREE ? paged_base(rq, (int)a.by_g.div((uint32_t)rq.R)) : 0;
+    const int lim_min = TREE ? (base < 0 ? 0 : (base < rq.keys ? base : rq.keys)) : paged_limit(a, rq, row0);
+    const int lim_max = TREE ? rq.keys : paged_limit(a, rq, last);
     const int k_begin = (int)((int64_t)p.run * p.per << a.cut.unit_shift);
     const int64_t run_end = (int64_t)k_begin + ((int64_t)p.per << a.cut.unit_shift);
     const int L = (run_end < lim_max ? (int)run_end : lim_max) - k_begin;  // keys to visit
@@ -72,7 +74,7 @@ __device__ __forceinline__ void paged_chunk_body(const PagedArgs& a, uint32_t in
     const int n_tiles = (L + kPreK - 1) / kPreK;
     const int whole = lim_min - k_begin < L ? lim_min - k_begin : L;  // keys that every row sees
     int t_mask0 = whole > 0 ? whole / kPreK : 0;                      // first tile that some row does not see whole
-    const int own = paged_limit(a, rq, row) - k_begin;
+    const int own = (TREE ? rq.keys : paged_limit(a, rq, row)) - k_begin;
     const int key_lim = own < L ? own : L;                            // this lane's row sees keys < key_lim
 
     vec8 qop[KS];  // Q^T operands: column li, channels 16 i + 8 lh
@@ -200,6 +202,14 @@ __device__ __forceinline__ void paged_chunk_body(const PagedArgs& a, uint32_t in
         return __builtin_bit_cast(vec8, w);
     };
 
+    auto tree_bits = [&](int tile) {  // keys of the tile that this lane's row sees by its mask
+        const PagedArgsLate& z = late_args<ARGS>();
+        int l = threadIdx.x % 32;  // anew: nothing of this is kept in registers through the loops
+        pin_here(l);
+        const int row = row_w + l < rq.R ? row_w + l : rq.R - 1;
+        return paged_tree_bits(z, rq, base, (int)FastDiv::div_by(z.by_g.m, z.by_g.s, (uint32_t)row), k_begin + tile * kPreK);
+    };
+
     // par: t & 1 as a constant, so that the double sets are addressed statically.  kFirst: A and B1 of a tile (masked if need be);
     // kLast: B2 and C of the one before; kSteady: all, on tiles that every row sees whole.
     enum { kFirst, kSteady, kLast };
@@ -257,6 +267,15 @@ __device__ __forceinline__ void paged_chunk_body(const PagedArgs& a, uint32_t in
                     const int key = key0 + 8 * (r / 4) + (r % 4);
                     if (key >= key_lim) S0[r] = -INFINITY;
                     if (key + 32 >= key_lim) S1[c][r] = -INFINITY;
+                }
+                if constexpr (TREE) {
+                    const uint64_t seen = tree_bits(tile);
+                    const uint32_t s0 = (uint32_t)seen >> (4 * lh), s1 = (uint32_t)(seen >> 32) >> (4 * lh);
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        if (!(s0 >> (8 * (r / 4) + r % 4) & 1)) S0[r] = -INFINITY;
+                        if (!(s1 >> (8 * (r / 4) + r % 4) & 1)) S1[c][r] = -INFINITY;
+                    }
                 }
                 if (t_mask0 < 0) {  // pages are missing: 16 keys lie in one
                     bool gone[4];
@@ -388,7 +407,10 @@ __device__ __forceinline__ void paged_chunk_body(const PagedArgs& a, uint32_t in
 #pragma unroll
         for (int i = 0; i < MT; ++i) acc_o[i] *= alph[0];
         alph[0] = 1.0f;
-        for (int k = 0; k < kPreK && tile * kPreK + k < key_lim; ++k)
+        uint64_t seen = ~(uint64_t)0;
+        if constexpr (TREE) seen = tree_bits(tile);
+        for (int k = 0; k < kPreK && tile * kPreK + k < key_lim; ++k) {
+            if (TREE && !(seen >> k & 1)) continue;
 #pragma unroll
             for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -401,6 +423,7 @@ __device__ __forceinline__ void paged_chunk_body(const PagedArgs& a, uint32_t in
                     }
                     __builtin_amdgcn_sched_barrier(0);  // (more of these reads in flight would take registers from the loops)
                 }
+        }
         __syncthreads();
 #pragma unroll 1
         for (int j = 0; j < SLOT / 16 / kThreads; ++j) {
@@ -501,8 +524,14 @@ __device__ __forceinline__ void paged_chunk_body(const PagedArgs& a, uint32_t in
             const int64_t to = ((int64_t)__shfl((int)(at >> 32), r) << 32) | (uint32_t)__shfl((int)at, r);
             const float sum = __shfl(l_tot, r);
             if (row_w + r >= rq.R || all_finite(o) || !__builtin_isfinite(sum)) continue;
-            const int own = paged_limit(z, rq, row_w + r), end = own < k_begin + L ? own : k_begin + L;
-            const f32x4_t more = paged_odd_values<elem, D>(z, p.b, p.head, shared > k_begin ? shared : k_begin, end, chunk * 4);
+            const int own = TREE ? rq.keys : paged_limit(z, rq, row_w + r), end = own < k_begin + L ? own : k_begin + L;
+            const int from = shared > k_begin ? shared : k_begin;
+            f32x4_t more;
+            if constexpr (TREE)
+                more = paged_odd_tree_values<elem, D>(z, rq, base, (int)FastDiv::div_by(z.by_g.m, z.by_g.s, (uint32_t)(row_w + r)), p.b, p.head, from, end,
+                                                      chunk * 4);
+            else
+                more = paged_odd_values<elem, D>(z, p.b, p.head, from, end, chunk * 4);
             *(f32x4_t*)(O + to * D + chunk * 4) = paged_with_odd(o, all + more);
         }
     };

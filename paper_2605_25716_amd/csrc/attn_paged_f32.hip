@@ -18,8 +18,9 @@ namespace fedrag {
 
 __device__ __forceinline__ f32x4_t paged_mfma_f32(float a, float b, f32x4_t c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
 
-template <int D, int NQ>
-FEDRAG_KERNEL __launch_bounds__(256, 2) void paged_f32_kernel(const PagedArgs a) {
+// TREE: rows have masks of their own.
+template <int D, int NQ, bool TREE>
+__device__ __forceinline__ void paged_f32_body(const PagedArgs& a) {
     constexpr int W = 4;
     constexpr int kKeys = 16;    // keys per wave step
     constexpr int DCH = D / 16;  // channels per lane and key of V (= 16-row tiles of O^T)
@@ -38,7 +39,9 @@ FEDRAG_KERNEL __launch_bounds__(256, 2) void paged_f32_kernel(const PagedArgs a)
     const PagedRequest& rq = p.req;
     const int row0 = p.tile * (NQ * 16);
     const int last = (row0 + NQ * 16 < rq.R ? row0 + NQ * 16 : rq.R) - 1;
-    const int lim_min = paged_limit(a, rq, row0), lim_max = paged_limit(a, rq, last);
+    const int base = TREE ? paged_base(rq, (int)a.by_g.div((uint32_t)rq.R)) : 0;
+    const int lim_min = TREE ? (base < 0 ? 0 : (base < rq.keys ? base : rq.keys)) : paged_limit(a, rq, row0);
+    const int lim_max = TREE ? rq.keys : paged_limit(a, rq, last);
     const int k_begin = (int)((int64_t)p.run * p.per << a.cut.unit_shift);
     const int64_t run_end = (int64_t)k_begin + ((int64_t)p.per << a.cut.unit_shift);
     const int k_end = run_end < lim_max ? (int)run_end : lim_max;
@@ -55,7 +58,7 @@ FEDRAG_KERNEL __launch_bounds__(256, 2) void paged_f32_kernel(const PagedArgs a)
         const char* Q = a.Q + ((int64_t)p.head * a.G + g) * a.q_head_stride + ((int64_t)rq.begin + t) * a.q_token_stride + 16 * lq;
 #pragma unroll
         for (int j = 0; j < KJ; ++j) q[n][j] = *(const f32x4_t*)(Q + 64 * j);
-        const int own = paged_limit(a, rq, row);
+        const int own = TREE ? rq.keys : paged_limit(a, rq, row);
         lim[n] = own < k_end ? own : k_end;
         m_run[n] = -__FLT_MAX__;  // not -inf: a row may see nothing of a tile, and -inf - m has to be -inf then
         l_run[n] = 0.f;
@@ -115,6 +118,16 @@ FEDRAG_KERNEL __launch_bounds__(256, 2) void paged_f32_kernel(const PagedArgs a)
             load_k(i + 1, k);
         }
         const bool whole = id >= 0 && key0 + kKeys <= lim_min && key0 + kKeys <= k_end;  // wave-uniform
+        uint32_t seen[NQ];  // of the tile's keys, by the rows' masks
+        if constexpr (TREE)
+            if (!whole) {
+                const PagedArgsLate& z = late_args<0>();
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) {
+                    const int row = row0 + n * 16 + lr < rq.R ? row0 + n * 16 + lr : rq.R - 1;
+                    seen[n] = (uint32_t)paged_tree_bits(z, rq, base, (int)FastDiv::div_by(z.by_g.m, z.by_g.s, (uint32_t)row), key0);
+                }
+            }
         if (!whole && lim_min != lim_max) {
             // Some rows see a token that others do not.  Where its V is not finite, a product with the probability 0 would bring it to
             // them: such values are taken out, and added by themselves for the rows that see them.
@@ -138,7 +151,7 @@ FEDRAG_KERNEL __launch_bounds__(256, 2) void paged_f32_kernel(const PagedArgs a)
                                 float, __builtin_amdgcn_raw_buffer_load_b32(rv, key * ROWB + (DCH * (4 * lq + r) + t) * 4, 0, 0));
 #pragma unroll
                             for (int n = 0; n < NQ; ++n)
-                                if (!__builtin_isfinite(x) && key0 + key < lim[n]) acc[n][t][r] += x;
+                                if (!__builtin_isfinite(x) && key0 + key < lim[n] && (!TREE || (seen[n] >> key & 1))) acc[n][t][r] += x;
                         }
                         __builtin_amdgcn_sched_barrier(0);  // (more of these loads in flight would take registers from the loop)
                     }
@@ -150,7 +163,7 @@ FEDRAG_KERNEL __launch_bounds__(256, 2) void paged_f32_kernel(const PagedArgs a)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 s[n][r] *= a.scale;
-                if (!whole && (id < 0 || key0 + 4 * lq + r >= lim[n])) s[n][r] = -INFINITY;
+                if (!whole && (id < 0 || key0 + 4 * lq + r >= lim[n] || (TREE && !(seen[n] >> (4 * lq + r) & 1)))) s[n][r] = -INFINITY;
                 mx = fmaxf(mx, s[n][r]);
             }
             mx = xor32_max(xor16_max(mx));
@@ -213,7 +226,11 @@ FEDRAG_KERNEL __launch_bounds__(256, 2) void paged_f32_kernel(const PagedArgs a)
 #pragma unroll
         for (int e = 0; e < 4; ++e) num[e] = any ? num[e] * inv : 0.f;
         if (!all_finite(num) && __builtin_isfinite(den)) {
-            num = paged_with_odd(num, paged_odd_values<float, D>(late_args<0>(), p.b, p.head, k_begin, sm_lim[n], c));
+            if constexpr (TREE)
+                num = paged_with_odd(num, paged_odd_tree_values<float, D>(late_args<0>(), rq, base, (int)a.by_g.div((uint32_t)(row0 + n)), p.b, p.head, k_begin,
+                                                                          sm_lim[n], c));
+            else
+                num = paged_with_odd(num, paged_odd_values<float, D>(late_args<0>(), p.b, p.head, k_begin, sm_lim[n], c));
         }
         const uint32_t t = a.by_g.div((uint32_t)(row0 + n)), g = (uint32_t)(row0 + n) - t * a.by_g.d;
         const int64_t at = p.runs > 1 ? ((int64_t)p.slot << a.cut.tile_shift) + n : ((int64_t)p.head * a.G + g) * a.T + rq.begin + t;
@@ -222,10 +239,26 @@ FEDRAG_KERNEL __launch_bounds__(256, 2) void paged_f32_kernel(const PagedArgs a)
     }
 }
 
+template <int D, int NQ>
+FEDRAG_KERNEL __launch_bounds__(256, 2) void paged_f32_kernel(const PagedArgs a) {
+    paged_f32_body<D, NQ, false>(a);
+}
+template <int D, int NQ>
+FEDRAG_KERNEL __launch_bounds__(256, 2) void tree_f32_kernel(const PagedArgs a) {
+    paged_f32_body<D, NQ, true>(a);
+}
+
 hipError_t launch_paged_f32(const PagedArgs& a, int64_t grid, int D, hipStream_t stream) {
     const bool wide = a.cut.tile_shift == 5;
     const auto kernel = D == 128 ? (wide ? paged_f32_kernel<128, 2> : paged_f32_kernel<128, 1>)
                                  : (wide ? paged_f32_kernel<64, 2> : paged_f32_kernel<64, 1>);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(256), 0, stream, a);
+    return hipGetLastError();
+}
+hipError_t launch_tree_f32(const PagedArgs& a, int64_t grid, int D, hipStream_t stream) {
+    const bool wide = a.cut.tile_shift == 5;
+    const auto kernel = D == 128 ? (wide ? tree_f32_kernel<128, 2> : tree_f32_kernel<128, 1>)
+                                 : (wide ? tree_f32_kernel<64, 2> : tree_f32_kernel<64, 1>);
     hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(256), 0, stream, a);
     return hipGetLastError();
 }

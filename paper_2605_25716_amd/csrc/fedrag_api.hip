@@ -113,16 +113,117 @@ fedrag_status check_cache(const fedrag_paged_cache* c, const fedrag_shape* s, Pa
 
 // K's pages and V's share bytes.  (They may take turns in one tensor: then their distance, modulo a page's stride, leaves
 // room for a page on either side.)
-bool pages_overlap(const Pages& p, size_t extent, size_t block) {
-    if (!overlaps(p.K, extent, p.V, extent)) return false;
-    const uintptr_t k = reinterpret_cast<uintptr_t>(p.K), v = reinterpret_cast<uintptr_t>(p.V);
-    const size_t d = (size_t)((k < v ? v - k : k - v) % (uintptr_t)p.page_bytes);
-    return d < block || (size_t)p.page_bytes - d < block;
+bool pages_meet(const char* a, size_t extent_a, const char* b, size_t extent_b, int64_t stride, size_t block) {
+    if (!overlaps(a, extent_a, b, extent_b)) return false;
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    const size_t d = (size_t)((x < y ? y - x : x - y) % (uintptr_t)stride);
+    return d < block || (size_t)stride - d < block;
 }
+bool pages_overlap(const Pages& p, size_t extent, size_t block) { return pages_meet(p.K, extent, p.V, extent, p.page_bytes, block); }
 
 fedrag_status check_paged_sizes(int32_t batch, int64_t n_rows, int64_t max_pages, int64_t max_q_len) {
     return batch > kMostRequests || n_rows < 0 || n_rows > INT32_MAX || max_pages < 0 || max_pages > INT32_MAX || max_q_len < 0 ? FEDRAG_ERR_SHAPE
                                                                                                         : FEDRAG_OK;
+}
+
+// What a call reads and what it writes: whether something that it writes overlaps anything else.
+struct Range {
+    const void* p;
+    size_t n;
+};
+template <size_t I, size_t O>
+bool any_overlap(const Range (&in)[I], const Range (&out)[O]) {
+    for (const Range& o : out) {
+        for (const Range& i : in)
+            if (overlaps(o.p, o.n, i.p, i.n)) return true;
+        for (const Range& other : out)
+            if (&other != &o && overlaps(o.p, o.n, other.p, other.n)) return true;
+    }
+    return false;
+}
+
+bool verify_sizes_ok(int32_t batch, int64_t vocab) {
+    return batch >= 0 && batch <= 65535 && vocab >= 1 && vocab <= (1 << 20);  // (a launch holds all of these: below 2^24 workgroups)
+}
+
+bool tree_sizes_ok(int64_t n_rows, int32_t mask_words) {
+    return n_rows <= INT32_MAX - 255 && mask_words >= 1 && mask_words <= FEDRAG_TREE_WORDS;
+}
+
+size_t paged_attn_workspace(const fedrag_shape* shape, int64_t n_rows, int64_t max_pages, int32_t page_tokens, int64_t max_q_len, bool tree) {
+    if (check_shape(shape, true) != FEDRAG_OK || check_paged_sizes(shape->batch, n_rows, max_pages, max_q_len) != FEDRAG_OK ||
+        !page_tokens_ok(page_tokens) || max_pages * page_tokens > kMostTokens)
+        return 0;
+    size_t need;
+    paged_attn_fits(shape->batch, shape->n_q_heads, shape->n_kv_heads, shape->d_head, shape->dtype, n_rows, max_pages, page_tokens,
+                    max_q_len, tree, &need);
+    return need;
+}
+
+// tree: each row has a mask, of mask_words words (fedrag_paged_tree_attn); else the one that `causal` says.
+fedrag_status paged_attn(const fedrag_shape* shape, int64_t n_rows, const fedrag_rows* Q, const fedrag_paged_cache* cache,
+                         const int32_t* block_table, int64_t max_pages, const int32_t* q_start, const int32_t* kv_lens,
+                         bool tree, const uint64_t* tree_mask, int32_t mask_words, int64_t max_q_len, int32_t causal,
+                         float softmax_scale, float* O, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+    fedrag_status st = check_shape(shape, true);
+    if (st == FEDRAG_OK) st = check_paged_sizes(shape->batch, n_rows, max_pages, max_q_len);
+    if (st != FEDRAG_OK) return st;
+    PagedAttnProblem p{};
+    size_t extent, block, qb;
+    st = check_cache(cache, shape, &p.pages, &extent, &block);
+    if (st != FEDRAG_OK) return st;
+    if (max_pages * cache->page_tokens > kMostTokens) return FEDRAG_ERR_SHAPE;
+    if (tree && !tree_sizes_ok(n_rows, mask_words)) return FEDRAG_ERR_SHAPE;
+    if (n_rows == 0 || shape->batch == 0) return FEDRAG_OK;  // no rows: nothing to do, tensor pointers may be NULL
+    if (!(softmax_scale > 0.0f) || softmax_scale - softmax_scale != 0.0f) return FEDRAG_ERR_SHAPE;  // finite, > 0
+    st = check_rows(Q, n_rows, shape->n_q_heads, shape, &qb);
+    if (st != FEDRAG_OK) return st;
+    if (!O || !lse || !q_start || !kv_lens || (max_pages > 0 && !block_table) || (tree && !tree_mask)) return FEDRAG_ERR_NULL;
+    int64_t n, rows, table;
+    if (!tensor_elems(1, shape->n_q_heads, n_rows, shape->d_head, &n) || !mul_fits(shape->n_q_heads, n_rows, &rows) ||
+        !mul_fits((int64_t)shape->batch * 4, max_pages, &table))
+        return FEDRAG_ERR_SHAPE;
+    const uintptr_t words = reinterpret_cast<uintptr_t>(block_table) | reinterpret_cast<uintptr_t>(q_start) |
+                            reinterpret_cast<uintptr_t>(kv_lens) | reinterpret_cast<uintptr_t>(lse);
+    if (!aligned16(O) || (words & 3u) || (reinterpret_cast<uintptr_t>(tree_mask) & 7u) || !aligned16(workspace)) return FEDRAG_ERR_ALIAS;
+    size_t need;
+    if (!paged_attn_fits(shape->batch, shape->n_q_heads, shape->n_kv_heads, shape->d_head, shape->dtype, n_rows, max_pages,
+                         cache->page_tokens, max_q_len, tree, &need))
+        return FEDRAG_ERR_SHAPE;
+    if (need > 0 && (!workspace || workspace_bytes < need)) return FEDRAG_ERR_WORKSPACE;
+    const struct { const void* p; size_t n; } in[] = {{Q->data, qb}, {p.pages.K, extent}, {p.pages.V, extent}, {block_table, (size_t)table},
+                                                      {q_start, ((size_t)shape->batch + 1) * 4}, {kv_lens, (size_t)shape->batch * 4},
+                                                      {tree_mask, (size_t)n_rows * (size_t)mask_words * 8}},
+        out[] = {{O, (size_t)n * 4}, {lse, (size_t)rows * 4}, {workspace, need}};
+    for (const auto& o : out) {
+        for (const auto& i : in)
+            if (overlaps(o.p, o.n, i.p, i.n)) return FEDRAG_ERR_ALIAS;
+        for (const auto& other : out)
+            if (&other != &o && overlaps(o.p, o.n, other.p, other.n)) return FEDRAG_ERR_ALIAS;
+    }
+    const int64_t e = (int64_t)elem_size(shape->dtype);
+    p.B = shape->batch;
+    p.Hq = shape->n_q_heads;
+    p.Hkv = shape->n_kv_heads;
+    p.D = shape->d_head;
+    p.dtype = shape->dtype;
+    p.T = n_rows;
+    p.Q = (const char*)Q->data;
+    p.q_head_stride = Q->head_stride * e;
+    p.q_token_stride = Q->token_stride * e;
+    p.table = block_table;
+    p.max_pages = max_pages;
+    p.q_start = q_start;
+    p.kv_lens = kv_lens;
+    p.max_q_len = max_q_len;
+    p.causal = causal != 0;
+    p.tree = tree_mask;
+    p.tree_words = mask_words;
+    p.scale = softmax_scale;
+    p.O = O;
+    p.lse = lse;
+    p.workspace = workspace;
+    return dev(launch_paged_attn(p, (hipStream_t)stream));
 }
 
 }  // namespace
@@ -846,74 +947,173 @@ fedrag_status fedrag_paged_write(const fedrag_shape* shape, int64_t n_rows, cons
 
 size_t fedrag_paged_attn_workspace_bytes(const fedrag_shape* shape, int64_t n_rows, int64_t max_pages, int32_t page_tokens,
                                          int64_t max_q_len) {
-    if (check_shape(shape, true) != FEDRAG_OK || check_paged_sizes(shape->batch, n_rows, max_pages, max_q_len) != FEDRAG_OK ||
-        !page_tokens_ok(page_tokens) || max_pages * page_tokens > kMostTokens)
-        return 0;
-    size_t need;
-    paged_attn_fits(shape->batch, shape->n_q_heads, shape->n_kv_heads, shape->d_head, shape->dtype, n_rows, max_pages, page_tokens,
-                    max_q_len, &need);
-    return need;
+    return paged_attn_workspace(shape, n_rows, max_pages, page_tokens, max_q_len, false);
 }
 
 fedrag_status fedrag_paged_attn(const fedrag_shape* shape, int64_t n_rows, const fedrag_rows* Q, const fedrag_paged_cache* cache,
                                 const int32_t* block_table, int64_t max_pages, const int32_t* q_start, const int32_t* kv_lens,
                                 int64_t max_q_len, int32_t causal, float softmax_scale, float* O, float* lse, void* workspace,
                                 size_t workspace_bytes, void* stream) {
+    return paged_attn(shape, n_rows, Q, cache, block_table, max_pages, q_start, kv_lens, false, nullptr, 0, max_q_len, causal,
+                      softmax_scale, O, lse, workspace, workspace_bytes, stream);
+}
+
+size_t fedrag_paged_tree_attn_workspace_bytes(const fedrag_shape* shape, int64_t n_rows, int64_t max_pages, int32_t page_tokens,
+                                              int64_t max_q_len) {
+    if (!tree_sizes_ok(n_rows, 1)) return 0;
+    return paged_attn_workspace(shape, n_rows, max_pages, page_tokens, max_q_len, true);
+}
+
+fedrag_status fedrag_paged_tree_attn(const fedrag_shape* shape, int64_t n_rows, const fedrag_rows* Q, const fedrag_paged_cache* cache,
+                                     const int32_t* block_table, int64_t max_pages, const int32_t* q_start, const int32_t* kv_lens,
+                                     const uint64_t* tree_mask, int32_t mask_words, int64_t max_q_len, float softmax_scale, float* O,
+                                     float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+    return paged_attn(shape, n_rows, Q, cache, block_table, max_pages, q_start, kv_lens, true, tree_mask, mask_words, max_q_len, 0,
+                      softmax_scale, O, lse, workspace, workspace_bytes, stream);
+}
+
+fedrag_status fedrag_tree_map(int32_t batch, int64_t n_rows, int32_t mask_words, const int32_t* q_start, const int32_t* kv_lens,
+                              const int32_t* parents, uint64_t* tree_mask, int32_t* positions, int32_t* flags, void* stream) {
+    if (batch < 0 || check_paged_sizes(batch, n_rows, 0, 0) != FEDRAG_OK || !tree_sizes_ok(n_rows, mask_words)) return FEDRAG_ERR_SHAPE;
+    if (batch == 0 && n_rows == 0) return FEDRAG_OK;
+    if ((batch > 0 && (!q_start || !kv_lens || !flags)) || (n_rows > 0 && (!parents || !tree_mask))) return FEDRAG_ERR_NULL;
+    if (!tree_map_fits(batch, n_rows)) return FEDRAG_ERR_SHAPE;
+    const uintptr_t words = reinterpret_cast<uintptr_t>(q_start) | reinterpret_cast<uintptr_t>(kv_lens) | reinterpret_cast<uintptr_t>(parents) |
+                            reinterpret_cast<uintptr_t>(positions) | reinterpret_cast<uintptr_t>(flags);
+    if ((words & 3u) || (reinterpret_cast<uintptr_t>(tree_mask) & 7u)) return FEDRAG_ERR_ALIAS;
+    const size_t nb = (size_t)batch * 4, nr = (size_t)n_rows * 4;
+    const Range in[] = {{q_start, batch > 0 ? nb + 4 : 0}, {kv_lens, nb}, {parents, nr}},
+                out[] = {{tree_mask, (size_t)n_rows * (size_t)mask_words * 8}, {positions, nr}, {flags, nb}};
+    if (any_overlap(in, out)) return FEDRAG_ERR_ALIAS;
+    return dev(launch_tree_map(batch, n_rows, mask_words, q_start, kv_lens, parents, tree_mask, positions, flags, (hipStream_t)stream));
+}
+
+size_t fedrag_tree_verify_workspace_bytes(int32_t batch, int64_t vocab) {
+    return verify_sizes_ok(batch, vocab) ? tree_verify_workspace(batch, (int)vocab) : 0;
+}
+
+fedrag_status fedrag_tree_verify(int32_t batch, int64_t n_rows, int64_t vocab, int32_t dtype, const int32_t* q_start,
+                                 const int32_t* parents, const int32_t* tokens, const void* target, int64_t target_stride,
+                                 const void* draft, int64_t draft_stride, const double* u, const double* u_next, int64_t max_kept,
+                                 int32_t* kept, int32_t* n_kept, int32_t* next_token, void* workspace, size_t workspace_bytes,
+                                 void* stream) {
+    if (!verify_sizes_ok(batch, vocab) || !tree_sizes_ok(n_rows, 1) || n_rows < 0 || max_kept < 1 || max_kept > INT32_MAX)
+        return FEDRAG_ERR_SHAPE;
+    if (dtype != FEDRAG_F32 && dtype != FEDRAG_BF16 && dtype != FEDRAG_F16) return FEDRAG_ERR_UNSUPPORTED;
+    const int64_t e = (int64_t)elem_size(dtype);
+    if (target_stride < vocab || (draft && draft_stride < vocab)) return FEDRAG_ERR_SHAPE;
+    int64_t target_bytes = 0, draft_bytes = 0, kept_bytes;
+    auto extent = [&](int64_t stride, int64_t* bytes) {  // of rows with that stride
+        if (n_rows == 0) return true;
+        int64_t rows;
+        if (stride > kMostBytes / e || !mul_fits(n_rows - 1, stride * e, &rows) || rows > kMostBytes / 2) return false;
+        *bytes = rows + vocab * e;
+        return true;
+    };
+    if (!extent(target_stride, &target_bytes) || (draft && !extent(draft_stride, &draft_bytes)) ||
+        !mul_fits((int64_t)batch * 4, max_kept, &kept_bytes))
+        return FEDRAG_ERR_SHAPE;
+    if (batch == 0) return FEDRAG_OK;
+    if (!q_start || !u_next || !kept || !n_kept || !next_token || (n_rows > 0 && (!parents || !tokens || !target || !u))) return FEDRAG_ERR_NULL;
+    const uintptr_t words = reinterpret_cast<uintptr_t>(q_start) | reinterpret_cast<uintptr_t>(parents) | reinterpret_cast<uintptr_t>(tokens) |
+                            reinterpret_cast<uintptr_t>(kept) | reinterpret_cast<uintptr_t>(n_kept) | reinterpret_cast<uintptr_t>(next_token);
+    const uintptr_t values = reinterpret_cast<uintptr_t>(target) | reinterpret_cast<uintptr_t>(draft);
+    if ((words & 3u) || ((reinterpret_cast<uintptr_t>(u) | reinterpret_cast<uintptr_t>(u_next)) & 7u) || (values & (uintptr_t)(e - 1)) ||
+        !aligned16(workspace))
+        return FEDRAG_ERR_ALIAS;
+    const size_t need = tree_verify_workspace(batch, (int)vocab);
+    if (!workspace || workspace_bytes < need) return FEDRAG_ERR_WORKSPACE;
+    const size_t nb = (size_t)batch, nr = (size_t)n_rows;
+    const Range in[] = {{q_start, nb * 4 + 4}, {parents, nr * 4}, {tokens, nr * 4}, {target, (size_t)target_bytes}, {draft, (size_t)draft_bytes},
+                        {u, nr * 8}, {u_next, nb * 8}},
+                out[] = {{kept, (size_t)kept_bytes}, {n_kept, nb * 4}, {next_token, nb * 4}, {workspace, need}};
+    if (any_overlap(in, out)) return FEDRAG_ERR_ALIAS;
+    return dev(launch_tree_verify(TreeVerifyJob{batch, (int)n_rows, (int)vocab, dtype, q_start, parents, tokens, target, draft, target_stride,
+                                                draft_stride, u, u_next, max_kept, kept, n_kept, next_token, workspace},
+                                  (hipStream_t)stream));
+}
+
+fedrag_status fedrag_paged_keep(const fedrag_shape* shape, int32_t n_caches, const fedrag_paged_cache* caches, const int32_t* block_table,
+                                int64_t max_pages, const int32_t* q_start, const int32_t* kv_lens, const int32_t* kept, int64_t max_kept,
+                                const int32_t* n_kept, void* stream) {
     fedrag_status st = check_shape(shape, true);
-    if (st == FEDRAG_OK) st = check_paged_sizes(shape->batch, n_rows, max_pages, max_q_len);
+    if (st == FEDRAG_OK) st = check_paged_sizes(shape->batch, 0, max_pages, 0);
     if (st != FEDRAG_OK) return st;
-    PagedAttnProblem p{};
-    size_t extent, block, qb;
-    st = check_cache(cache, shape, &p.pages, &extent, &block);
-    if (st != FEDRAG_OK) return st;
-    if (max_pages * cache->page_tokens > kMostTokens) return FEDRAG_ERR_SHAPE;
-    if (n_rows == 0 || shape->batch == 0) return FEDRAG_OK;  // no rows: nothing to do, tensor pointers may be NULL
-    if (!(softmax_scale > 0.0f) || softmax_scale - softmax_scale != 0.0f) return FEDRAG_ERR_SHAPE;  // finite, > 0
-    st = check_rows(Q, n_rows, shape->n_q_heads, shape, &qb);
-    if (st != FEDRAG_OK) return st;
-    if (!O || !lse || !q_start || !kv_lens || (max_pages > 0 && !block_table)) return FEDRAG_ERR_NULL;
-    int64_t n, rows, table;
-    if (!tensor_elems(1, shape->n_q_heads, n_rows, shape->d_head, &n) || !mul_fits(shape->n_q_heads, n_rows, &rows) ||
-        !mul_fits((int64_t)shape->batch * 4, max_pages, &table))
-        return FEDRAG_ERR_SHAPE;
-    const uintptr_t words = reinterpret_cast<uintptr_t>(block_table) | reinterpret_cast<uintptr_t>(q_start) |
-                            reinterpret_cast<uintptr_t>(kv_lens) | reinterpret_cast<uintptr_t>(lse);
-    if (!aligned16(O) || (words & 3u) || !aligned16(workspace)) return FEDRAG_ERR_ALIAS;
-    size_t need;
-    if (!paged_attn_fits(shape->batch, shape->n_q_heads, shape->n_kv_heads, shape->d_head, shape->dtype, n_rows, max_pages,
-                         cache->page_tokens, max_q_len, &need))
-        return FEDRAG_ERR_SHAPE;
-    if (need > 0 && (!workspace || workspace_bytes < need)) return FEDRAG_ERR_WORKSPACE;
-    const struct { const void* p; size_t n; } in[] = {{Q->data, qb}, {p.pages.K, extent}, {p.pages.V, extent}, {block_table, (size_t)table},
-                                                      {q_start, ((size_t)shape->batch + 1) * 4}, {kv_lens, (size_t)shape->batch * 4}},
-        out[] = {{O, (size_t)n * 4}, {lse, (size_t)rows * 4}, {workspace, need}};
-    for (const auto& o : out) {
-        for (const auto& i : in)
-            if (overlaps(o.p, o.n, i.p, i.n)) return FEDRAG_ERR_ALIAS;
-        for (const auto& other : out)
-            if (&other != &o && overlaps(o.p, o.n, other.p, other.n)) return FEDRAG_ERR_ALIAS;
+    if (n_caches < 1 || n_caches > FEDRAG_KEEP_CACHES || max_kept < 0 || max_kept > INT32_MAX) return FEDRAG_ERR_SHAPE;
+    if (!caches) return FEDRAG_ERR_NULL;
+    PagedKeep j{};
+    size_t extent[FEDRAG_KEEP_CACHES], block[FEDRAG_KEEP_CACHES];
+    for (int i = 0; i < n_caches; ++i) {
+        st = check_cache(&caches[i], shape, &j.pages[i], &extent[i], &block[i]);
+        if (st != FEDRAG_OK) return st;
+        if (caches[i].page_tokens != caches[0].page_tokens) return FEDRAG_ERR_SHAPE;
     }
-    const int64_t e = (int64_t)elem_size(shape->dtype);
-    p.B = shape->batch;
-    p.Hq = shape->n_q_heads;
-    p.Hkv = shape->n_kv_heads;
-    p.D = shape->d_head;
-    p.dtype = shape->dtype;
-    p.T = n_rows;
-    p.Q = (const char*)Q->data;
-    p.q_head_stride = Q->head_stride * e;
-    p.q_token_stride = Q->token_stride * e;
-    p.table = block_table;
-    p.max_pages = max_pages;
-    p.q_start = q_start;
-    p.kv_lens = kv_lens;
-    p.max_q_len = max_q_len;
-    p.causal = causal != 0;
-    p.scale = softmax_scale;
-    p.O = O;
-    p.lse = lse;
-    p.workspace = workspace;
-    return dev(launch_paged_attn(p, (hipStream_t)stream));
+    if (max_pages * caches[0].page_tokens > kMostTokens) return FEDRAG_ERR_SHAPE;
+    int64_t table, list;
+    if (!mul_fits((int64_t)shape->batch * 4, max_pages, &table) || !mul_fits((int64_t)shape->batch * 4, max_kept, &list) ||
+        (int64_t)shape->batch * shape->n_kv_heads >= (1 << 20) || (int64_t)shape->batch * shape->n_kv_heads * n_caches >= (1 << 20))
+        return FEDRAG_ERR_SHAPE;
+    if (shape->batch == 0 || max_kept == 0 || max_pages == 0) return FEDRAG_OK;  // nothing is kept, or nothing is there
+    if (!block_table || !q_start || !kv_lens || !kept || !n_kept) return FEDRAG_ERR_NULL;
+    const uintptr_t words = reinterpret_cast<uintptr_t>(block_table) | reinterpret_cast<uintptr_t>(q_start) | reinterpret_cast<uintptr_t>(kv_lens) |
+                            reinterpret_cast<uintptr_t>(kept) | reinterpret_cast<uintptr_t>(n_kept);
+    if (words & 3u) return FEDRAG_ERR_ALIAS;
+    const size_t nb = (size_t)shape->batch * 4;
+    const Range in[] = {{block_table, (size_t)table}, {q_start, nb + 4}, {kv_lens, nb}, {kept, (size_t)list}, {n_kept, nb}};
+    // K's and V's pages of all caches apart from each other, or in turns in one tensor
+    for (int i = 0; i < n_caches; ++i)
+        for (const char* pages : {j.pages[i].K, j.pages[i].V}) {
+            for (const auto& r : in)
+                if (overlaps(pages, extent[i], r.p, r.n)) return FEDRAG_ERR_ALIAS;
+        }
+    for (int i = 0; i < 2 * n_caches; ++i)
+        for (int k = 0; k < i; ++k) {
+            const Pages &x = j.pages[i / 2], &y = j.pages[k / 2];
+            const char *a = i % 2 ? x.V : x.K, *b = k % 2 ? y.V : y.K;
+            if (x.page_bytes == y.page_bytes ? pages_meet(a, extent[i / 2], b, extent[k / 2], x.page_bytes, block[0])
+                                             : overlaps(a, extent[i / 2], b, extent[k / 2]))
+                return FEDRAG_ERR_ALIAS;
+        }
+    j.B = shape->batch;
+    j.H = shape->n_kv_heads;
+    j.D = shape->d_head;
+    j.elem_bytes = (int)elem_size(shape->dtype);
+    j.n_caches = n_caches;
+    j.table = block_table;
+    j.q_start = q_start;
+    j.kv_lens = kv_lens;
+    j.kept = kept;
+    j.n_kept = n_kept;
+    j.max_pages = max_pages;
+    j.max_kept = max_kept;
+    return dev(launch_paged_keep(j, (hipStream_t)stream));
+}
+
+fedrag_status fedrag_paged_trim(int32_t batch, int32_t page_tokens, int64_t max_pages, const int32_t* kv_lens, const int32_t* q_start,
+                                const int32_t* n_kept, const int32_t* block_table, int32_t* free_pages, int64_t n_free,
+                                const int32_t* free_count, int32_t* lens_out, int32_t* free_left, int32_t* flags, void* stream) {
+    if (batch < 0 || n_free < 0 || n_free > INT32_MAX) return FEDRAG_ERR_SHAPE;
+    fedrag_status st = check_paged_sizes(batch, 0, max_pages, 0);
+    if (st != FEDRAG_OK) return st;
+    if (!page_tokens_ok(page_tokens)) return FEDRAG_ERR_UNSUPPORTED;
+    if (!free_count || !free_left || !flags || (batch > 0 && (!kv_lens || !n_kept || !lens_out)) || (n_free > 0 && !free_pages) ||
+        (batch > 0 && max_pages > 0 && !block_table))
+        return FEDRAG_ERR_NULL;
+    int64_t table;
+    if (!mul_fits((int64_t)batch * 4, max_pages, &table)) return FEDRAG_ERR_SHAPE;
+    const uintptr_t words = reinterpret_cast<uintptr_t>(kv_lens) | reinterpret_cast<uintptr_t>(q_start) | reinterpret_cast<uintptr_t>(n_kept) |
+                            reinterpret_cast<uintptr_t>(block_table) | reinterpret_cast<uintptr_t>(free_pages) |
+                            reinterpret_cast<uintptr_t>(free_count) | reinterpret_cast<uintptr_t>(lens_out) |
+                            reinterpret_cast<uintptr_t>(free_left) | reinterpret_cast<uintptr_t>(flags);
+    if (words & 3u) return FEDRAG_ERR_ALIAS;
+    const size_t nb = (size_t)batch * 4;
+    const Range in[] = {{lens_out == kv_lens ? nullptr : kv_lens, nb}, {q_start, nb + 4}, {n_kept, nb}, {block_table, (size_t)table},
+                        {free_left == free_count ? nullptr : free_count, 4}},
+                out[] = {{free_pages, (size_t)n_free * 4}, {lens_out, nb}, {free_left, 4}, {flags, 4}};
+    if (any_overlap(in, out)) return FEDRAG_ERR_ALIAS;
+    return dev(launch_paged_trim(PagedTrimJob{batch, max_pages, n_free, page_tokens, kv_lens, q_start, n_kept, block_table, free_count, free_pages,
+                                              lens_out, free_left, flags},
+                                 (hipStream_t)stream));
 }
 
 const char* fedrag_status_string(fedrag_status status) {

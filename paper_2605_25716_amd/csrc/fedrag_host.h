@@ -268,12 +268,52 @@ struct PagedAttnProblem {
     const int32_t *q_start, *kv_lens;
     int64_t max_q_len;       // 0: not known
     bool causal;
+    const uint64_t* tree;    // NULL, or a mask for each row, [T, tree_words]
+    int tree_words;
     float scale;
     float *O, *lse;
     void* workspace;
 };
 hipError_t launch_paged_attn(const PagedAttnProblem& p, hipStream_t stream);
 // Whether a problem of these sizes fits a launch, and the workspace it needs.
-bool paged_attn_fits(int B, int Hq, int Hkv, int D, int dtype, int64_t T, int64_t max_pages, int page_tokens, int64_t max_q_len, size_t* bytes);
+bool paged_attn_fits(int B, int Hq, int Hkv, int D, int dtype, int64_t T, int64_t max_pages, int page_tokens, int64_t max_q_len, bool tree, size_t* bytes);
+
+// A drafted step: its trees' masks (fedrag_tree_map).
+bool tree_map_fits(int batch, int64_t n_rows);
+hipError_t launch_tree_map(int batch, int64_t n_rows, int words, const int32_t* q_start, const int32_t* kv_lens, const int32_t* parents,
+                           uint64_t* mask, int32_t* positions, int32_t* flags, hipStream_t stream);
+
+// The walk over the drafts (fedrag_tree_verify); row strides in elements.
+struct TreeVerifyJob {
+    int batch, n_rows, vocab, dtype;
+    const int32_t *q_start, *parents, *tokens;
+    const void *target, *draft;
+    int64_t target_stride, draft_stride;
+    const double *u, *u_next;
+    int64_t max_kept;
+    int32_t *kept, *n_kept, *next_token;
+    void* workspace;
+};
+size_t tree_verify_workspace(int batch, int vocab);
+hipError_t launch_tree_verify(const TreeVerifyJob& job, hipStream_t stream);
+
+// Accepted rows to the front of a request's rows (fedrag_paged_keep).
+struct PagedKeep {
+    int B, H, D, elem_bytes, n_caches;
+    Pages pages[FEDRAG_KEEP_CACHES];
+    const int32_t *table, *q_start, *kv_lens, *kept, *n_kept;
+    int64_t max_pages, max_kept;
+};
+hipError_t launch_paged_keep(const PagedKeep& job, hipStream_t stream);
+
+// What is left of the requests, and pages back on the stack (fedrag_paged_trim).
+struct PagedTrimJob {
+    int batch;
+    int64_t max_pages, n_free;
+    int page_tokens;
+    const int32_t *kv_lens, *q_start, *n_kept, *block_table, *free_count;
+    int32_t *free_pages, *lens_out, *free_left, *flags;
+};
+hipError_t launch_paged_trim(const PagedTrimJob& job, hipStream_t stream);
 
 }  // namespace fedrag

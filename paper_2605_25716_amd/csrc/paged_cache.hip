@@ -240,4 +240,173 @@ hipError_t launch_paged_write(const PagedWriteJob& job, hipStream_t stream) {
     return hipGetLastError();
 }
 
+// ------------------------------------------------------------------------------------------------ keep
+// Rows of a request move towards its front, in place: row j comes from kept[j] >= j.  Rows are read some at a time and written after
+// all of these have arrived; what the writes cover are rows of the same ones or before (a row that is still to be read, kept[i] for a
+// later i, lies above kept[j] >= j), so that the next ones need not wait.  A workgroup has one head of K or of V of a request in one
+// cache; its threads move 16 bytes of a row each.
+struct PagedKeepJob {
+    const int32_t *table, *q_start, *kv_lens, *kept, *n_kept;
+    int64_t max_pages, max_kept;
+    int B, H, row_bytes, shift, n_caches;
+    FastDiv by_h;
+    struct {
+        char *K, *V;
+        int64_t page_bytes;
+        uint32_t n_pages;
+    } cache[FEDRAG_KEEP_CACHES];
+};
+
+template <int THREADS, int CH>  // CH: 16-byte chunks per row
+FEDRAG_KERNEL __launch_bounds__(THREADS) void paged_keep_kernel(const PagedKeepJob j) {
+    constexpr int kRows = THREADS / CH;  // rows that the workgroup's threads hold one chunk each of
+    constexpr int kSteps = 4;
+    const int b = (int)j.by_h.div(blockIdx.x), h = (int)(blockIdx.x - (uint32_t)b * j.by_h.d);
+    const auto& cache = j.cache[blockIdx.y];
+    char* const pages = blockIdx.z ? cache.V : cache.K;
+    const int kv = j.kv_lens[b] < 0 ? 0 : j.kv_lens[b];
+    const int64_t n = (int64_t)j.q_start[b + 1] - j.q_start[b], base = kv - n;
+    int64_t count = j.n_kept[b] < n ? j.n_kept[b] : n;
+    count = count < j.max_kept ? count : j.max_kept;
+    const int32_t* const kept = j.kept + b * j.max_kept;
+    const int32_t* const table = j.table + b * j.max_pages;
+    const int c = threadIdx.x % CH * 16;
+    auto place = [&](int64_t token) -> char* {  // of a token's row, or null
+        if (token < 0 || token >= kv || token >> j.shift >= j.max_pages) return nullptr;
+        const uint32_t id = (uint32_t)table[token >> j.shift];
+        return id < cache.n_pages ? pages + (int64_t)id * cache.page_bytes + (((int64_t)h << j.shift) + (token & ((1 << j.shift) - 1))) * (CH * 16) + c
+                                  : nullptr;
+    };
+    for (int64_t j0 = 0; j0 < count; j0 += kSteps * kRows) {
+        u32x4_t row[kSteps];
+        char* to[kSteps];
+#pragma unroll
+        for (int u = 0; u < kSteps; ++u) {
+            const int64_t i = j0 + u * kRows + threadIdx.x / CH;
+            to[u] = nullptr;
+            if (i < count) {
+                const int64_t k = kept[i];
+                if (k > i && k < n) {  // (a row that stays where it is has nothing to do)
+                    const char* from = place(base + k);
+                    if (from) {
+                        to[u] = place(base + i);
+                        row[u] = *(const u32x4_t*)from;
+                    }
+                }
+            }
+        }
+        __builtin_amdgcn_s_waitcnt(0x0f70);  // all of the rows are here
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < kSteps; ++u)
+            if (to[u]) *(u32x4_t*)to[u] = row[u];
+    }
+}
+
+hipError_t launch_paged_keep(const PagedKeep& k, hipStream_t stream) {
+    PagedKeepJob j{};
+    j.table = k.table;
+    j.q_start = k.q_start;
+    j.kv_lens = k.kv_lens;
+    j.kept = k.kept;
+    j.n_kept = k.n_kept;
+    j.max_pages = k.max_pages;
+    j.max_kept = k.max_kept;
+    j.B = k.B;
+    j.H = k.H;
+    j.row_bytes = k.D * k.elem_bytes;
+    j.shift = k.pages[0].shift;
+    j.n_caches = k.n_caches;
+    j.by_h = FastDiv(k.H);
+    for (int i = 0; i < k.n_caches; ++i) {
+        j.cache[i].K = (char*)k.pages[i].K;
+        j.cache[i].V = (char*)k.pages[i].V;
+        j.cache[i].page_bytes = k.pages[i].page_bytes;
+        j.cache[i].n_pages = k.pages[i].n_pages;
+    }
+    const int chunks = j.row_bytes / 16;
+    const bool few = k.max_kept <= 64;
+#define FEDRAG_KEEP(CH) (few ? paged_keep_kernel<64, CH> : paged_keep_kernel<1024, CH>)
+    const auto kernel = chunks == 8 ? FEDRAG_KEEP(8) : chunks == 16 ? FEDRAG_KEEP(16) : FEDRAG_KEEP(32);
+#undef FEDRAG_KEEP
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(k.B * k.H), (unsigned)k.n_caches, 2), dim3(few ? 64 : 1024), 0, stream, j);
+    return hipGetLastError();
+}
+
+// ------------------------------------------------------------------------------------------------ trim
+// One workgroup takes the requests 1024 at a time: prefix sums of the columns that each gives back, then these columns side by side, a
+// few in a row to a thread, which counts those that name a page; prefix sums of the counts are the places on the stack.
+constexpr int kTrimEach = 16;  // columns in a row of a thread
+
+FEDRAG_KERNEL __launch_bounds__(kMapThreads) void paged_trim_kernel(PagedTrimJob j, int shift) {
+    __shared__ MapPrefix waves[kMapThreads / kWave];
+    __shared__ uint32_t col_end[kMapThreads];
+    __shared__ int first_col[kMapThreads];
+    __shared__ int flags;
+    const int tid = threadIdx.x;
+    const int64_t max_pages = j.max_pages;
+    const int count_in = *j.free_count;
+    const uint32_t count = count_in < 0 ? 0 : (uint32_t)(count_in < j.n_free ? count_in : j.n_free);
+    const uint32_t most = INT_MAX;
+    uint32_t top = count;
+    if (tid == 0) flags = (uint32_t)count_in == count ? 0 : FEDRAG_TRIM_BAD_LENGTH;
+    for (int64_t b0 = 0; b0 < j.batch; b0 += kMapThreads) {
+        __syncthreads();
+        const int64_t b = b0 + tid;
+        const int n_req = (int)(j.batch - b0 < kMapThreads ? j.batch - b0 : kMapThreads);
+        uint32_t mine = 0;
+        first_col[tid] = 0;
+        if (b < j.batch) {
+            const int kv_in = j.kv_lens[b], kv = kv_in < 0 ? 0 : kv_in;
+            int64_t len = j.n_kept[b];
+            if (j.q_start) len += kv - ((int64_t)j.q_start[b + 1] - j.q_start[b]);
+            const int64_t in = len;
+            len = len < 0 ? 0 : (len < kv ? len : kv);
+            if (in != len || kv_in < 0) atomicOr(&flags, FEDRAG_TRIM_BAD_LENGTH);
+            const int64_t all = ((int64_t)kv + (1 << shift) - 1) >> shift, had = all < max_pages ? all : max_pages;
+            const int64_t stay = (len + (1 << shift) - 1) >> shift;
+            mine = had > stay ? (uint32_t)(had - stay) : 0;
+            first_col[tid] = (int)stay;
+            j.lens_out[b] = (int)len;
+        }
+        MapPrefix total;
+        const MapPrefix p = map_scan(MapPrefix{mine, 0}, most, waves, &total);
+        col_end[tid] = p.rows;
+        __syncthreads();
+        for (uint32_t c0 = 0; c0 < total.rows; c0 += kMapThreads * kTrimEach) {
+            uint32_t at = c0 + tid * kTrimEach;
+            const uint32_t end = min(at + kTrimEach, total.rows);
+            int ids[kTrimEach], n = 0;
+            if (at < end) {
+                int k = first_above(col_end, n_req, at);
+                for (; at < end; ++at) {
+                    while (col_end[k] <= at) ++k;
+                    const uint32_t first = k == 0 ? 0 : col_end[k - 1];
+                    const int id = j.block_table[(b0 + k) * max_pages + first_col[k] + (at - first)];
+                    if (id >= 0) ids[n++] = id;
+                }
+            }
+            MapPrefix found;
+            __syncthreads();  // (the waves' sums of before have been read)
+            const MapPrefix q = map_scan(MapPrefix{(uint32_t)n, 0}, most, waves, &found);
+            uint32_t to = top + q.rows - n;
+            for (int i = 0; i < n; ++i, ++to) {
+                if (to < j.n_free) j.free_pages[to] = ids[i];
+                else atomicOr(&flags, FEDRAG_TRIM_NO_ROOM);
+            }
+            top = min(top + found.rows, (uint32_t)j.n_free);
+        }
+    }
+    __syncthreads();
+    if (tid == 0) {
+        *j.free_left = (int)top;
+        *j.flags = flags;
+    }
+}
+
+hipError_t launch_paged_trim(const PagedTrimJob& job, hipStream_t stream) {
+    hipLaunchKernelGGL(paged_trim_kernel, dim3(1), dim3(kMapThreads), 0, stream, job, __builtin_ctz((unsigned)job.page_tokens));
+    return hipGetLastError();
+}
+
 }  // namespace fedrag

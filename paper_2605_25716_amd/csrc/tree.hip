@@ -1,0 +1,490 @@
+// A drafted step's trees: masks and positions from the nodes' parents (fedrag_tree_map), and the walk that verifies the drafts
+// (fedrag_tree_verify).
+#include "fedrag_device.h"
+#include "fedrag_host.h"
+
+namespace fedrag {
+
+// ------------------------------------------------------------------------------------------------ map
+// A wave per request takes its nodes 64 at a time, a node a lane.  mask[i] = bit i | mask[parent[i]], and so for the number of nodes on
+// the way up: within the 64, each lane's way doubles in length from step to step, six at most, until it ends or leaves the 64; what
+// lies above is the finished mask of the node where it left, read back.
+constexpr int kTreeMapThreads = 256;
+
+struct TreeMapJob {
+    int batch, n_rows, words;
+    const int32_t *q_start, *kv_lens, *parents;
+    uint64_t* mask;
+    int32_t *positions, *flags;
+};
+
+__device__ __forceinline__ int clamped(int x, int lo, int hi) { return x < lo ? lo : (x < hi ? x : hi); }
+
+FEDRAG_KERNEL __launch_bounds__(kTreeMapThreads) void tree_map_kernel(TreeMapJob j, int request_wgs) {
+    const int lane = threadIdx.x % kWave;
+    const int words = j.words;
+    if ((int)blockIdx.x >= request_wgs) {  // padding rows
+        const int64_t t = (int64_t)(blockIdx.x - request_wgs) * kTreeMapThreads + threadIdx.x;
+        const int end = j.batch > 0 ? clamped(j.q_start[j.batch], 0, j.n_rows) : 0;
+        if (t < end || t >= j.n_rows) return;
+        for (int w = 0; w < words; ++w) j.mask[t * words + w] = 0;
+        if (j.positions) j.positions[t] = -1;
+        return;
+    }
+    const int64_t b = (int64_t)blockIdx.x * (kTreeMapThreads / kWave) + threadIdx.x / kWave;
+    if (b >= j.batch) return;
+    const int s = clamped(j.q_start[b], 0, j.n_rows), e = clamped(j.q_start[b + 1], 0, j.n_rows), kv = j.kv_lens[b];
+    const int n = e > s ? e - s : 0, base = (kv < 0 ? 0 : kv) - n;
+    int bad = n > (int64_t)64 * words ? FEDRAG_TREE_NO_WORDS : 0;
+    for (int i0 = 0; i0 < n; i0 += kWave) {
+        const int i = i0 + lane;
+        int up = i < n ? j.parents[s + i] : -1;
+        if (up < -1 || up >= i) {
+            if (i < n) bad |= FEDRAG_TREE_BAD_PARENT;
+            up = -1;
+        }
+        int inside = up - i0, outside = up;  // the next on the way up: a lane, or (inside < 0) a node before these, or none
+        uint64_t bits = (uint64_t)1 << lane;
+        int count = 1;
+#pragma unroll 1
+        for (int step = 0; step < 6 && __builtin_amdgcn_ballot_w64(inside >= 0) != 0; ++step) {
+            const int from = inside < 0 ? lane : inside;
+            const uint64_t more = __shfl((unsigned long long)bits, from);
+            const int n_more = __shfl(count, from), in = __shfl(inside, from), out = __shfl(outside, from);
+            if (inside >= 0) {
+                bits |= more;
+                count += n_more;
+                inside = in;
+                outside = out;
+            }
+        }
+        if (i < n) {
+            uint64_t* const mine = j.mask + (int64_t)(s + i) * words;
+            const uint64_t* const above = j.mask + (int64_t)(s + outside) * words;  // (read only where there is such a node)
+            for (int w = 0; w < words; ++w) mine[w] = w == i0 / kWave ? bits : (outside >= 0 && w < i0 / kWave ? above[w] : 0);
+            if (j.positions) j.positions[s + i] = outside >= 0 ? j.positions[s + outside] + count : base + count - 1;
+        }
+        if (i0 + kWave < n) __threadfence_block();  // the next nodes read what this wave has stored
+    }
+    const uint64_t any1 = __builtin_amdgcn_ballot_w64((bad & 1) != 0), any2 = __builtin_amdgcn_ballot_w64((bad & 2) != 0);
+    if (lane == 0) j.flags[b] = (any1 ? 1 : 0) | (any2 ? 2 : 0);
+}
+
+static int64_t tree_map_wgs(int batch, int64_t n_rows) {
+    return ((int64_t)batch + kTreeMapThreads / kWave - 1) / (kTreeMapThreads / kWave) + (n_rows + kTreeMapThreads - 1) / kTreeMapThreads;
+}
+bool tree_map_fits(int batch, int64_t n_rows) { return tree_map_wgs(batch, n_rows) == 0 || grid_fits(tree_map_wgs(batch, n_rows), kTreeMapThreads); }
+
+hipError_t launch_tree_map(int batch, int64_t n_rows, int words, const int32_t* q_start, const int32_t* kv_lens, const int32_t* parents,
+                           uint64_t* mask, int32_t* positions, int32_t* flags, hipStream_t stream) {
+    const int64_t wgs = tree_map_wgs(batch, n_rows);
+    if (wgs == 0) return hipSuccess;
+    const int requests = (batch + kTreeMapThreads / kWave - 1) / (kTreeMapThreads / kWave);
+    hipLaunchKernelGGL(tree_map_kernel, dim3((unsigned)wgs), dim3(kTreeMapThreads), 0, stream,
+                       TreeMapJob{batch, (int)n_rows, words, q_start, kv_lens, parents, mask, positions, flags}, requests);
+    return hipGetLastError();
+}
+
+// ------------------------------------------------------------------------------------------------ verify
+// A request's walk is a chain: what a rejection leaves of the target's probabilities has to be summed before the next sibling is
+// tried.  The launches are rounds.  In each, kPart tokens of the vocabulary are a workgroup's, for every request; it goes on with the
+// request's walk by itself, from the state and the sums of the round before, until a sum over the vocabulary is needed, and adds up
+// its part of it.  The state is the same in all of a request's workgroups, and the first one writes it down.  No workgroup waits for
+// another.  What the last round finds unfinished, the request's first workgroup finishes alone.
+// The walk itself costs two trips to memory for 64 nodes: a lane has a node, and fetches both of its probabilities ahead of the walk.
+// A sum is over whole numbers of units, so that neither parts nor rounds show in the result.
+constexpr int kVerifyThreads = 256;
+constexpr int kPart = 4096;                          // tokens of a workgroup
+constexpr int kEach = kPart / kVerifyThreads;        // and of a thread
+constexpr int kMostParts = (1 << 20) / kPart;
+static_assert(kMostParts <= kVerifyThreads, "a thread per part finds the part of a threshold");
+constexpr double kUnits = 8796093022208.0;           // 2^43
+constexpr uint64_t kUnit = (uint64_t)1 << 43;
+constexpr uint64_t kMostUnits = (uint64_t)1 << 63;
+
+enum : int { kVerifyDone = 0, kVerifyMass = 1, kVerifyDraw = 2 };
+struct VerifyState {
+    int need;          // what the sums of this round are for
+    int node, last;    // where the walk is, and the child tried last (or the node)
+    int n_kept;
+    uint64_t taken;    // C
+};
+struct VerifySums {
+    uint64_t left, all;  // of r, of p
+};
+
+__device__ __forceinline__ float verify_value(float x) { return fminf(fmaxf(x, 0.f), 1.f); }  // (not a number: 0)
+__device__ __forceinline__ double verify_random(double u) { return fmin(fmax(u, 0.0), 0x1.fffffffffffffp-1); }
+// r in units: adding 2^52 rounds to a whole number, which is then the low bits.
+__device__ __forceinline__ uint64_t verify_units(double r) {
+    return __builtin_bit_cast(uint64_t, __builtin_fma(r, kUnits, 0x1p52)) & (((uint64_t)1 << 52) - 1);
+}
+__device__ __forceinline__ double verify_left(float p, float q, double taken) {
+#pragma clang fp contract(off)
+    const double product = taken * (double)q;
+    return fmax((double)p - product, 0.0);
+}
+
+template <class E, bool DRAFT>
+struct Verify {
+    const TreeVerifyJob& j;
+    int b, s, n, parts;
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    uint64_t (*scratch)[2];  // LDS, a pair for each wave
+
+    __device__ __forceinline__ const E* row_p(int node) const { return (const E*)j.target + (int64_t)(s + node) * j.target_stride; }
+    __device__ __forceinline__ const E* row_q(int node) const { return (const E*)j.draft + (int64_t)(s + node) * j.draft_stride; }
+
+    // ---- the nodes, 64 at a time
+    int at;  // the first of them; < 0: none yet
+    int parent, token;
+    float p, q;
+    double u;
+    __device__ __forceinline__ void window(int i0) {
+        if (i0 == at) return;
+        at = i0;
+        const int i = i0 + lane;
+        parent = -1;
+        token = -1;
+        p = q = 0.f;
+        u = 0.0;
+        if (i < n) {
+            parent = j.parents[s + i];
+            token = j.tokens[s + i];
+            u = verify_random(j.u[s + i]);
+            if (parent >= i || token >= j.vocab) parent = -1;
+            if (token < 0) parent = -1;
+            if (parent >= 0) {
+                p = verify_value((float)row_p(parent)[token]);
+                if constexpr (DRAFT) q = verify_value((float)row_q(parent)[token]);
+            }
+        }
+    }
+    static __device__ __forceinline__ float lane_float(float x, int l) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), l)); }
+    static __device__ __forceinline__ double lane_double(double x, int l) {
+        const uint64_t v = __builtin_bit_cast(uint64_t, x);
+        const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, l), hi = (uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), l);
+        return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+    }
+    // Whether a child of `node` before child i has its token x.
+    __device__ __forceinline__ bool repeated(int node, int i, int x) {
+        bool found = __builtin_amdgcn_ballot_w64(parent == node && at + lane < i && token == x) != 0;
+        for (int k = (node + 1) & ~(kWave - 1); k < at && !found; k += kWave) {
+            const int c = k + lane;
+            found = __builtin_amdgcn_ballot_w64(c > node && j.parents[s + c] == node && j.tokens[s + c] == x) != 0;
+        }
+        return found;
+    }
+    // f(child, token) for each child of the node up to child `last`, in order
+    template <class F>
+    __device__ __forceinline__ void rejected(const VerifyState& st, F f) {
+        if (st.last <= st.node) return;
+        for (int k = (st.node + 1) & ~(kWave - 1); k <= st.last; k += kWave) {
+            window(k);
+            uint64_t m = __builtin_amdgcn_ballot_w64(parent == st.node && k + lane <= st.last);
+            for (; m; m &= m - 1) {
+                const int l = __builtin_ctzll(m);
+                f(k + l, __builtin_amdgcn_readlane(token, l));
+            }
+        }
+    }
+
+    // Goes on from `st`, whose M is known, until a sum is needed.  first: whether this workgroup writes what is accepted.
+    __device__ __forceinline__ void walk(VerifyState& st, uint64_t mass, bool first) {
+        bool known = true;
+        st.need = kVerifyDraw;
+        if (st.n_kept >= j.max_kept) return;
+        int i0 = (st.last + 1) & ~(kWave - 1);
+        while (i0 < n) {
+            window(i0);
+            const uint64_t m = __builtin_amdgcn_ballot_w64(parent == st.node && i0 + lane > st.last);
+            if (m == 0) {
+                i0 += kWave;
+                continue;
+            }
+            if (!known) {
+                st.need = kVerifyMass;
+                return;
+            }
+            const int l = __builtin_ctzll(m), child = i0 + l;
+            const float pc = lane_float(p, l);
+            const double uc = lane_double(u, l);
+            bool yes;
+            uint64_t gone = 0;
+            if constexpr (DRAFT) {
+#pragma clang fp contract(off)
+                const float qc = lane_float(q, l);
+                const double low = uc * (double)qc * (double)mass;
+                yes = low < verify_left(pc, qc, (double)st.taken / kUnits) * kUnits;
+            } else {
+                const double left = repeated(st.node, child, __builtin_amdgcn_readlane(token, l)) ? 0.0 : (double)pc;
+                yes = uc * (double)mass < left * kUnits;
+                gone = verify_units(left);
+            }
+            st.last = child;
+            if (yes) {
+                st.node = child;
+                if (first && threadIdx.x == 0) j.kept[b * j.max_kept + st.n_kept] = child;
+                ++st.n_kept;
+                st.taken = 0;
+                mass = kUnit;
+                if (st.n_kept >= j.max_kept) return;
+            } else if constexpr (DRAFT) {
+                st.taken = mass < kMostUnits - st.taken ? st.taken + mass : kMostUnits;
+                known = false;
+            } else {
+                mass = mass > gone ? mass - gone : 0;
+            }
+        }
+    }
+
+    // ---- sums over the vocabulary
+    __device__ __forceinline__ VerifySums weights(float pv, float qv, double taken) const {
+        const float x = verify_value(pv);
+        const uint64_t all = verify_units((double)x);
+        return VerifySums{DRAFT ? verify_units(verify_left(x, verify_value(qv), taken)) : all, all};
+    }
+    // This thread's share of a part's sums; every token of the part is some thread's.  Where nothing was rejected r is p, and q is not read.
+    __device__ __forceinline__ VerifySums part_sums(const VerifyState& st, int part) const {
+        const E* const pr = row_p(st.node);
+        const E* const qr = DRAFT ? row_q(st.node) : pr;
+        const bool with_q = DRAFT && st.taken != 0;
+        const double taken = (double)st.taken / kUnits;
+        const int begin = part * kPart, end = begin + kPart < j.vocab ? begin + kPart : j.vocab;
+        VerifySums sum{0, 0};
+        auto add = [&](float pv, float qv) {
+            const VerifySums w = weights(pv, qv, taken);
+            sum.left += w.left;
+            sum.all += w.all;
+        };
+        constexpr int VEC = 16 / (int)sizeof(E);
+        typedef E vec __attribute__((ext_vector_type(VEC)));
+        const bool wide = ((reinterpret_cast<uintptr_t>(pr) | (with_q ? reinterpret_cast<uintptr_t>(qr) : 0)) & 15) == 0;
+        if (wide && end - begin == kPart) {
+            vec pv[kEach / VEC], qv[kEach / VEC];
+#pragma unroll
+            for (int i = 0; i < kEach / VEC; ++i) pv[i] = *(const vec*)(pr + begin + (i * kVerifyThreads + (int)threadIdx.x) * VEC);
+            if (with_q) {
+#pragma unroll
+                for (int i = 0; i < kEach / VEC; ++i) qv[i] = *(const vec*)(qr + begin + (i * kVerifyThreads + (int)threadIdx.x) * VEC);
+            }
+#pragma unroll
+            for (int i = 0; i < kEach / VEC; ++i)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) add((float)pv[i][e], with_q ? (float)qv[i][e] : 0.f);
+        } else {
+#pragma unroll 4
+            for (int v = begin + (int)threadIdx.x; v < end; v += kVerifyThreads) add((float)pr[v], with_q ? (float)qr[v] : 0.f);
+        }
+        return sum;
+    }
+    static __device__ __forceinline__ uint64_t wave_add(uint64_t x) {
+#pragma unroll
+        for (int o = 1; o < kWave; o <<= 1) x += __shfl_xor((unsigned long long)x, o);
+        return x;
+    }
+    __device__ __forceinline__ VerifySums total(VerifySums x) const {
+        x.left = wave_add(x.left);
+        x.all = wave_add(x.all);
+        __syncthreads();
+        if (lane == 0) {
+            scratch[wave][0] = x.left;
+            scratch[wave][1] = x.all;
+        }
+        __syncthreads();
+        x = VerifySums{0, 0};
+#pragma unroll
+        for (int w = 0; w < kVerifyThreads / kWave; ++w) {
+            x.left += scratch[w][0];
+            x.all += scratch[w][1];
+        }
+        return x;
+    }
+    // A part's sums, in every thread.
+    __device__ __forceinline__ VerifySums part_total(const VerifyState& st, int part) {
+        VerifySums x = total(part_sums(st, part));
+        if constexpr (!DRAFT) {
+            if (st.need == kVerifyDraw)
+                rejected(st, [&](int child, int v) {
+                    if (v / kPart == part && !repeated(st.node, child, v)) x.left -= verify_units((double)verify_value((float)row_p(st.node)[v]));
+                });
+        }
+        return x;
+    }
+    // Of numbers x, one a thread: the first thread whose inclusive sum is above `t` (kVerifyThreads: none), and the sum before it.
+    __device__ __forceinline__ int first_beyond(uint64_t x, uint64_t t, uint64_t* before) const {
+        uint64_t to = x;
+#pragma unroll
+        for (int o = 1; o < kWave; o <<= 1) {
+            const uint64_t y = __shfl_up((unsigned long long)to, o);
+            if (lane >= o) to += y;
+        }
+        __syncthreads();
+        if (lane == kWave - 1) scratch[wave][0] = to;
+        __syncthreads();
+        uint64_t base = 0;
+        int found = kVerifyThreads;
+        *before = 0;
+#pragma unroll
+        for (int w = 0; w < kVerifyThreads / kWave; ++w) {
+            const uint64_t sum = scratch[w][0];
+            if (found == kVerifyThreads && base + sum > t) {
+                found = w;
+                *before = base;
+            }
+            base += sum;
+        }
+        if (found == kVerifyThreads) return found;
+        const int in = found;
+        __syncthreads();
+        if (wave == in) {
+            const int l = __builtin_popcountll(__builtin_amdgcn_ballot_w64(*before + to <= t));
+            if (lane == l) {
+                scratch[0][0] = *before + to - x;
+                scratch[0][1] = (uint64_t)l;
+            }
+        }
+        __syncthreads();
+        *before = scratch[0][0];
+        return in * kWave + (int)scratch[0][1];
+    }
+    // The token, from the sums of the parts, a thread each.  only: the workgroup's part, or -1: whichever it is.
+    __device__ __forceinline__ void draw(const VerifyState& st, VerifySums mine, int only) {
+        const VerifySums sum = total(mine);
+        const bool left = sum.left != 0;
+        const uint64_t all = left ? sum.left : sum.all;
+        if (all == 0) {
+            if (only <= 0 && threadIdx.x == 0) j.next_token[b] = -1;
+            return;
+        }
+        const double x = verify_random(j.u_next[b]) * (double)all;
+        uint64_t t = (uint64_t)x;
+        t = t < all ? t : all - 1;
+        uint64_t before;
+        const int part = first_beyond(left ? mine.left : mine.all, t, &before);
+        if (only >= 0 && part != only) return;
+        const E* const pr = row_p(st.node);
+        const E* const qr = DRAFT ? row_q(st.node) : pr;
+        const double taken = (double)st.taken / kUnits;
+        const int v0 = part * kPart + (int)threadIdx.x * kEach;
+        uint64_t w[kEach], here = 0;
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+            VerifySums x{0, 0};
+            if (v0 + e < j.vocab) x = weights((float)pr[v0 + e], DRAFT && st.taken != 0 ? (float)qr[v0 + e] : 0.f, taken);
+            w[e] = left ? x.left : x.all;
+        }
+        if constexpr (!DRAFT) {
+            if (left)
+                rejected(st, [&](int, int v) {
+#pragma unroll
+                    for (int e = 0; e < kEach; ++e) w[e] = v0 + e == v ? 0 : w[e];
+                });
+        }
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) here += w[e];
+        const uint64_t t_part = t - before;
+        uint64_t in_part;
+        const int thread = first_beyond(here, t_part, &in_part);
+        if ((int)threadIdx.x == thread) {
+            int v = v0;
+            uint64_t to = in_part;
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) {
+                to += w[e];
+                if (to <= t_part) v = v0 + e + 1;
+            }
+            j.next_token[b] = v;
+        }
+    }
+};
+
+template <class E, bool DRAFT>
+FEDRAG_KERNEL __launch_bounds__(kVerifyThreads) void tree_verify_kernel(TreeVerifyJob j, int parts, int round, int last_round) {
+    __shared__ uint64_t scratch[kVerifyThreads / kWave][2];
+    const int part = (int)blockIdx.x, b = (int)blockIdx.y;
+    VerifyState* const states = (VerifyState*)j.workspace;  // [2][batch], then the sums [2][batch][parts]
+    VerifySums* const sums = (VerifySums*)(states + 2 * (int64_t)j.batch);
+    const int now = round & 1, before = 1 - now;
+    const int s = clamped(j.q_start[b], 0, j.n_rows), e = clamped(j.q_start[b + 1], 0, j.n_rows);
+    Verify<E, DRAFT> v{j, b, s, e > s ? e - s : 0, parts};
+    v.scratch = scratch;
+    v.at = -1;
+    VerifyState st{kVerifyDone, 0, 0, 1, 0};
+    auto own_sum = [&]() {
+        const int t = threadIdx.x;
+        return t < parts ? sums[((int64_t)before * j.batch + b) * parts + t] : VerifySums{0, 0};
+    };
+    if (round == 0) {
+        if (v.n > 0) {
+            if (part == 0 && threadIdx.x == 0) j.kept[b * j.max_kept] = 0;
+            v.walk(st, kUnit, part == 0);
+        } else if (part == 0) {
+            for (int64_t i = threadIdx.x; i < j.max_kept; i += kVerifyThreads) j.kept[b * j.max_kept + i] = 0;
+            if (threadIdx.x == 0) {
+                j.n_kept[b] = 0;
+                j.next_token[b] = -1;
+            }
+        }
+    } else {
+        st = states[(int64_t)before * j.batch + b];
+        if (st.need == kVerifyDraw) {
+            v.draw(st, own_sum(), part);
+            st.need = kVerifyDone;
+        } else if (st.need == kVerifyMass) {
+            const VerifySums sum = v.total(own_sum());
+            v.walk(st, sum.left, part == 0);
+        }
+    }
+    auto finish_kept = [&]() {  // the path is complete
+        if (part != 0) return;
+        for (int64_t i = st.n_kept + threadIdx.x; i < j.max_kept; i += kVerifyThreads) j.kept[b * j.max_kept + i] = 0;
+        if (threadIdx.x == 0) j.n_kept[b] = st.n_kept;
+    };
+    if (round < last_round) {
+        if (part == 0 && threadIdx.x == 0) states[(int64_t)now * j.batch + b] = st;
+        if (st.need == kVerifyDone) return;
+        if (st.need == kVerifyDraw) finish_kept();
+        const VerifySums sum = v.part_total(st, part);
+        if (threadIdx.x == 0) sums[((int64_t)now * j.batch + b) * parts + part] = sum;
+        return;
+    }
+    if (st.need == kVerifyDone || part != 0) return;
+    while (st.need == kVerifyMass) {  // (each time around a child has been tried)
+        VerifySums sum{0, 0};
+        for (int i = 0; i < parts; ++i) sum.left += v.part_sums(st, i).left;
+        sum = v.total(sum);
+        v.walk(st, sum.left, true);
+    }
+    finish_kept();
+    VerifySums mine{0, 0};
+    for (int i = 0; i < parts; ++i) {
+        const VerifySums sum = v.part_total(st, i);
+        if ((int)threadIdx.x == i) mine = sum;
+    }
+    v.draw(st, mine, -1);
+}
+
+static int verify_parts(int vocab) { return (vocab + kPart - 1) / kPart; }
+size_t tree_verify_workspace(int batch, int vocab) {
+    return 2 * (size_t)batch * (sizeof(VerifyState) + (size_t)verify_parts(vocab) * sizeof(VerifySums));
+}
+
+template <class E>
+static hipError_t launch_tree_verify_t(const TreeVerifyJob& job, hipStream_t stream) {
+    const int parts = verify_parts(job.vocab);
+    const int last = job.draft ? 3 : 1;
+    const auto kernel = job.draft ? tree_verify_kernel<E, true> : tree_verify_kernel<E, false>;
+    for (int round = 0; round <= last; ++round)
+        hipLaunchKernelGGL(kernel, dim3((unsigned)parts, (unsigned)job.batch), dim3(kVerifyThreads), 0, stream, job, parts, round, last);
+    return hipGetLastError();
+}
+hipError_t launch_tree_verify(const TreeVerifyJob& job, hipStream_t stream) {
+    switch (job.dtype) {
+        case FEDRAG_F32: return launch_tree_verify_t<float>(job, stream);
+        case FEDRAG_BF16: return launch_tree_verify_t<__bf16>(job, stream);
+        default: return launch_tree_verify_t<_Float16>(job, stream);
+    }
+}
+
+}  // namespace fedrag
