@@ -32,7 +32,7 @@ namespace fedrag {
 constexpr uint32_t kPagedShortRun = 8, kPagedWhole = 48;
 struct PagedCut {
     int tile_shift, unit_shift, least, target_shift;
-    int gain;       // runs: a tile is cut only if they are shorter than the whole by so many units
+    int gain;       // runs: a tile is cut only if they are shorter than the whole by so many units; shares: units that a tile counts beside its own
     int few, many;  // only requests with few <= R <= many are this launch's
 };
 
@@ -271,30 +271,42 @@ struct PagedSpan {
 struct PagedLanes {
     uint32_t to[kWave];       // units up to the lane's last request
     PagedRequest one[kWave];  // its request, where it has one
+    uint32_t extra;
 };
 template <class Args>
 struct PagedShares {
     PagedLanes& lanes;
     uint32_t total, share, whole;  // a tile of no more than `whole` units is not cut
 
-    static __device__ __forceinline__ uint32_t cost(Args& a, const PagedRequest& r) {
-        return paged_tiles(a, r) * (uint32_t)a.Hkv * paged_units(a, r);
+    uint32_t extra;                // units that a tile counts beside its own
+
+    __device__ __forceinline__ uint32_t cost(Args& a, const PagedRequest& r) const {
+        return paged_tiles(a, r) * (uint32_t)a.Hkv * (paged_units(a, r) + extra);
     }
     // By all threads: the first wave counts, the others wait for it.
     __device__ __forceinline__ PagedShares(Args& a, PagedLanes& found) : lanes(found) {
         const int lane = threadIdx.x % kWave;
         if (threadIdx.x < kWave) {
             PagedRequest one{};
-            uint32_t mine = 0;
+            uint32_t mine = 0, tiles = 0;
+            extra = 0;
             paged_each(a, [&](const PagedRequest& r, bool is) {
                 one = r;
                 mine += is ? cost(a, r) : 0;
+                tiles += is ? paged_tiles(a, r) * (uint32_t)a.Hkv : 0;
             });
-            lanes.to[lane] = wave_scan(mine);
+            uint32_t to = wave_scan(mine);
+            if (a.cut.gain != 0 && lane_value(to, kWave - 1) >> a.cut.target_shift >= 2) {
+                extra = (uint32_t)a.cut.gain;
+                to += extra * wave_scan(tiles);
+            }
+            lanes.to[lane] = to;
             lanes.one[lane] = one;
+            lanes.extra = extra;
         }
         __syncthreads();
         total = lane_value(lanes.to[kWave - 1], 0);
+        extra = lane_value(lanes.extra, 0);
         share = (uint32_t)(((uint64_t)total + ((uint64_t)1 << a.cut.target_shift) - 1) >> a.cut.target_shift);
         share = share > (uint32_t)a.cut.least ? share : (uint32_t)a.cut.least;
         whole = share / 8 > (uint32_t)a.cut.least ? share / 8 : (uint32_t)a.cut.least;
@@ -307,7 +319,7 @@ struct PagedShares {
         uint32_t base;
         const int lane = threadIdx.x % kWave;
         s.req = paged_find(a, pos, lanes.to[lane], lanes.one[lane], [&](const PagedRequest& r) { return cost(a, r); }, &s.b, &base);
-        s.n = paged_units(a, s.req);
+        s.n = paged_units(a, s.req) + extra;
         const uint32_t i = (pos - base) / s.n, tile = FastDiv::div_by(a.by_hkv.m, a.by_hkv.s, i);
         s.begin = base + i * s.n;
         s.head = (int)(i - tile * a.by_hkv.d);
@@ -427,7 +439,7 @@ __device__ __forceinline__ float paged_log2_sum(float reference, float sum) {
 hipError_t launch_paged_16(const PagedArgs& a, int64_t chunks, const PagedArgs& d, int64_t decodes, int D, int dtype, hipStream_t stream);
 hipError_t launch_paged_f32(const PagedArgs& a, int64_t grid, int D, hipStream_t stream);
 // The same for rows with masks of their own.
-hipError_t launch_tree_16(const PagedArgs& a, int64_t chunks, const PagedArgs& d, int64_t decodes, int D, int dtype, hipStream_t stream);
+hipError_t launch_tree_16(const PagedArgs& a, int64_t many, const PagedArgs& d, int64_t few, int D, int dtype, hipStream_t stream);
 hipError_t launch_tree_f32(const PagedArgs& a, int64_t grid, int D, hipStream_t stream);
 
 }  // namespace fedrag

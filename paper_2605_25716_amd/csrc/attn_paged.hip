@@ -157,7 +157,7 @@ static int64_t paged_units_of(PagedCut& cut, int64_t tiles, int64_t keys) {
     int64_t units = 1;
     do {
         units = keys > 0 ? ((keys - 1) >> cut.unit_shift) + 1 : 1;
-    } while (tiles > INT32_MAX / units && ++cut.unit_shift < 31);
+    } while (tiles > INT32_MAX / (units + cut.gain) && ++cut.unit_shift < 31);
     return units;
 }
 static PagedLaunch paged_runs(PagedCut cut, int64_t tiles, int64_t keys) {
@@ -189,7 +189,7 @@ struct PagedPlan {
     PagedLaunch runs, shares;
     size_t bytes(int D) const { return runs.bytes(D) + shares.bytes(D); }
 };
-static PagedPlan paged_plan(int B, int Hq, int Hkv, int dtype, int64_t T, int64_t keys, int64_t max_q_len) {
+static PagedPlan paged_plan(int B, int Hq, int Hkv, int dtype, int64_t T, int64_t keys, int64_t max_q_len, bool tree) {
     const int64_t G = Hq / Hkv, some = B < T ? B : T;
     // at least the tiles that T rows of B requests come to
     auto tiles = [&](int tile_shift) { return ((T * G >> tile_shift) + some) * Hkv; };
@@ -206,6 +206,12 @@ static PagedPlan paged_plan(int B, int Hq, int Hkv, int dtype, int64_t T, int64_
         p.runs = paged_runs(PagedCut{tile, 6, 4 * t < full ? 1 : 2 * t < full ? 2 : 4, cus + 1, 0, 1, INT32_MAX}, t, keys);
         return p;
     }
+    if (tree && most * G <= 64) {
+        const int tile = !many ? 4 : most * G <= 32 ? 5 : 6;
+        p.shares = paged_shares(PagedCut{tile, 8, 1, tile == 6 ? cus : cus + 1, 1, 1, INT32_MAX}, tiles(tile), keys);
+        return p;
+    }
+    const int few_rows = tree ? 2 * kPagedDecodeRows : kPagedDecodeRows;  // of a request of few rows, beside others of many
     if (many) {
         // Runs have four tiles of keys at least, but twice or four times that where the tiles alone occupy much of the device, as then
         // the aggregation costs more than shorter runs save (32 heads of 128, least 4 and by this rule: 512 rows over 512 keys 27.2 and
@@ -213,25 +219,24 @@ static PagedPlan paged_plan(int B, int Hq, int Hkv, int dtype, int64_t T, int64_
         // 19.0, 20 over 500 19.2 and 15.6, 569 and 57 of 2 heads over as many 20.6 and 16.7; with 32 tiles 117 over 4001 30.1 and 31.2).
         // A cut has to save 6 units, 4 of few tiles (300 over 500 24.2 us without, 22.4 so; 64 over 300 17.1, and 18.3 with 6).
         // (t: beside the other form a request of this one has more than its rows)
-        const int64_t by_rows = T * G / (kPagedDecodeRows + 1) * Hkv;
+        const int64_t by_rows = T * G / (few_rows + 1) * Hkv;
         const int64_t t = few && by_rows < tiles(7) ? by_rows : tiles(7), full = (int64_t)3 << cus >> 2;
         const int least = 8 * t <= full ? 1 : 2 * t < full ? 4 : t < full ? 8 : 16, gain = least == 1 ? 4 : 6;
-        p.runs = paged_runs(PagedCut{7, 6, least, cus + 1, gain, few ? kPagedDecodeRows + 1 : 1, INT32_MAX}, t, keys);
+        p.runs = paged_runs(PagedCut{7, 6, least, cus + 1, gain, few ? few_rows + 1 : 1, INT32_MAX}, t, keys);
     }
     // beside requests of many rows: one workgroup to a compute unit, for as long as the others take
     if (few)
-        p.shares = paged_shares(PagedCut{4, 8, 1, many ? cus : cus + 1, 0, 1, many ? kPagedDecodeRows : INT32_MAX}, many ? some * Hkv : tiles(4), keys);
+        p.shares = paged_shares(PagedCut{tree ? 5 : 4, 8, 1, many ? cus : cus + 1, 0, 1, many ? few_rows : INT32_MAX}, many ? some * Hkv : tiles(4), keys);
     return p;
 }
 
 bool paged_attn_fits(int B, int Hq, int Hkv, int D, int dtype, int64_t T, int64_t max_pages, int page_tokens, int64_t max_q_len, bool tree,
                      size_t* bytes) {
-    (void)tree;
     *bytes = 0;
     if (T == 0 || B == 0) return true;
     const int64_t rows = T * (Hq / Hkv);
     if (rows > INT32_MAX || ((rows >> 4) + (B < T ? B : T)) * Hkv > INT32_MAX) return false;  // (tiles of 16 rows, the finest)
-    const PagedPlan plan = paged_plan(B, Hq, Hkv, dtype, T, max_pages * page_tokens, max_q_len);
+    const PagedPlan plan = paged_plan(B, Hq, Hkv, dtype, T, max_pages * page_tokens, max_q_len, tree);
     if (!grid_fits(plan.runs.grid + plan.shares.grid, 256)) return false;  // (the aggregation's is below 2^14)
     *bytes = plan.bytes(D);
     return true;
@@ -260,7 +265,7 @@ hipError_t launch_paged_attn(const PagedAttnProblem& p, hipStream_t stream) {
     a.lse = p.lse;
     a.tree = p.tree;
     a.tree_words = p.tree_words;
-    const PagedPlan plan = paged_plan(p.B, p.Hq, p.Hkv, p.dtype, p.T, p.max_pages << p.pages.shift, p.max_q_len);
+    const PagedPlan plan = paged_plan(p.B, p.Hq, p.Hkv, p.dtype, p.T, p.max_pages << p.pages.shift, p.max_q_len, p.tree != nullptr);
     auto with = [&](const PagedLaunch& l, char* scratch) {
         PagedArgs x = a;
         x.cut = l.cut;

@@ -29,8 +29,8 @@ struct PagedSmall {
 };
 // Wave w's slot of two arrays (by value: a choice between variables that a lambda holds puts them in scratch memory).
 __device__ __forceinline__ char* paged_slot(char* first, char* second, int w, int bytes) { return (w < 2 ? first : second) + w % 2 * bytes; }
-// ARGS: which of the kernel's arguments `a` is.  TREE: rows have masks of their own.
-template <class T, int D, int ARGS, bool TREE = false>
+// ARGS: which of the kernel's arguments `a` is.
+template <class T, int D, int ARGS>
 __device__ __forceinline__ void paged_decode_body(const PagedArgs& a, uint32_t index, char* ks0, char* ks1, char* vs0, char* vs1, PagedSmall<D>& sm) {
     typedef typename T::elem elem;
     typedef typename T::vec8 vec8;
@@ -53,10 +53,8 @@ __device__ __forceinline__ void paged_decode_body(const PagedArgs& a, uint32_t i
     const int row0 = p.tile << a.cut.tile_shift;                                  // the tile's first flattened row
     const int R = q.R - row0 < 16 ? q.R - row0 : 16;
     const int row = row0 + (lr < R ? lr : R - 1);
-    const int lim = TREE ? q.keys : paged_limit(a, q, row);                // this lane's row sees keys < lim
-    const int base = TREE ? paged_base(q, (int)a.by_g.div((uint32_t)q.R)) : 0;
-    const int lim_min = TREE ? (base < 0 ? 0 : (base < q.keys ? base : q.keys)) : __builtin_amdgcn_readlane(lim, 0);
-    const int lim_max = TREE ? q.keys : __builtin_amdgcn_readlane(lim, 15);
+    const int lim = paged_limit(a, q, row);                                // this lane's row sees keys < lim
+    const int lim_min = __builtin_amdgcn_readlane(lim, 0), lim_max = __builtin_amdgcn_readlane(lim, 15);
     const int k_begin = (int)((int64_t)u0 << a.cut.unit_shift);            // below the request's keys: 31 bits
     const int64_t span_end = ((int64_t)u0 + take) << a.cut.unit_shift;
     const int k_end = span_end < lim_max ? (int)span_end : lim_max;        // (may lie before k_begin: nothing to see)
@@ -128,9 +126,6 @@ __device__ __forceinline__ void paged_decode_body(const PagedArgs& a, uint32_t i
         const int key0 = k_begin + (wave + i * WAVES) * kDecTile;
         const int id0 = __builtin_amdgcn_readlane((int)(offset >> 32), 2 * (i % 32)), id1 = __builtin_amdgcn_readlane((int)(offset >> 32), 2 * (i % 32) + 1);
         const bool masked = key0 + kDecTile > (lim_min < k_end ? lim_min : k_end) || (id0 | id1) < 0;
-        uint32_t seen_bits = ~0u;  // of the tile's keys, by the row's mask
-        if constexpr (TREE)
-            if (masked) seen_bits = (uint32_t)paged_tree_bits(a, q, base, (int)tok, key0);
         if (MORE && i % 32 == 31) offset = offsets(i + 1);
         wait_loads(std::integral_constant<int, KL>{});  // K's (V's are younger)
         f32x4_t s[2];
@@ -155,8 +150,7 @@ __device__ __forceinline__ void paged_decode_body(const PagedArgs& a, uint32_t i
             const int left = (lim < k_end ? lim : k_end) - key0 - lq * 4;
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                if ((e / 4) * 16 + e % 4 >= left || (e < 4 ? id0 : id1) < 0 || (TREE && !(seen_bits >> (lq * 4) >> ((e / 4) * 16 + e % 4) & 1)))
-                    x[e] = -INFINITY;
+                if ((e / 4) * 16 + e % 4 >= left || (e < 4 ? id0 : id1) < 0) x[e] = -INFINITY;
         }
         float mx = -INFINITY;
 #pragma unroll
@@ -218,8 +212,7 @@ __device__ __forceinline__ void paged_decode_body(const PagedArgs& a, uint32_t i
                         vt[t][w] = v;
                     }
                 const int seen = (lim < k_end ? lim : k_end) - key0;
-                for (int key = 0; key < kDecTile && key < seen; ++key) {
-                    if (TREE && !(seen_bits >> key & 1)) continue;
+                for (int key = 0; key < kDecTile && key < seen; ++key)
 #pragma unroll
                     for (int t = 0; t < DCH; ++t) {
                         // acc[t] holds channels 16 t + 4 lq + 0..3: half of a 16-byte chunk
@@ -230,7 +223,6 @@ __device__ __forceinline__ void paged_decode_body(const PagedArgs& a, uint32_t i
                             if ((v & kExp) == kExp) acc[t][e] += T::to_float(__builtin_bit_cast(elem, (uint16_t)v));
                         }
                     }
-                }
             }
         }
 #pragma unroll
@@ -295,11 +287,7 @@ __device__ __forceinline__ void paged_decode_body(const PagedArgs& a, uint32_t i
         for (int e = 0; e < 4; ++e) num[e] = any ? num[e] / den : 0.f;
         const float lse = any ? paged_log2_sum<T>(M, den) * kLn2 : -INFINITY;
         if (!all_finite(num) && __builtin_isfinite(den)) {
-            if constexpr (TREE)
-                num = paged_with_odd(num, paged_odd_tree_values<elem, D>(z, q, base, (int)FastDiv::div_by(z.by_g.m, z.by_g.s, (uint32_t)(row0 + n)), p.b,
-                                                                         p.head, k_begin, sm.lim[n], c));
-            else
-                num = paged_with_odd(num, paged_odd_values<elem, D>(z, p.b, p.head, k_begin, sm.lim[n], c));
+            num = paged_with_odd(num, paged_odd_values<elem, D>(z, p.b, p.head, k_begin, sm.lim[n], c));
         }
         const uint32_t t = FastDiv::div_by(z.by_g.m, z.by_g.s, (uint32_t)(row0 + n)), g = (uint32_t)(row0 + n) - t * z.by_g.d;
         const int64_t at = part ? (slot << z.cut.tile_shift) + n : ((int64_t)p.head * z.G + g) * z.T + q.begin + t;

@@ -91,6 +91,7 @@ struct AttnProblem {
 struct FastDiv {
     uint32_t m, s, d;
     FastDiv() = default;
+    __host__ __device__ FastDiv(uint32_t m, uint32_t s, uint32_t d) : m(m), s(s), d(d) {}
     explicit FastDiv(int64_t div) : d((uint32_t)div) {
         s = 31 + (div > 1 ? 64 - (uint32_t)__builtin_clzll((uint64_t)div - 1) : 0);  // + ceil(log2(div))
         m = (uint32_t)((((uint64_t)1 << s) + (uint64_t)div - 1) / (uint64_t)div);
