@@ -9,7 +9,8 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
-from operator import index
+import struct
+from operator import attrgetter, index
 from typing import Optional
 
 import torch  # noqa: F401  (imported before the library so that both share one HIP runtime)
@@ -835,6 +836,17 @@ def fedrag_tree_verify(target, tokens, parents, q_start, u, u_next, draft=None, 
     return kept, n_kept, next_token
 
 
+_size, _strides, _dense = torch.Tensor.size, torch.Tensor.stride, torch.Tensor.is_contiguous
+_address, _index = torch.Tensor.data_ptr, torch.Tensor.get_device
+_dtype = attrgetter("dtype")
+
+
+@functools.lru_cache(maxsize=64)
+def _cache_structs(n) -> struct.Struct:
+    """An array of n fedrag_paged_cache."""
+    return struct.Struct("@" + "PPqqi4x" * n)
+
+
 def fedrag_paged_keep(caches, block_table, q_start, kv_lens, kept, n_kept):
     """Moves the K, V of the rows that stay to the front of each request's rows, in place, in every one of the caches, a list of (K_pages,
     V_pages) of one shape and type but for their numbers of pages.  kept int32 [B, max_kept], rising; n_kept int32 [B]."""
@@ -842,19 +854,28 @@ def fedrag_paged_keep(caches, block_table, q_start, kv_lens, kept, n_kept):
         raise ValueError("caches: a list of (K_pages, V_pages)")
     first, i32 = caches[0][0], torch.int32
     dev, dtype = _device(first), first.dtype
-    structs = (PagedCache * len(caches))()
-    for at, (K_pages, V_pages) in zip(structs, caches):
-        shape = K_pages.shape
-        if V_pages.shape != shape or V_pages.stride() != K_pages.stride() or V_pages.dtype is not dtype or K_pages.dtype is not dtype or \
-                K_pages.get_device() != dev or V_pages.get_device() != dev or shape[1:] != first.shape[1:]:
-            raise ValueError("caches: K_pages and V_pages alike in shape, type, strides and device, and all of them but for n_pages")
-        at.K, at.V, at.n_pages, at.page_stride, at.page_tokens = (K_pages.data_ptr(), V_pages.data_ptr(), shape[0],
-                                                                   _page_stride(shape, K_pages.stride()), shape[2])
+    # All tensors in one sweep of each property (a loop in Python over 32 layers took 40 us, the launch takes 6).
+    K, V = zip(*caches)
+    tensors, n = K + V, len(K)
+    shapes = list(map(_size, tensors))
+    if all(map(_dense, tensors)):
+        page_strides = [0] * n
+    else:
+        strides = list(map(_strides, tensors))
+        page_strides = [_page_stride(*x) for x in zip(shapes, strides[:n])] if strides[:n] == strides[n:] else []
+    if (not page_strides or shapes[:n] != shapes[n:] or (shapes.count(shapes[0]) != 2 * n and any(x[1:] != shapes[0][1:] for x in shapes))
+            or len(shapes[0]) != 4 or set(map(_dtype, tensors)) != {dtype} or set(map(_index, tensors)) != {dev}):
+        raise ValueError("caches: K_pages and V_pages [n_pages, Hkv, page_tokens, d], alike in shape, type, strides and device, and all of them "
+                         "but for n_pages")
+    numbers = [shapes[0][2]] * (5 * n)
+    numbers[0::5], numbers[1::5] = map(_address, K), map(_address, V)
+    numbers[2::5], numbers[3::5] = [x[0] for x in shapes[:n]], page_strides
+    structs = _cache_structs(n).pack(*numbers)
     if block_table.dim() != 2 or kept.dim() != 2:
         raise ValueError("block_table: int32 [B, max_pages], kept: int32 [B, max_kept]")
     (B, columns), (_, H, _, d), most = block_table.shape, first.shape, kept.shape[1]
     st = load().fedrag_paged_keep(
-        _shape_ref(B, H, H, d, dtype), len(caches), structs, _exactly("block_table", block_table, i32, dev, (B, columns)), columns,
+        _shape_ref(B, H, H, d, dtype), len(caches), ctypes.cast(structs, ctypes.POINTER(PagedCache)), _exactly("block_table", block_table, i32, dev, (B, columns)), columns,
         _values("q_start", q_start, i32, dev, B + 1), _exactly("kv_lens", kv_lens, i32, dev, (B,)), _exactly("kept", kept, i32, dev, (B, most)),
         most, _exactly("n_kept", n_kept, i32, dev, (B,)), torch._C._cuda_getCurrentRawStream(dev))
     if st != OK:

@@ -2,6 +2,8 @@
 // Every check below runs before the first HIP call, so the error paths work on a machine without a GPU.
 #include "fedrag_host.h"
 
+#include <algorithm>
+
 using namespace fedrag;
 
 namespace {
@@ -1060,18 +1062,25 @@ fedrag_status fedrag_paged_keep(const fedrag_shape* shape, int32_t n_caches, con
     if (words & 3u) return FEDRAG_ERR_ALIAS;
     const size_t nb = (size_t)shape->batch * 4;
     const Range in[] = {{block_table, (size_t)table}, {q_start, nb + 4}, {kv_lens, nb}, {kept, (size_t)list}, {n_kept, nb}};
-    // K's and V's pages of all caches apart from each other, or in turns in one tensor
+    // K's and V's pages of all caches apart from each other, or in turns in one tensor: by their order in memory, and pair by pair only
+    // those whose extents meet
+    struct Extent {
+        const char* p;
+        size_t n;
+        int cache;
+    } all[2 * FEDRAG_KEEP_CACHES];
     for (int i = 0; i < n_caches; ++i)
-        for (const char* pages : {j.pages[i].K, j.pages[i].V}) {
-            for (const auto& r : in)
+        for (int v = 0; v < 2; ++v) {
+            const char* const pages = v ? j.pages[i].V : j.pages[i].K;
+            for (const Range& r : in)
                 if (overlaps(pages, extent[i], r.p, r.n)) return FEDRAG_ERR_ALIAS;
+            all[2 * i + v] = Extent{extent[i] > 0 ? pages : nullptr, extent[i], i};
         }
+    std::sort(all, all + 2 * n_caches, [](const Extent& x, const Extent& y) { return reinterpret_cast<uintptr_t>(x.p) < reinterpret_cast<uintptr_t>(y.p); });
     for (int i = 0; i < 2 * n_caches; ++i)
-        for (int k = 0; k < i; ++k) {
-            const Pages &x = j.pages[i / 2], &y = j.pages[k / 2];
-            const char *a = i % 2 ? x.V : x.K, *b = k % 2 ? y.V : y.K;
-            if (x.page_bytes == y.page_bytes ? pages_meet(a, extent[i / 2], b, extent[k / 2], x.page_bytes, block[0])
-                                             : overlaps(a, extent[i / 2], b, extent[k / 2]))
+        for (int k = i + 1; k < 2 * n_caches && reinterpret_cast<uintptr_t>(all[k].p) < reinterpret_cast<uintptr_t>(all[i].p) + all[i].n; ++k) {
+            const int64_t x = j.pages[all[i].cache].page_bytes, y = j.pages[all[k].cache].page_bytes;
+            if (x == y ? pages_meet(all[i].p, all[i].n, all[k].p, all[k].n, x, block[0]) : overlaps(all[i].p, all[i].n, all[k].p, all[k].n))
                 return FEDRAG_ERR_ALIAS;
         }
     j.B = shape->batch;

@@ -243,13 +243,14 @@ hipError_t launch_paged_write(const PagedWriteJob& job, hipStream_t stream) {
 // ------------------------------------------------------------------------------------------------ keep
 // Rows of a request move towards its front, in place: row j comes from kept[j] >= j.  Rows are read some at a time and written after
 // all of these have arrived; what the writes cover are rows of the same ones or before (a row that is still to be read, kept[i] for a
-// later i, lies above kept[j] >= j), so that the next ones need not wait.  A workgroup has one head of K or of V of a request in one
-// cache; its threads move 16 bytes of a row each.
+// later i, lies above kept[j] >= j), so that the next ones need not wait.  A workgroup has CH 16-byte chunks of one head's rows, K's
+// or V's, of a request in one cache: the rows of a workgroup follow each other, but its chunks are its own.  The next rows' places are
+// looked up while the rows at hand are on their way.
 struct PagedKeepJob {
     const int32_t *table, *q_start, *kv_lens, *kept, *n_kept;
     int64_t max_pages, max_kept;
-    int B, H, row_bytes, shift, n_caches;
-    FastDiv by_h;
+    int row_bytes, shift;
+    FastDiv by_h, by_splits;
     struct {
         char *K, *V;
         int64_t page_bytes;
@@ -257,49 +258,66 @@ struct PagedKeepJob {
     } cache[FEDRAG_KEEP_CACHES];
 };
 
-template <int THREADS, int CH>  // CH: 16-byte chunks per row
+template <int THREADS, int CH>
 FEDRAG_KERNEL __launch_bounds__(THREADS) void paged_keep_kernel(const PagedKeepJob j) {
     constexpr int kRows = THREADS / CH;  // rows that the workgroup's threads hold one chunk each of
     constexpr int kSteps = 4;
     const int b = (int)j.by_h.div(blockIdx.x), h = (int)(blockIdx.x - (uint32_t)b * j.by_h.d);
-    const auto& cache = j.cache[blockIdx.y];
+    const uint32_t layer = j.by_splits.div(blockIdx.y), split = blockIdx.y - layer * j.by_splits.d;
+    const auto& cache = j.cache[layer];
     char* const pages = blockIdx.z ? cache.V : cache.K;
+    const int64_t page_bytes = cache.page_bytes;
+    const uint32_t n_pages = cache.n_pages;
     const int kv = j.kv_lens[b] < 0 ? 0 : j.kv_lens[b];
     const int64_t n = (int64_t)j.q_start[b + 1] - j.q_start[b], base = kv - n;
     int64_t count = j.n_kept[b] < n ? j.n_kept[b] : n;
     count = count < j.max_kept ? count : j.max_kept;
     const int32_t* const kept = j.kept + b * j.max_kept;
     const int32_t* const table = j.table + b * j.max_pages;
-    const int c = threadIdx.x % CH * 16;
-    auto place = [&](int64_t token) -> char* {  // of a token's row, or null
-        if (token < 0 || token >= kv || token >> j.shift >= j.max_pages) return nullptr;
-        const uint32_t id = (uint32_t)table[token >> j.shift];
-        return id < cache.n_pages ? pages + (int64_t)id * cache.page_bytes + (((int64_t)h << j.shift) + (token & ((1 << j.shift) - 1))) * (CH * 16) + c
-                                  : nullptr;
+    const int64_t c = ((int64_t)h << j.shift) * j.row_bytes + ((int)split * CH + threadIdx.x % CH) * 16;
+    const int row_bytes = j.row_bytes;
+    auto page_of = [&](int64_t token) {  // -1: there is no such token, or no column for it
+        return token >= 0 && token < kv && token >> j.shift < j.max_pages ? table[token >> j.shift] : -1;
     };
-    for (int64_t j0 = 0; j0 < count; j0 += kSteps * kRows) {
-        u32x4_t row[kSteps];
-        char* to[kSteps];
+    auto place = [&](int page, int64_t token) {
+        return (uint32_t)page < n_pages ? pages + (int64_t)page * page_bytes + (token & ((1 << j.shift) - 1)) * row_bytes + c : nullptr;
+    };
+    char *from[kSteps], *to[kSteps];
+    auto look_up = [&](int64_t j0) {  // the places of kSteps * kRows rows from j0 on; null: nothing to move
+        int64_t k[kSteps], i[kSteps];
+        int from_page[kSteps], to_page[kSteps];
 #pragma unroll
         for (int u = 0; u < kSteps; ++u) {
-            const int64_t i = j0 + u * kRows + threadIdx.x / CH;
-            to[u] = nullptr;
-            if (i < count) {
-                const int64_t k = kept[i];
-                if (k > i && k < n) {  // (a row that stays where it is has nothing to do)
-                    const char* from = place(base + k);
-                    if (from) {
-                        to[u] = place(base + i);
-                        row[u] = *(const u32x4_t*)from;
-                    }
-                }
-            }
+            i[u] = j0 + u * kRows + threadIdx.x / CH;
+            k[u] = i[u] < count ? kept[i[u]] : 0;
         }
-        __builtin_amdgcn_s_waitcnt(0x0f70);  // all of the rows are here
+#pragma unroll
+        for (int u = 0; u < kSteps; ++u) {
+            const bool moves = i[u] < count && k[u] > i[u] && k[u] < n;  // (a row that stays where it is has nothing to do)
+            from_page[u] = moves ? page_of(base + k[u]) : -1;
+            to_page[u] = moves ? page_of(base + i[u]) : -1;
+        }
+#pragma unroll
+        for (int u = 0; u < kSteps; ++u) {
+            from[u] = place(from_page[u], base + k[u]);
+            to[u] = from[u] ? place(to_page[u], base + i[u]) : nullptr;
+        }
+    };
+    look_up(0);
+    for (int64_t j0 = 0; j0 < count; j0 += kSteps * kRows) {
+        u32x4_t row[kSteps];
+        char* dest[kSteps];
+#pragma unroll
+        for (int u = 0; u < kSteps; ++u) {
+            dest[u] = to[u];
+            if (to[u]) row[u] = *(const u32x4_t*)from[u];
+        }
+        if (j0 + kSteps * kRows < count) look_up(j0 + kSteps * kRows);
+        __builtin_amdgcn_s_waitcnt(0x0f70);  // this thread's chunks are here, and behind the barrier everybody's
         __syncthreads();
 #pragma unroll
         for (int u = 0; u < kSteps; ++u)
-            if (to[u]) *(u32x4_t*)to[u] = row[u];
+            if (dest[u]) *(u32x4_t*)dest[u] = row[u];
     }
 }
 
@@ -312,11 +330,8 @@ hipError_t launch_paged_keep(const PagedKeep& k, hipStream_t stream) {
     j.n_kept = k.n_kept;
     j.max_pages = k.max_pages;
     j.max_kept = k.max_kept;
-    j.B = k.B;
-    j.H = k.H;
     j.row_bytes = k.D * k.elem_bytes;
     j.shift = k.pages[0].shift;
-    j.n_caches = k.n_caches;
     j.by_h = FastDiv(k.H);
     for (int i = 0; i < k.n_caches; ++i) {
         j.cache[i].K = (char*)k.pages[i].K;
@@ -324,38 +339,51 @@ hipError_t launch_paged_keep(const PagedKeep& k, hipStream_t stream) {
         j.cache[i].page_bytes = k.pages[i].page_bytes;
         j.cache[i].n_pages = k.pages[i].n_pages;
     }
+    // Accepted drafts: a wave for all chunks of a head's rows.  Long lists are a chain of steps, which workgroups of many threads and few
+    // chunks make short: two to a workgroup, or more while there are two workgroups to a compute unit all the same.
     const int chunks = j.row_bytes / 16;
     const bool few = k.max_kept <= 64;
-#define FEDRAG_KEEP(CH) (few ? paged_keep_kernel<64, CH> : paged_keep_kernel<1024, CH>)
-    const auto kernel = chunks == 8 ? FEDRAG_KEEP(8) : chunks == 16 ? FEDRAG_KEEP(16) : FEDRAG_KEEP(32);
-#undef FEDRAG_KEEP
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(k.B * k.H), (unsigned)k.n_caches, 2), dim3(few ? 64 : 1024), 0, stream, j);
+    int each = few ? chunks : 2;
+    while (!few && each < chunks && (int64_t)k.B * k.H * 2 * k.n_caches * (chunks / each) > 2 * attn_target_wgs()) each *= 2;
+    j.by_splits = FastDiv(chunks / each);
+    const auto kernel = few ? (each == 8 ? paged_keep_kernel<64, 8> : each == 16 ? paged_keep_kernel<64, 16> : paged_keep_kernel<64, 32>)
+                            : (each == 2 ? paged_keep_kernel<1024, 2> : each == 4 ? paged_keep_kernel<1024, 4> : each == 8 ? paged_keep_kernel<1024, 8>
+                                         : each == 16 ? paged_keep_kernel<1024, 16> : paged_keep_kernel<1024, 32>);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(k.B * k.H), (unsigned)(k.n_caches * (chunks / each)), 2), dim3(few ? 64 : 1024), 0, stream, j);
     return hipGetLastError();
 }
 
 // ------------------------------------------------------------------------------------------------ trim
-// One workgroup takes the requests 1024 at a time: prefix sums of the columns that each gives back, then these columns side by side, a
-// few in a row to a thread, which counts those that name a page; prefix sums of the counts are the places on the stack.
-constexpr int kTrimEach = 16;  // columns in a row of a thread
+// One workgroup takes the requests 1024 at a time.  Their places on the stack are prefix sums of the pages that each gives back: entries of
+// the table below 0 are none, so that the columns are looked at before any is written.  Up to 1024 columns are a thread's each; more are
+// a wave's request by request, twice (the second time out of L2), the columns of two requests in flight together.
+constexpr int kTrimWaves = kMapThreads / kWave;
+constexpr int kTrimAhead = 4;  // columns of a request that a lane has in flight
 
 FEDRAG_KERNEL __launch_bounds__(kMapThreads) void paged_trim_kernel(PagedTrimJob j, int shift) {
-    __shared__ MapPrefix waves[kMapThreads / kWave];
-    __shared__ uint32_t col_end[kMapThreads];
+    __shared__ MapPrefix waves[kTrimWaves];
+    __shared__ uint32_t col_end[kMapThreads], found[kMapThreads];
     __shared__ int first_col[kMapThreads];
     __shared__ int flags;
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
     const int64_t max_pages = j.max_pages;
     const int count_in = *j.free_count;
     const uint32_t count = count_in < 0 ? 0 : (uint32_t)(count_in < j.n_free ? count_in : j.n_free);
     const uint32_t most = INT_MAX;
     uint32_t top = count;
     if (tid == 0) flags = (uint32_t)count_in == count ? 0 : FEDRAG_TRIM_BAD_LENGTH;
+    auto below = [&](uint64_t lanes) { return (uint32_t)__builtin_popcountll(lanes & (((uint64_t)1 << lane) - 1)); };
+    auto push = [&](uint32_t to, int id) {
+        if (to < j.n_free) j.free_pages[to] = id;
+        else atomicOr(&flags, FEDRAG_TRIM_NO_ROOM);
+    };
     for (int64_t b0 = 0; b0 < j.batch; b0 += kMapThreads) {
         __syncthreads();
         const int64_t b = b0 + tid;
         const int n_req = (int)(j.batch - b0 < kMapThreads ? j.batch - b0 : kMapThreads);
         uint32_t mine = 0;
         first_col[tid] = 0;
+        found[tid] = 0;
         if (b < j.batch) {
             const int kv_in = j.kv_lens[b], kv = kv_in < 0 ? 0 : kv_in;
             int64_t len = j.n_kept[b];
@@ -371,31 +399,74 @@ FEDRAG_KERNEL __launch_bounds__(kMapThreads) void paged_trim_kernel(PagedTrimJob
         }
         MapPrefix total;
         const MapPrefix p = map_scan(MapPrefix{mine, 0}, most, waves, &total);
-        col_end[tid] = p.rows;
+        if (total.rows <= kMapThreads) {
+            col_end[tid] = p.rows;
+            __syncthreads();
+            int id = -1;
+            if ((uint32_t)tid < total.rows) {
+                const int k = first_above(col_end, n_req, tid);
+                id = j.block_table[(b0 + k) * max_pages + first_col[k] + (tid - (k == 0 ? 0 : col_end[k - 1]))];
+            }
+            const uint64_t pages = __builtin_amdgcn_ballot_w64(id >= 0);
+            if (lane == 0) found[wave] = (uint32_t)__builtin_popcountll(pages);
+            __syncthreads();
+            uint32_t before = 0, sum = 0;
+#pragma unroll
+            for (int w = 0; w < kTrimWaves; ++w) {
+                if (w == wave) before = sum;
+                sum += found[w];
+            }
+            if (id >= 0) push(top + before + below(pages), id);
+            top = min(top + sum, (uint32_t)j.n_free);
+            continue;
+        }
+        col_end[tid] = mine;  // (how many, here)
         __syncthreads();
-        for (uint32_t c0 = 0; c0 < total.rows; c0 += kMapThreads * kTrimEach) {
-            uint32_t at = c0 + tid * kTrimEach;
-            const uint32_t end = min(at + kTrimEach, total.rows);
-            int ids[kTrimEach], n = 0;
-            if (at < end) {
-                int k = first_above(col_end, n_req, at);
-                for (; at < end; ++at) {
-                    while (col_end[k] <= at) ++k;
-                    const uint32_t first = k == 0 ? 0 : col_end[k - 1];
-                    const int id = j.block_table[(b0 + k) * max_pages + first_col[k] + (at - first)];
-                    if (id >= 0) ids[n++] = id;
+        // f(request, a lane's entries of it from column c on, one every 64; -1: none)
+        auto each = [&](auto f) {
+            for (int k0 = wave; k0 < n_req; k0 += 2 * kTrimWaves) {
+                const int k1 = k0 + kTrimWaves < n_req ? k0 + kTrimWaves : k0;
+                const uint32_t n0 = col_end[k0], n1 = k1 != k0 ? col_end[k1] : 0;
+                const int32_t* const row0 = j.block_table + (b0 + k0) * max_pages + first_col[k0];
+                const int32_t* const row1 = j.block_table + (b0 + k1) * max_pages + first_col[k1];
+                for (uint32_t c = 0; c < (n0 > n1 ? n0 : n1); c += kTrimAhead * kWave) {
+                    int id[2][kTrimAhead];
+#pragma unroll
+                    for (int u = 0; u < kTrimAhead; ++u) {
+                        const uint32_t at = c + u * kWave + lane;
+                        id[0][u] = at < n0 ? row0[at] : -1;
+                        id[1][u] = at < n1 ? row1[at] : -1;
+                    }
+                    f(k0, id[0]);
+                    if (k1 != k0) f(k1, id[1]);
                 }
             }
-            MapPrefix found;
-            __syncthreads();  // (the waves' sums of before have been read)
-            const MapPrefix q = map_scan(MapPrefix{(uint32_t)n, 0}, most, waves, &found);
-            uint32_t to = top + q.rows - n;
-            for (int i = 0; i < n; ++i, ++to) {
-                if (to < j.n_free) j.free_pages[to] = ids[i];
-                else atomicOr(&flags, FEDRAG_TRIM_NO_ROOM);
+        };
+        each([&](int k, const int (&id)[kTrimAhead]) {
+            uint32_t n = 0;
+#pragma unroll
+            for (int u = 0; u < kTrimAhead; ++u) n += (uint32_t)__builtin_popcountll(__builtin_amdgcn_ballot_w64(id[u] >= 0));
+            if (lane == 0) found[k] += n;
+        });
+        __syncthreads();
+        MapPrefix all;
+        const uint32_t here = found[tid];
+        const MapPrefix q = map_scan(MapPrefix{here, 0}, most, waves, &all);
+        found[tid] = top + (q.rows - here);  // where the request's next page goes
+        __syncthreads();
+        each([&](int k, const int (&id)[kTrimAhead]) {
+            uint32_t to = found[k];
+            wave_lds_fence();  // (all lanes have it)
+#pragma unroll
+            for (int u = 0; u < kTrimAhead; ++u) {
+                const uint64_t pages = __builtin_amdgcn_ballot_w64(id[u] >= 0);
+                if (id[u] >= 0) push(to + below(pages), id[u]);
+                to += (uint32_t)__builtin_popcountll(pages);
             }
-            top = min(top + found.rows, (uint32_t)j.n_free);
-        }
+            if (lane == 0) found[k] = to;
+            wave_lds_fence();
+        });
+        top = min(top + all.rows, (uint32_t)j.n_free);
     }
     __syncthreads();
     if (tid == 0) {

@@ -109,16 +109,13 @@ struct VerifyState {
     int n_kept;
     uint64_t taken;    // C
 };
-struct VerifySums {
-    uint64_t left, all;  // of r, of p
-};
 
-__device__ __forceinline__ float verify_value(float x) { return fminf(fmaxf(x, 0.f), 1.f); }  // (not a number: 0)
+__device__ __forceinline__ float verify_value(float x) { return __builtin_amdgcn_fmed3f(x, 0.f, 1.f); }  // (not a number: 0, the least of the others)
 __device__ __forceinline__ double verify_random(double u) { return fmin(fmax(u, 0.0), 0x1.fffffffffffffp-1); }
-// r in units: adding 2^52 rounds to a whole number, which is then the low bits.
-__device__ __forceinline__ uint64_t verify_units(double r) {
-    return __builtin_bit_cast(uint64_t, __builtin_fma(r, kUnits, 0x1p52)) & (((uint64_t)1 << 52) - 1);
-}
+// r in units, and kUnitsBias: adding 2^52 rounds to a whole number, which is then the low bits.
+constexpr uint64_t kUnitsBias = 0x4330000000000000;
+__device__ __forceinline__ uint64_t verify_units_biased(double r) { return __builtin_bit_cast(uint64_t, __builtin_fma(r, kUnits, 0x1p52)); }
+__device__ __forceinline__ uint64_t verify_units(double r) { return verify_units_biased(r) - kUnitsBias; }
 __device__ __forceinline__ double verify_left(float p, float q, double taken) {
 #pragma clang fp contract(off)
     const double product = taken * (double)q;
@@ -131,6 +128,7 @@ struct Verify {
     int b, s, n, parts;
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     uint64_t (*scratch)[2];  // LDS, a pair for each wave
+    bool target_only = false;  // weights are p's
 
     __device__ __forceinline__ const E* row_p(int node) const { return (const E*)j.target + (int64_t)(s + node) * j.target_stride; }
     __device__ __forceinline__ const E* row_q(int node) const { return (const E*)j.draft + (int64_t)(s + node) * j.draft_stride; }
@@ -238,75 +236,80 @@ struct Verify {
         }
     }
 
-    // ---- sums over the vocabulary
-    __device__ __forceinline__ VerifySums weights(float pv, float qv, double taken) const {
+    // ---- sums over the vocabulary.  Where nothing was rejected, r is p and q is not read.
+    __device__ __forceinline__ bool with_draft(const VerifyState& st) const { return DRAFT && st.taken != 0 && !target_only; }
+    // A token's weight and kUnitsBias.  WITH: 0 r is p, 1 C is one (no product to round), 2 any C.
+    template <int WITH>
+    static __device__ __forceinline__ uint64_t weight(float pv, float qv, double taken) {
         const float x = verify_value(pv);
-        const uint64_t all = verify_units((double)x);
-        return VerifySums{DRAFT ? verify_units(verify_left(x, verify_value(qv), taken)) : all, all};
+        if constexpr (WITH == 0) return verify_units_biased((double)x);
+        if constexpr (WITH == 1) return verify_units_biased(fmax((double)x - (double)verify_value(qv), 0.0));
+        return verify_units_biased(verify_left(x, verify_value(qv), taken));
     }
-    // This thread's share of a part's sums; every token of the part is some thread's.  Where nothing was rejected r is p, and q is not read.
-    __device__ __forceinline__ VerifySums part_sums(const VerifyState& st, int part) const {
-        const E* const pr = row_p(st.node);
-        const E* const qr = DRAFT ? row_q(st.node) : pr;
-        const bool with_q = DRAFT && st.taken != 0;
-        const double taken = (double)st.taken / kUnits;
+    // This thread's share of a part's sum; every token of the part is some thread's.
+    template <int WITH>
+    __device__ __forceinline__ uint64_t part_sum_of(const E* pr, const E* qr, double taken, int part) const {
         const int begin = part * kPart, end = begin + kPart < j.vocab ? begin + kPart : j.vocab;
-        VerifySums sum{0, 0};
-        auto add = [&](float pv, float qv) {
-            const VerifySums w = weights(pv, qv, taken);
-            sum.left += w.left;
-            sum.all += w.all;
-        };
         constexpr int VEC = 16 / (int)sizeof(E);
         typedef E vec __attribute__((ext_vector_type(VEC)));
-        const bool wide = ((reinterpret_cast<uintptr_t>(pr) | (with_q ? reinterpret_cast<uintptr_t>(qr) : 0)) & 15) == 0;
-        if (wide && end - begin == kPart) {
+        uint64_t sum = 0;
+        if (((reinterpret_cast<uintptr_t>(pr) | (WITH ? reinterpret_cast<uintptr_t>(qr) : 0)) & 15) == 0 && end - begin == kPart) {
             vec pv[kEach / VEC], qv[kEach / VEC];
 #pragma unroll
-            for (int i = 0; i < kEach / VEC; ++i) pv[i] = *(const vec*)(pr + begin + (i * kVerifyThreads + (int)threadIdx.x) * VEC);
-            if (with_q) {
-#pragma unroll
-                for (int i = 0; i < kEach / VEC; ++i) qv[i] = *(const vec*)(qr + begin + (i * kVerifyThreads + (int)threadIdx.x) * VEC);
+            for (int i = 0; i < kEach / VEC; ++i) {
+                pv[i] = *(const vec*)(pr + begin + (i * kVerifyThreads + (int)threadIdx.x) * VEC);
+                if constexpr (WITH != 0) qv[i] = *(const vec*)(qr + begin + (i * kVerifyThreads + (int)threadIdx.x) * VEC);
             }
 #pragma unroll
             for (int i = 0; i < kEach / VEC; ++i)
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) add((float)pv[i][e], with_q ? (float)qv[i][e] : 0.f);
-        } else {
-#pragma unroll 4
-            for (int v = begin + (int)threadIdx.x; v < end; v += kVerifyThreads) add((float)pr[v], with_q ? (float)qr[v] : 0.f);
+                for (int e = 0; e < VEC; ++e) sum += weight<WITH>((float)pv[i][e], WITH ? (float)qv[i][e] : 0.f, taken);
+            return sum - kEach * kUnitsBias;
         }
-        return sum;
+        // (single values, as many in flight; what is not there has no weight)
+        E pv[kEach], qv[kEach];
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int v = begin + i * kVerifyThreads + (int)threadIdx.x;
+            pv[i] = v < end ? pr[v] : (E)0.f;
+            if constexpr (WITH != 0) qv[i] = v < end ? qr[v] : (E)0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) sum += weight<WITH>((float)pv[i], WITH ? (float)qv[i] : 0.f, taken);
+        return sum - kEach * kUnitsBias;
+    }
+    __device__ __forceinline__ uint64_t part_sum(const VerifyState& st, int part) const {
+        const E* const pr = row_p(st.node);
+        if constexpr (DRAFT) {
+            if (with_draft(st)) {
+                if (st.taken == kUnit) return part_sum_of<1>(pr, row_q(st.node), 1.0, part);
+                return part_sum_of<2>(pr, row_q(st.node), (double)st.taken / kUnits, part);
+            }
+        }
+        return part_sum_of<0>(pr, pr, 0.0, part);
     }
     static __device__ __forceinline__ uint64_t wave_add(uint64_t x) {
 #pragma unroll
         for (int o = 1; o < kWave; o <<= 1) x += __shfl_xor((unsigned long long)x, o);
         return x;
     }
-    __device__ __forceinline__ VerifySums total(VerifySums x) const {
-        x.left = wave_add(x.left);
-        x.all = wave_add(x.all);
+    __device__ __forceinline__ uint64_t total(uint64_t x) const {
+        x = wave_add(x);
         __syncthreads();
-        if (lane == 0) {
-            scratch[wave][0] = x.left;
-            scratch[wave][1] = x.all;
-        }
+        if (lane == 0) scratch[wave][0] = x;
         __syncthreads();
-        x = VerifySums{0, 0};
+        x = 0;
 #pragma unroll
-        for (int w = 0; w < kVerifyThreads / kWave; ++w) {
-            x.left += scratch[w][0];
-            x.all += scratch[w][1];
-        }
+        for (int w = 0; w < kVerifyThreads / kWave; ++w) x += scratch[w][0];
         return x;
     }
-    // A part's sums, in every thread.
-    __device__ __forceinline__ VerifySums part_total(const VerifyState& st, int part) {
-        VerifySums x = total(part_sums(st, part));
+    // A part's sum, in every thread.
+    __device__ __forceinline__ uint64_t part_total(const VerifyState& st, int part) {
+        uint64_t x = total(part_sum(st, part));
         if constexpr (!DRAFT) {
-            if (st.need == kVerifyDraw)
+            if (!target_only)
                 rejected(st, [&](int child, int v) {
-                    if (v / kPart == part && !repeated(st.node, child, v)) x.left -= verify_units((double)verify_value((float)row_p(st.node)[v]));
+                    if (v / kPart == part && !repeated(st.node, child, v)) x -= verify_units((double)verify_value((float)row_p(st.node)[v]));
                 });
         }
         return x;
@@ -348,34 +351,46 @@ struct Verify {
         *before = scratch[0][0];
         return in * kWave + (int)scratch[0][1];
     }
+    // The sums of all parts, a thread each, by this workgroup alone.
+    __device__ __forceinline__ uint64_t all_parts(const VerifyState& st) {
+        uint64_t mine = 0;
+        for (int i = 0; i < parts; ++i) {
+            const uint64_t x = part_total(st, i);
+            if ((int)threadIdx.x == i) mine = x;
+        }
+        return mine;
+    }
     // The token, from the sums of the parts, a thread each.  only: the workgroup's part, or -1: whichever it is.
-    __device__ __forceinline__ void draw(const VerifyState& st, VerifySums mine, int only) {
-        const VerifySums sum = total(mine);
-        const bool left = sum.left != 0;
-        const uint64_t all = left ? sum.left : sum.all;
-        if (all == 0) {
-            if (only <= 0 && threadIdx.x == 0) j.next_token[b] = -1;
-            return;
+    __device__ __forceinline__ void draw(const VerifyState& st, uint64_t mine, int only) {
+        uint64_t all = total(mine);
+        if (all == 0) {  // nothing is left of r: p, by one workgroup
+            if (only > 0) return;
+            only = -1;
+            target_only = true;
+            mine = all_parts(st);
+            all = total(mine);
+            if (all == 0) {
+                if (threadIdx.x == 0) j.next_token[b] = -1;
+                return;
+            }
         }
         const double x = verify_random(j.u_next[b]) * (double)all;
         uint64_t t = (uint64_t)x;
         t = t < all ? t : all - 1;
         uint64_t before;
-        const int part = first_beyond(left ? mine.left : mine.all, t, &before);
+        const int part = first_beyond(mine, t, &before);
         if (only >= 0 && part != only) return;
         const E* const pr = row_p(st.node);
         const E* const qr = DRAFT ? row_q(st.node) : pr;
-        const double taken = (double)st.taken / kUnits;
+        const bool with = with_draft(st);
+        const double taken = with ? (double)st.taken / kUnits : 0.0;  // (of p with q = 0: p)
         const int v0 = part * kPart + (int)threadIdx.x * kEach;
         uint64_t w[kEach], here = 0;
 #pragma unroll
-        for (int e = 0; e < kEach; ++e) {
-            VerifySums x{0, 0};
-            if (v0 + e < j.vocab) x = weights((float)pr[v0 + e], DRAFT && st.taken != 0 ? (float)qr[v0 + e] : 0.f, taken);
-            w[e] = left ? x.left : x.all;
-        }
+        for (int e = 0; e < kEach; ++e)
+            w[e] = v0 + e < j.vocab ? weight<2>((float)pr[v0 + e], with ? (float)qr[v0 + e] : 0.f, taken) - kUnitsBias : 0;
         if constexpr (!DRAFT) {
-            if (left)
+            if (!target_only)
                 rejected(st, [&](int, int v) {
 #pragma unroll
                     for (int e = 0; e < kEach; ++e) w[e] = v0 + e == v ? 0 : w[e];
@@ -404,7 +419,7 @@ FEDRAG_KERNEL __launch_bounds__(kVerifyThreads) void tree_verify_kernel(TreeVeri
     __shared__ uint64_t scratch[kVerifyThreads / kWave][2];
     const int part = (int)blockIdx.x, b = (int)blockIdx.y;
     VerifyState* const states = (VerifyState*)j.workspace;  // [2][batch], then the sums [2][batch][parts]
-    VerifySums* const sums = (VerifySums*)(states + 2 * (int64_t)j.batch);
+    uint64_t* const sums = (uint64_t*)(states + 2 * (int64_t)j.batch);
     const int now = round & 1, before = 1 - now;
     const int s = clamped(j.q_start[b], 0, j.n_rows), e = clamped(j.q_start[b + 1], 0, j.n_rows);
     Verify<E, DRAFT> v{j, b, s, e > s ? e - s : 0, parts};
@@ -413,7 +428,7 @@ FEDRAG_KERNEL __launch_bounds__(kVerifyThreads) void tree_verify_kernel(TreeVeri
     VerifyState st{kVerifyDone, 0, 0, 1, 0};
     auto own_sum = [&]() {
         const int t = threadIdx.x;
-        return t < parts ? sums[((int64_t)before * j.batch + b) * parts + t] : VerifySums{0, 0};
+        return t < parts ? sums[((int64_t)before * j.batch + b) * parts + t] : 0;
     };
     if (round == 0) {
         if (v.n > 0) {
@@ -432,8 +447,7 @@ FEDRAG_KERNEL __launch_bounds__(kVerifyThreads) void tree_verify_kernel(TreeVeri
             v.draw(st, own_sum(), part);
             st.need = kVerifyDone;
         } else if (st.need == kVerifyMass) {
-            const VerifySums sum = v.total(own_sum());
-            v.walk(st, sum.left, part == 0);
+            v.walk(st, v.total(own_sum()), part == 0);
         }
     }
     auto finish_kept = [&]() {  // the path is complete
@@ -445,35 +459,29 @@ FEDRAG_KERNEL __launch_bounds__(kVerifyThreads) void tree_verify_kernel(TreeVeri
         if (part == 0 && threadIdx.x == 0) states[(int64_t)now * j.batch + b] = st;
         if (st.need == kVerifyDone) return;
         if (st.need == kVerifyDraw) finish_kept();
-        const VerifySums sum = v.part_total(st, part);
+        const uint64_t sum = v.part_total(st, part);
         if (threadIdx.x == 0) sums[((int64_t)now * j.batch + b) * parts + part] = sum;
         return;
     }
     if (st.need == kVerifyDone || part != 0) return;
     while (st.need == kVerifyMass) {  // (each time around a child has been tried)
-        VerifySums sum{0, 0};
-        for (int i = 0; i < parts; ++i) sum.left += v.part_sums(st, i).left;
-        sum = v.total(sum);
-        v.walk(st, sum.left, true);
+        uint64_t sum = 0;
+        for (int i = 0; i < parts; ++i) sum += v.part_sum(st, i);
+        v.walk(st, v.total(sum), true);
     }
     finish_kept();
-    VerifySums mine{0, 0};
-    for (int i = 0; i < parts; ++i) {
-        const VerifySums sum = v.part_total(st, i);
-        if ((int)threadIdx.x == i) mine = sum;
-    }
-    v.draw(st, mine, -1);
+    v.draw(st, v.all_parts(st), -1);
 }
 
 static int verify_parts(int vocab) { return (vocab + kPart - 1) / kPart; }
 size_t tree_verify_workspace(int batch, int vocab) {
-    return 2 * (size_t)batch * (sizeof(VerifyState) + (size_t)verify_parts(vocab) * sizeof(VerifySums));
+    return 2 * (size_t)batch * (sizeof(VerifyState) + (size_t)verify_parts(vocab) * sizeof(uint64_t));
 }
 
 template <class E>
 static hipError_t launch_tree_verify_t(const TreeVerifyJob& job, hipStream_t stream) {
     const int parts = verify_parts(job.vocab);
-    const int last = job.draft ? 3 : 1;
+    const int last = !job.draft ? 1 : job.batch < 4 ? 2 : job.batch < 32 ? 3 : 4;
     const auto kernel = job.draft ? tree_verify_kernel<E, true> : tree_verify_kernel<E, false>;
     for (int round = 0; round <= last; ++round)
         hipLaunchKernelGGL(kernel, dim3((unsigned)parts, (unsigned)job.batch), dim3(kVerifyThreads), 0, stream, job, parts, round, last);
