@@ -277,13 +277,15 @@ __device__ __forceinline__ void tree_body(const PagedArgs& a, uint32_t wg, Slots
         bool odd = false;
         if constexpr (masked) {
             bool bad = false;
-#pragma unroll 1
-            for (int t = 0; t < DCH; ++t) {
-                const u32x4_t vt = vop_of(t);
+            if (key0 + kDecTile > shared) {
+#pragma unroll 4
+                for (int t = 0; t < DCH; ++t) {
+                    const u32x4_t vt = vop_of(t);
 #pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    const bool lo = (vt[w] & kExp) == kExp, up = (vt[w] >> 16 & kExp) == kExp;
-                    bad |= lo || up;
+                    for (int w = 0; w < 4; ++w) {
+                        const bool lo = (vt[w] & kExp) == kExp, up = (vt[w] >> 16 & kExp) == kExp;
+                        bad |= lo || up;
+                    }
                 }
             }
             odd = __builtin_amdgcn_ballot_w64(bad) != 0;
