@@ -206,7 +206,13 @@ static PagedPlan paged_plan(int B, int Hq, int Hkv, int dtype, int64_t T, int64_
         p.runs = paged_runs(PagedCut{tile, 6, 4 * t < full ? 1 : 2 * t < full ? 2 : 4, cus + 1, 0, 1, INT32_MAX}, t, keys);
         return p;
     }
-    if (tree && most * G <= 64) {
+    // Rows with masks: up to 32 a workgroup has them all, and the keys are read at the rate of the memory.  For 33 to 64 two workgroups share them, if
+    // (nearly) all requests have so many: 16 tokens of 32 heads of 128 each over 1000 to 32768 keys 276 us, 308 by the form for many rows; 200 to 2000 67 and
+    // 69; one request over 1000 15.2 and 17.8, over 8000 28.8 and 27.7.  Beside requests of fewer rows the forms for many and for few in one launch are
+    // ahead, the one bound by the matrix pipe, the other by the memory: 16 tokens for every other request, 1 else, 232 us and 289; 16 and 8 93 and
+    // 102; 1 beside 31 of one token 222 and 264.  (128 rows by four workgroups on the same keys: 371 us where the form for many takes 294.)
+    const bool alike = 8 * T > 7 * (int64_t)B * most;
+    if (tree && (most * G <= 32 || (most * G <= 64 && alike))) {
         const int tile = !many ? 4 : most * G <= 32 ? 5 : 6;
         p.shares = paged_shares(PagedCut{tile, 8, 1, tile == 6 ? cus : cus + 1, 1, 1, INT32_MAX}, tiles(tile), keys);
         return p;

@@ -11,7 +11,8 @@
 //   which are also its contraction slice of O^T (d x 16) += V^T (d x 32) . P^T (32 x 16), whose V^T operands come through
 //   the transposing LDS read.  An operand of K or V is read once for all of a wave's rows.
 // Probabilities enter the second product as two storage-type terms (about 16 significant bits): outputs are fp32.  They are relative to
-// the largest score of some tile before, which is replaced, and the outputs rescaled, only by one that is kTreeSlack above it.
+// the largest score so far, whose own probability is a power of two and exact; outputs are rescaled only where it moves.  (Leaving it
+// until it is 2^8 off takes 1 % off the time and doubles the error of rows whose weight sits on few tokens.)
 // Only the key tiles that hold drafted tokens are masked, by bits of the rows' words.
 #pragma once
 #include "attn_paged.h"
@@ -19,12 +20,6 @@
 namespace fedrag {
 
 constexpr int kTreeWaves = 4;
-
-// How far (in units of a factor of two) a score may lie above what probabilities are relative to.  bf16: they have fp32's range, and 2^8
-// is no matter to the sums.  fp16: paged_reference puts them up to 2^15, and its largest number is 65504 = 2^15.999; the quarter that is left is for
-// the last places of scores of up to 2^20.
-template <class T>
-constexpr float kTreeSlack = std::is_same<T, F16>::value ? 0.75f : 8.0f;
 
 // What a workgroup has in LDS beside its tiles of K and of V, which are arrays of the kernel (one for every two waves' slots, so that a
 // launch can share them with the form for many rows): the waves' maxima and sums of the rows, the rows' first words, and the requests
@@ -229,7 +224,7 @@ __device__ __forceinline__ void tree_body(const PagedArgs& a, uint32_t wg, Slots
             for (int e = 1; e < 8; ++e) mx = fmaxf(mx, s[g][e / 4][e % 4]);
             mx = xor32_max(xor16_max(mx));
             const float top = paged_reference<T>(mx * scale_log2);
-            if (__builtin_amdgcn_ballot_w64(top > m_run[g] + kTreeSlack<T>) != 0) {
+            if (__builtin_amdgcn_ballot_w64(top > m_run[g]) != 0) {
                 const float m_new = fmaxf(m_run[g], top);
                 const float alpha = fast_exp2(m_run[g] - m_new);
                 l_run[g] *= alpha;
