@@ -322,7 +322,8 @@ struct PagedShares {
         extra = lane_value(lanes.extra, 0);
         share = (uint32_t)(((uint64_t)total + ((uint64_t)1 << a.cut.target_shift) - 1) >> a.cut.target_shift);
         share = share > (uint32_t)a.cut.least ? share : (uint32_t)a.cut.least;
-        whole = share / 8 > (uint32_t)a.cut.least ? share / 8 : (uint32_t)a.cut.least;
+        // (its own units: where no request has more than `least`, the host has set no partials aside)
+        whole = (share / 8 > (uint32_t)a.cut.least ? share / 8 : (uint32_t)a.cut.least) + extra;
     }
     // The tile that unit `pos` belongs to.
     __device__ __forceinline__ PagedSpan find(Args& a, uint32_t pos) const {

@@ -153,11 +153,11 @@ struct PagedLaunch {
 constexpr int kPagedDecodeRows = 16;  // a tile of the kernel for few rows
 
 // tiles: at least the tiles of all requests and heads; keys: at most a request's.
-static int64_t paged_units_of(PagedCut& cut, int64_t tiles, int64_t keys) {
+static int64_t paged_units_of(PagedCut& cut, int64_t tiles, int64_t keys, int extra = 0) {
     int64_t units = 1;
     do {
         units = keys > 0 ? ((keys - 1) >> cut.unit_shift) + 1 : 1;
-    } while (tiles > INT32_MAX / (units + cut.gain) && ++cut.unit_shift < 31);
+    } while (tiles > INT32_MAX / (units + extra) && ++cut.unit_shift < 31);
     return units;
 }
 static PagedLaunch paged_runs(PagedCut cut, int64_t tiles, int64_t keys) {
@@ -173,7 +173,7 @@ static PagedLaunch paged_runs(PagedCut cut, int64_t tiles, int64_t keys) {
 }
 static PagedLaunch paged_shares(PagedCut cut, int64_t tiles, int64_t keys) {
     const int64_t target = (int64_t)1 << cut.target_shift;
-    const int64_t units = paged_units_of(cut, tiles, keys);
+    const int64_t units = paged_units_of(cut, tiles, keys, cut.gain);
     const int64_t total = tiles * units;
     PagedLaunch l{};
     l.cut = cut;

@@ -6,7 +6,8 @@ namespace fedrag {
 
 // Requests of at most 16 NQ SUBS rows.
 template <class T, int D, int NQ, int SUBS>
-FEDRAG_KERNEL __launch_bounds__(kTreeWaves * kWave, 2) void tree_16_kernel(const PagedArgs a) {
+FEDRAG_KERNEL __launch_bounds__(kTreeWaves * kWave, 2) void tree_16_kernel(const PagedArgs a, uint32_t shares) {
+    if (SUBS > 1 && tree_index<SUBS>(blockIdx.x).share >= shares) return;  // (what makes the grid a whole number of XCDs)
     constexpr int SLOT = kDecTile * D * 2;
     __shared__ __attribute__((aligned(16))) char ks[kTreeWaves * SLOT], vs[kTreeWaves * SLOT];
     __shared__ TreeSmall<NQ> sm;
@@ -49,7 +50,7 @@ static hipError_t launch_tree_16_t(const PagedArgs& a, int64_t many, const Paged
     } else {
         const auto kernel = d.cut.tile_shift == 4 ? tree_16_kernel<T, D, 1, 1> : d.cut.tile_shift == 5 ? tree_16_kernel<T, D, 2, 1> : tree_16_kernel<T, D, 2, 2>;
         const int64_t grid = d.cut.tile_shift == 6 ? (few + 7) / 8 * 16 : few;  // (tree_index)
-        hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(kTreeWaves * kWave), 0, stream, d);
+        hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(kTreeWaves * kWave), 0, stream, d, (uint32_t)few);
     }
     return hipGetLastError();
 }

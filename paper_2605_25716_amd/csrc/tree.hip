@@ -129,6 +129,7 @@ struct Verify {
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     uint64_t (*scratch)[2];  // LDS, a pair for each wave
     bool target_only = false;  // weights are p's
+    double next = 0.0;         // the request's u_next
 
     __device__ __forceinline__ const E* row_p(int node) const { return (const E*)j.target + (int64_t)(s + node) * j.target_stride; }
     __device__ __forceinline__ const E* row_q(int node) const { return (const E*)j.draft + (int64_t)(s + node) * j.draft_stride; }
@@ -374,7 +375,7 @@ struct Verify {
                 return;
             }
         }
-        const double x = verify_random(j.u_next[b]) * (double)all;
+        const double x = next * (double)all;
         uint64_t t = (uint64_t)x;
         t = t < all ? t : all - 1;
         uint64_t before;
@@ -426,10 +427,14 @@ FEDRAG_KERNEL __launch_bounds__(kVerifyThreads) void tree_verify_kernel(TreeVeri
     v.scratch = scratch;
     v.at = -1;
     VerifyState st{kVerifyDone, 0, 0, 1, 0};
-    auto own_sum = [&]() {
-        const int t = threadIdx.x;
-        return t < parts ? sums[((int64_t)before * j.batch + b) * parts + t] : 0;
-    };
+    // (what the round may need of the one before, in one trip to memory)
+    uint64_t own_sum = 0;
+    v.next = verify_random(j.u_next[b]);
+    if (round > 0) {
+        st = states[(int64_t)before * j.batch + b];
+        if ((int)threadIdx.x < parts) own_sum = sums[((int64_t)before * j.batch + b) * parts + threadIdx.x];
+        pin_here(own_sum);
+    }
     if (round == 0) {
         if (v.n > 0) {
             if (part == 0 && threadIdx.x == 0) j.kept[b * j.max_kept] = 0;
@@ -442,12 +447,11 @@ FEDRAG_KERNEL __launch_bounds__(kVerifyThreads) void tree_verify_kernel(TreeVeri
             }
         }
     } else {
-        st = states[(int64_t)before * j.batch + b];
         if (st.need == kVerifyDraw) {
-            v.draw(st, own_sum(), part);
+            v.draw(st, own_sum, part);
             st.need = kVerifyDone;
         } else if (st.need == kVerifyMass) {
-            v.walk(st, v.total(own_sum()), part == 0);
+            v.walk(st, v.total(own_sum), part == 0);
         }
     }
     auto finish_kept = [&]() {  // the path is complete

@@ -519,3 +519,22 @@ def test_trim_out_of_the_ordinary(what):
     _trim(kv, kept, table, free, count, page)
     if what == "lengths":
         _trim(kv, kept, table, free, count, page, TR.starts(rng.integers(0, 50, B)))
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("n,G", [(1, 4), (3, 8), (6, 8)])
+def test_many_short_requests(dt, n, G):
+    """So many requests that shares hold several tiles each, none of them long enough to be cut: no partials are set aside (a table of
+    256 tokens), and none are written."""
+    B, Hkv = 900, 2
+    rng = np.random.default_rng(n)
+    kv = [n + int(rng.integers(0, 200)) for _ in range(B)]
+    c = _attn_case([n] * B, kv, Hkv * G, Hkv, 64, 32, dt, seed=n)
+    c["table"] = np.concatenate([c["table"], np.full((B, 8), -1)], 1)[:, :8]
+    if dt != "f32":
+        assert fb.fedrag_paged_tree_attn_workspace_bytes(B, Hkv * G, Hkv, 64, DT[dt], n * B, 8, 32, n) == 0
+    O, lse = _attn(c, check=False)
+    pick = sorted(rng.choice(B, 12, replace=False))
+    rows = np.concatenate([np.arange(c["start"][b], c["start"][b + 1]) for b in pick])
+    ref = TR.attn_ref(c["Q"][:, rows], c["Kp"], c["Vp"], c["table"][pick], n * np.arange(13), [kv[b] for b in pick], c["mask"][rows], 64 ** -0.5)
+    R.check_attn(O[:, :, rows], lse[:, :, rows], ref, FILL)
