@@ -538,3 +538,52 @@ def test_many_short_requests(dt, n, G):
     rows = np.concatenate([np.arange(c["start"][b], c["start"][b + 1]) for b in pick])
     ref = TR.attn_ref(c["Q"][:, rows], c["Kp"], c["Vp"], c["table"][pick], n * np.arange(13), [kv[b] for b in pick], c["mask"][rows], 64 ** -0.5)
     R.check_attn(O[:, :, rows], lse[:, :, rows], ref, FILL)
+
+
+def test_pages_beyond_4_gib():
+    """Attention, and rows moved, in pages whose bytes are numbered beyond 2^32."""
+    H, page, d, n = 8, 256, 128, 9000
+    K, V = (torch.zeros((n, H, page, d), dtype=torch.bfloat16, device=DEV) for _ in range(2))  # 4.7 GB each
+    table = np.array([[8999, 3, 8500, 8998]])
+    g = torch.Generator().manual_seed(1)
+    small = [torch.randn((4, H, page, d), generator=g).to(torch.bfloat16) for _ in range(2)]
+    for big, x in zip((K, V), small):
+        big[torch.tensor(table[0]).to(DEV)] = x.to(DEV)
+    Q, up = torch.randn((8, 9, d), generator=g).to(torch.bfloat16), TR.trees(np.random.default_rng(1), [9])
+    mask = TR.signed(TR.map_ref(up, [0, 9], [1000], 1, 9)[0])
+    O, lse = fb.fedrag_paged_tree_attn(Q.to(DEV), K, V, i32(table), i32([0, 9]), i32([1000]), torch.from_numpy(mask).to(DEV), 9)
+    R.check_attn(O, lse, TR.attn_ref(Q, *small, np.arange(4)[None], [0, 9], [1000], mask, d ** -0.5), FILL)
+    kept = np.array([[0, 2, 5, 6, 8]])
+    fb.fedrag_paged_keep([(K, V)], i32(table), i32([0, 9]), i32([1000]), i32(kept), i32([5]))
+    for big, x in zip((K, V), small):
+        want = TR.keep_ref(x, np.arange(4)[None], [0, 9], [1000], kept, [5])
+        assert torch.equal(_bits(big[torch.tensor(table[0]).to(DEV)].cpu()), _bits(want))
+        assert not big[4:8400].any()
+
+
+def test_refusals_of_tensors():
+    """What the binding finds wrong with tensors on the device."""
+    i, f = torch.zeros(4, dtype=torch.int32, device=DEV), torch.zeros(4, dtype=torch.float64, device=DEV)
+    pages, p = torch.zeros((3, 1, 16, 64), device=DEV), torch.ones((4, 10), device=DEV)
+    table, kept, mask = i.view(2, 2), i.view(2, 2), torch.zeros((4, 1), dtype=torch.int64, device=DEV)
+    Q = torch.zeros((1, 4, 64), device=DEV)
+    attn = lambda **kw: fb.fedrag_paged_tree_attn(*{**dict(Q=Q, K=pages, V=pages.clone(), t=table, s=i[:3], kv=i[:2], m=mask), **kw}.values())  # noqa: E731
+    attn()
+    verify = lambda **kw: fb.fedrag_tree_verify(**{**dict(target=p, tokens=i, parents=i, q_start=i[:2], u=f, u_next=f[:1]), **kw})  # noqa: E731
+    verify()
+    for call in (lambda: attn(m=mask[:3]), lambda: attn(m=mask.int()), lambda: attn(m=mask[:, 0]), lambda: attn(Q=Q.half()), lambda: attn(s=i[:2]),
+                 lambda: attn(t=i), lambda: attn(K=pages.expand(3, 1, 16, 64)[:1].expand(3, 1, 16, 64)), lambda: verify(u=f.float()),
+                 lambda: verify(draft=p.half()), lambda: verify(draft=p[:3]), lambda: verify(target=p.double()), lambda: verify(tokens=i[:3]),
+                 lambda: verify(target=p.t().contiguous().t()), lambda: verify(target=p[:1].expand(4, 10)), lambda: verify(kept=kept, max_kept=3),
+                 lambda: fb.fedrag_tree_map(i, i[:3], i[:2], 0), lambda: fb.fedrag_tree_map(i.long(), i[:3], i[:2], 1),
+                 lambda: fb.fedrag_tree_map(i, i[:2], i[:2], 1), lambda: fb.fedrag_paged_keep([(pages, pages.half())], table, i[:3], i[:2], kept, i[:2]),
+                 lambda: fb.fedrag_paged_keep([(pages, pages.clone()), (pages[:, :, :, :32], pages[:, :, :, :32])], table, i[:3], i[:2], kept, i[:2]),
+                 lambda: fb.fedrag_paged_keep([(pages, pages.clone(), pages)], table, i[:3], i[:2], kept, i[:2]),
+                 lambda: fb.fedrag_paged_keep([(pages, pages.clone())], table, i[:3], i[:2], kept, i[:3]),
+                 lambda: fb.fedrag_paged_trim(i[:2], i[:2], table, i.long(), i[:1], 16), lambda: fb.fedrag_paged_trim(i[:2], i[:3], table, i, i[:1], 16)):
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: fb.fedrag_paged_keep([(pages, pages)], table, i[:3], i[:2], kept, i[:2]), lambda: fb.fedrag_tree_map(i, i[:3], i[:2], 65),
+                 lambda: fb.fedrag_paged_trim(i[:2], i[:2], table, i, i[:1], 24)):
+        with pytest.raises(fb.FedragError):
+            call()

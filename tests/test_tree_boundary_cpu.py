@@ -204,3 +204,15 @@ def test_binding_refuses_host_tensors():
                  lambda: fb.fedrag_paged_trim(i, i, i.view(2, 2), i, i, 16), lambda: fb.fedrag_paged_keep([], i, i, i, i, i)):
         with pytest.raises(ValueError):
             call()
+
+
+def test_attn_workspace_has_a_bound(lib):
+    """What a caller may set aside once for all its calls: 1024 partials of 128 rows of d + 1 numbers, and 512 of 32 rows."""
+    assert (1024 * 128 + 512 * 32) * 129 * 4 <= 73 * 2 ** 20
+    for B, T in [(B, T) for B in (1, 7, 64, 1000) for T in (1, 3, 17, 64, 300, 1000, 5000, 70000)]:
+        for Hkv, G in ((1, 1), (1, 16), (8, 4), (33, 2)):
+            for d, dtype in ((64, fb.F32), (128, fb.F32), (128, fb.BF16)):
+                for columns in (1, 9, 100, 3000, 40000):
+                    for max_q in (0, 1, 5, 12, T):
+                        need = lib.fedrag_paged_tree_attn_workspace_bytes(shape(B=B, Hq=G * Hkv, Hkv=Hkv, d=d, dt=dtype), T, columns, 16, max_q)
+                        assert need <= 73 * 2 ** 20, (B, T, Hkv, G, d, dtype, columns, max_q)
