@@ -121,6 +121,11 @@ template <int CTRL>
 __device__ __forceinline__ float dpp_move(float x) {
     return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
 }
+template <int CTRL>
+__device__ __forceinline__ uint64_t dpp_move64(uint64_t x) {
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)x, CTRL, 0xf, 0xf, true);
+    return (uint64_t)(uint32_t)__builtin_amdgcn_update_dpp(0, (int)(x >> 32), CTRL, 0xf, 0xf, true) << 32 | lo;
+}
 template <int N, class Op>
 __device__ __forceinline__ float group_reduce(float x, Op op) {
     static_assert(N == 8 || N == 16, "groups of 8 or 16 lanes");

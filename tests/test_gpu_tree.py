@@ -263,7 +263,7 @@ def test_verify(dt, with_draft, V):
 @pytest.mark.parametrize("with_draft", [True, False])
 def test_verify_many_siblings_rejected(with_draft):
     """Random numbers near one: one child after the other is rejected, many more than there are rounds; the sums go on and on."""
-    for V in (40, 5000):
+    for V in (40, 5000, 33000):
         c = _verify_case([30, 80, 9, 2], V, "f32", 3, noise=3.0, with_draft=with_draft)
         c[3] = TR.trees(np.random.default_rng(1), [30, 80, 9, 2], "star")
         c[5] = 1.0 - 1e-9 * np.random.default_rng(2).random(121)
@@ -279,12 +279,24 @@ def test_verify_many_siblings_rejected(with_draft):
 def test_verify_a_vocabulary_of_many_parts(dt):
     for with_draft in (True, False):
         _verify(*_verify_case([9, 5, 17], 50021, dt, 11, with_draft=with_draft), 6)
+        for sizes, most in (([1], 1), ([6, 1, 0, 12], 12), ([70, 3, 100], 40)):
+            _verify(*_verify_case(sizes, 70001, dt, len(sizes), with_draft=with_draft), most)
+
+
+@pytest.mark.parametrize("dt, V", [("f32", 32768), ("f32", 32769), ("f32", 32765), ("f32", 3), ("f32", 4), ("f32", 5), ("f32", 28673), ("bf16", 65536),
+                                   ("bf16", 65537), ("bf16", 65529), ("f16", 7), ("f16", 8), ("f16", 11), ("f16", 57351)])
+def test_verify_where_the_forms_meet(dt, V):
+    """Rows that fill one workgroup's registers, or one of its steps, by a token more or less; fewer tokens than a load has."""
+    for with_draft in (True, False):
+        c = _verify_case([12, 0, 7, 25, 1, 1, 1, 1], V, dt, V, with_draft=with_draft, spread=0.1)
+        c[6][:] = [0.0, 0.1, np.nextafter(1.0, 0.0), 0.5, 0.9, 0.99, 0.999, 0.99999]
+        _verify(*c, 9)
 
 
 @pytest.mark.parametrize("with_draft", [True, False])
 @pytest.mark.parametrize("what", ["extremes", "outside", "nan_u"])
 def test_verify_random_numbers_at_their_ends(with_draft, what):
-    for V in (3, 4500):
+    for V in (3, 4500, 33333):
         c = _verify_case([8] * 6, V, "f32", 5, with_draft=with_draft)
         ends = {"extremes": [0.0, np.nextafter(1.0, 0.0)], "outside": [-1.0, 1.0, 7.0, -np.inf, np.inf], "nan_u": [np.nan, 0.5]}[what]
         rng = np.random.default_rng(2)
@@ -295,13 +307,12 @@ def test_verify_random_numbers_at_their_ends(with_draft, what):
 @pytest.mark.parametrize("dt", ["f32", "f16"])
 def test_verify_values_at_their_ends(dt):
     """Rows of zeros, of one token, equal rows, values that are no probabilities; tokens and parents that are none."""
-    V = 4300
-    for with_draft in (True, False):
+    for V, with_draft in ((4300, True), (4300, False), (70003, True), (70003, False)):
         c = _verify_case([10] * 12, V, dt, 8, with_draft=with_draft)
         t, q = c[0], c[1]
         t[0:10] = 0
         t[10:20] = 0
-        t[10:20, 4299] = 1
+        t[10:20, V - 1] = 1
         t[20:30] = 1.0
         t[30:40, ::3] = float("nan")
         t[40:50, 7] = float("inf")
@@ -321,12 +332,13 @@ def test_verify_values_at_their_ends(dt):
 def test_verify_rows_with_strides():
     for dt in ("f32", "bf16"):
         for shift in (0, 1, 3):
-            target, draft, *c = _verify_case([6, 9, 4], 9001, dt, 4)
-            wide = torch.zeros((19, 9100), dtype=DT[dt], device=DEV)
-            wide[:, shift:shift + 9001] = target.to(DEV)
-            far = torch.zeros((19, 9001 + 16), dtype=DT[dt], device=DEV)
-            far[:, :9001] = draft.to(DEV)
-            _verify(wide[:, shift:shift + 9001], far[:, :9001], *c, 9)
+            for V in (9001, 70001):
+                target, draft, *c = _verify_case([6, 9, 4], V, dt, 4)
+                wide = torch.zeros((19, V + 99), dtype=DT[dt], device=DEV)
+                wide[:, shift:shift + V] = target.to(DEV)
+                far = torch.zeros((19, V + 16), dtype=DT[dt], device=DEV)
+                far[:, :V] = draft.to(DEV)
+                _verify(wide[:, shift:shift + V], far[:, :V], *c, 9)
 
 
 def test_verify_offsets_beyond_32_bits():

@@ -15,6 +15,6 @@ def test_residency_that_attention_by_masks_is_cut_for(kernels):  # noqa: F811
 def test_a_wave_has_its_registers(kernels):  # noqa: F811
     """Verification: eight workgroups of four waves to a compute unit would need 64 registers, four have 128."""
     found = [k for n, k in kernels.items() if "tree_verify_kernel" in n]
-    assert len(found) == 6
+    assert len(found) == 6, found
     for k in found:
         assert workgroups_per_unit(k) >= 4
