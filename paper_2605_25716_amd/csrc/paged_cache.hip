@@ -241,12 +241,13 @@ hipError_t launch_paged_write(const PagedWriteJob& job, hipStream_t stream) {
 }
 
 // ------------------------------------------------------------------------------------------------ keep
-// Rows of a request move towards its front, in place: row j comes from kept[j] >= j.  Rows are read some at a time and written after
-// all of these have arrived; what the writes cover are rows of the same ones or before (a row that is still to be read, kept[i] for a
-// later i, lies above kept[j] >= j), so that the next ones need not wait.  A workgroup has CH 16-byte chunks of one head's rows, K's
-// or V's, of a request in one cache: the rows of a workgroup follow each other, but its chunks are its own.  The next rows' places are
-// looked up while the rows at hand are on their way.  Bound for accepted drafts by its chain of trips (lengths, list, table, rows: 16
-// requests in 32 layers 6.1 us), for long lists by the addresses of a workgroup's loads, which are a lane's each for 16 bytes.
+// Rows of a request move towards its front, in place: row j comes from kept[j] >= j.  A round's rows are read and have arrived before any
+// of them is written; what the writes cover are rows of the same round or before (a row that is still to be read, kept[i] for a later i,
+// lies above kept[j] >= j), so that the next round's can be on their way by then.  A workgroup has CH 16-byte chunks of one head's rows,
+// K's or V's, of a request in one cache: its rounds follow each other, but its chunks are its own.  Bound for accepted drafts by its chain
+// of trips (lengths, list, table, rows: 16 requests in 32 layers 6.4 us), for long lists by the addresses of a workgroup's loads and
+// stores, a lane's each for 16 bytes: 4096 rows a round of 9 us (20001 of 32768 tokens of 8 heads of 64 in fp16 43 us, 1.9 TB/s; 51 with
+// the next round's rows asked for after this one's are written).
 struct PagedKeepJob {
     const int32_t *table, *q_start, *kv_lens, *kept, *n_kept;
     int64_t max_pages, max_kept;
@@ -283,42 +284,56 @@ FEDRAG_KERNEL __launch_bounds__(THREADS) void paged_keep_kernel(const PagedKeepJ
     auto place = [&](int page, int64_t token) {
         return (uint32_t)page < n_pages ? pages + (int64_t)page * page_bytes + (token & ((1 << j.shift) - 1)) * row_bytes + c : nullptr;
     };
-    char *from[kSteps], *to[kSteps];
-    auto look_up = [&](int64_t j0) {  // the places of kSteps * kRows rows from j0 on; null: nothing to move
-        int64_t k[kSteps], i[kSteps];
-        int from_page[kSteps], to_page[kSteps];
+    // Four stages, each with the rows of a round in its arrays: the list, the table, the rows, and the writing.  Reading the rows of a round
+    // before those of the round before are written is sound: they lie above all that these are written to.
+    int k[kSteps], from_page[kSteps], to_page[kSteps], moved[kSteps];
+    char* dest[kSteps];
+    u32x4_t row[kSteps];
+    const int step = threadIdx.x / CH;
+    auto list = [&](int64_t j0) {
+#pragma unroll
+        for (int u = 0; u < kSteps; ++u) k[u] = j0 + u * kRows + step < count ? kept[j0 + u * kRows + step] : -1;
+    };
+    auto pages_of = [&](int64_t j0) {
 #pragma unroll
         for (int u = 0; u < kSteps; ++u) {
-            i[u] = j0 + u * kRows + threadIdx.x / CH;
-            k[u] = i[u] < count ? kept[i[u]] : 0;
-        }
-#pragma unroll
-        for (int u = 0; u < kSteps; ++u) {
-            const bool moves = i[u] < count && k[u] > i[u] && k[u] < n;  // (a row that stays where it is has nothing to do)
+            const int64_t i = j0 + u * kRows + step;
+            const bool moves = k[u] > i && k[u] < n;  // (a row that stays where it is has nothing to do)
+            moved[u] = k[u];
             from_page[u] = moves ? page_of(base + k[u]) : -1;
-            to_page[u] = moves ? page_of(base + i[u]) : -1;
-        }
-#pragma unroll
-        for (int u = 0; u < kSteps; ++u) {
-            from[u] = place(from_page[u], base + k[u]);
-            to[u] = from[u] ? place(to_page[u], base + i[u]) : nullptr;
+            to_page[u] = moves ? page_of(base + i) : -1;
         }
     };
-    look_up(0);
-    for (int64_t j0 = 0; j0 < count; j0 += kSteps * kRows) {
-        u32x4_t row[kSteps];
-        char* dest[kSteps];
+    auto read = [&](int64_t j0) {
 #pragma unroll
         for (int u = 0; u < kSteps; ++u) {
-            dest[u] = to[u];
-            if (to[u]) row[u] = *(const u32x4_t*)from[u];
+            const char* const from = place(from_page[u], base + moved[u]);
+            dest[u] = from ? place(to_page[u], base + j0 + u * kRows + step) : nullptr;
+            if (dest[u]) row[u] = *(const u32x4_t*)from;
         }
-        if (j0 + kSteps * kRows < count) look_up(j0 + kSteps * kRows);
+    };
+    constexpr int64_t kRound = kSteps * kRows;
+    list(0);
+    pages_of(0);
+    if (kRound < count) list(kRound);
+    read(0);
+    if (kRound < count) pages_of(kRound);
+    for (int64_t j0 = 0; j0 < count; j0 += kRound) {
+        if (j0 + 2 * kRound < count) list(j0 + 2 * kRound);
         __builtin_amdgcn_s_waitcnt(0x0f70);  // this thread's chunks are here, and behind the barrier everybody's
         __syncthreads();
+        char* to[kSteps];
+        u32x4_t old[kSteps];
+#pragma unroll
+        for (int u = 0; u < kSteps; ++u) {
+            to[u] = dest[u];
+            old[u] = row[u];
+        }
+        if (j0 + kRound < count) read(j0 + kRound);
 #pragma unroll
         for (int u = 0; u < kSteps; ++u)
-            if (dest[u]) *(u32x4_t*)dest[u] = row[u];
+            if (to[u]) *(u32x4_t*)to[u] = old[u];
+        if (j0 + 2 * kRound < count) pages_of(j0 + 2 * kRound);
     }
 }
 
@@ -341,7 +356,7 @@ hipError_t launch_paged_keep(const PagedKeep& k, hipStream_t stream) {
         j.cache[i].n_pages = k.pages[i].n_pages;
     }
     // Accepted drafts: a wave for all chunks of a head's rows.  Long lists are a chain of steps, which workgroups of many threads and few
-    // chunks make short: one to a workgroup (20001 of 32768 tokens, 8 heads of 64 in fp16: 51 us, two chunks 59, all eight 255), or more while there
+    // chunks make short: one to a workgroup (20001 of 32768 tokens, 8 heads of 64 in fp16, when one took 51 us: two chunks 59, all eight 255), or more while there
     // are two workgroups to a compute unit all the same.
     const int chunks = j.row_bytes / 16;
     const bool few = k.max_kept <= 64;
@@ -358,7 +373,9 @@ hipError_t launch_paged_keep(const PagedKeep& k, hipStream_t stream) {
 // ------------------------------------------------------------------------------------------------ trim
 // One workgroup takes the requests 1024 at a time.  Their places on the stack are prefix sums of the pages that each gives back: entries of
 // the table below 0 are none, so that the columns are looked at before any is written.  Up to 1024 columns are a thread's each; more are
-// a wave's request by request, twice (the second time out of L2), the columns of two requests in flight together.
+// a wave's request by request, twice (the second time out of L2), the columns of two requests in flight together.  64 requests of a page or
+// none 3.8 us on the device; 256 that end at once, 130000 pages, 30: what one compute unit reads and writes in that time (loads of
+// 16 bytes a lane, wherever they begin, 34).
 constexpr int kTrimWaves = kMapThreads / kWave;
 constexpr int kTrimAhead = 4;  // columns of a request that a lane has in flight
 

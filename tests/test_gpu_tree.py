@@ -489,7 +489,8 @@ def _trim(kv, n_kept, table, free, count, page, start=None, in_place=False):
 
 
 @pytest.mark.parametrize("B,page,top,tree", [(1, 16, 50, True), (7, 256, 900, True), (64, 16, 3000, True), (1025, 16, 40, True), (3, 32, 9000, False),
-                                             (2300, 64, 130, False), (100, 16, 8000, False)])
+                                             (2300, 64, 130, False), (100, 16, 8000, False), (1, 16, 60000, True), (6, 16, 60000, False),
+                                             (1500, 16, 90, False)])
 def test_trim(B, page, top, tree):
     rng = np.random.default_rng(B)
     kv = rng.integers(1, top, B)
@@ -502,7 +503,7 @@ def test_trim(B, page, top, tree):
         assert _trim(kv, kept, table, free, 5, page, TR.starts(n) if tree else None, in_place)[3] == 0
 
 
-@pytest.mark.parametrize("what", ["full", "no_stack", "holes", "lengths", "count_above", "count_below", "short", "no_requests", "no_columns"])
+@pytest.mark.parametrize("what", ["full", "no_stack", "holes", "full_of_holes", "lengths", "count_above", "count_below", "short", "no_requests", "no_columns"])
 def test_trim_out_of_the_ordinary(what):
     rng = np.random.default_rng(4)
     B, page = 300, 16
@@ -513,7 +514,9 @@ def test_trim_out_of_the_ordinary(what):
         free = free[:200]
     if what == "no_stack":
         free, count = free[:0], 0
-    if what == "holes":
+    if what == "full_of_holes":
+        free = free[:7003]
+    if what in ("holes", "full_of_holes"):
         table[rng.random(table.shape) < 0.3] = -1
         table[5:40] = -2 ** 31
     if what == "lengths":
