@@ -4,15 +4,19 @@
 // 32-key tiles in turn, each for all rows, and are folded at the end.  A key tile goes from its pages to LDS in whole rows, into a slot
 // that belongs to one wave and needs no barrier; K's half is filled again after the first product, V's after the second, so that
 // two tiles' worth of loads fly behind every step, and two workgroups share a compute unit: 128 KiB in flight at 128 columns.
+// Bound by reading: 32 requests of 1000 to 32768 tokens, 8 KV heads of 128 in bf16, 1.24 GB: 16 rows a KV head 212 us (5.9 TB/s), 32 rows 224 (5.6).
 // SUBS = 2: a tile's rows are two workgroups', which take the same keys at the same time on one XCD: what the one has read is in L2 for
-// the other.
+// the other.  64 rows over the same keys 265 to 280 us (4.5 TB/s): 150 with all of them in L2, 200 by HBM, and the two hardly overlap.  (All 64 rows
+// in each of four waves, one to a SIMD: 343; eight waves, two to a key tile behind a barrier 265, but half as long again for short requests.)
 // Lane l of a wave: lr = l % 16, lq = l / 16.  For each 16 rows g:
 //   S^T (32 keys x 16 rows) = K (32 x d) . Q^T (d x 16): two 16-key MFMA tiles; this lane holds row lr and keys 16 mt + 4 lq + r,
 //   which are also its contraction slice of O^T (d x 16) += V^T (d x 32) . P^T (32 x 16), whose V^T operands come through
 //   the transposing LDS read.  An operand of K or V is read once for all of a wave's rows.
-// Probabilities enter the second product as two storage-type terms (about 16 significant bits): outputs are fp32.  They are relative to
-// the largest score so far, whose own probability is a power of two and exact; outputs are rescaled only where it moves.  (Leaving it
-// until it is 2^8 off takes 1 % off the time and doubles the error of rows whose weight sits on few tokens.)
+// Probabilities enter the second product as two storage-type terms in fp16 (22 significant bits) and three in bf16 (24; of two workgroups a
+// tile two, 16: there the third would cost 3 to 10 %, 64 rows of 64 columns 162 -> 177 us, up to 32 rows 0 to 1.5 %; outputs of drafts behind
+// short requests are 2e-7 to 4e-7 off with it, 6e-7 to 1e-6 without).  They are relative to the largest score so far, whose own probability
+// is a power of two and exact; outputs are rescaled only where it moves.  (Leaving it until it is 2^8 off takes 1 % off the time and doubles
+// the error of rows whose weight sits on few tokens.)
 // Only the key tiles that hold drafted tokens are masked, by bits of the rows' words.
 #pragma once
 #include "attn_paged.h"
@@ -54,6 +58,7 @@ __device__ __forceinline__ void tree_body(const PagedArgs& a, uint32_t wg, Slots
     constexpr int WAVES = kTreeWaves;
     constexpr int ROWS = 16 * NQ;
     constexpr int PCH = D / 4;  // 16-byte chunks of a row of O
+    constexpr bool kThree = std::is_same<T, BF16>::value && SUBS == 1;
     const float scale_log2 = a.scale * kLog2e;
     const int tid = threadIdx.x;
     const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
@@ -211,7 +216,7 @@ __device__ __forceinline__ void tree_body(const PagedArgs& a, uint32_t wg, Slots
         }
         fill(i + 1, kslot, true);
         __builtin_amdgcn_sched_barrier(0);
-        vec8 ph[NQ], pl[NQ];
+        vec8 ph[NQ], pl[NQ], pr[NQ];
 #pragma unroll
         for (int g = 0; g < NQ; ++g) {
             if constexpr (masked) {
@@ -240,18 +245,21 @@ __device__ __forceinline__ void tree_body(const PagedArgs& a, uint32_t wg, Slots
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x[e] = __builtin_fmaf(s[g][e / 4][e % 4], scale_log2, -m_run[g]);
             }
-            u32x4_t hi, lo;
+            u32x4_t hi, lo, rest;
             float sum = 0.f;
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
                 const float p0 = fast_exp2(x[2 * w]), p1 = fast_exp2(x[2 * w + 1]);
                 sum += p0 + p1;
                 hi[w] = T::pack(p0, p1);
-                lo[w] = T::pack(p0 - T::low(hi[w]), p1 - T::high(hi[w]));
+                const float l0 = p0 - T::low(hi[w]), l1 = p1 - T::high(hi[w]);
+                lo[w] = T::pack(l0, l1);
+                if constexpr (kThree) rest[w] = T::pack(l0 - T::low(lo[w]), l1 - T::high(lo[w]));
             }
             l_run[g] += sum;
             ph[g] = __builtin_bit_cast(vec8, hi);
             pl[g] = __builtin_bit_cast(vec8, lo);
+            if constexpr (kThree) pr[g] = __builtin_bit_cast(vec8, rest);
         }
         wait_loads(std::integral_constant<int, KL>{});  // V's
         int vt_at = v_at;
@@ -324,6 +332,9 @@ __device__ __forceinline__ void tree_body(const PagedArgs& a, uint32_t wg, Slots
             for (int g = 0; g < NQ; ++g) acc[g][t] = T::mfma16(vop, ph[g], acc[g][t]);
 #pragma unroll
             for (int g = 0; g < NQ; ++g) acc[g][t] = T::mfma16(vop, pl[g], acc[g][t]);
+            if constexpr (kThree)
+#pragma unroll
+                for (int g = 0; g < NQ; ++g) acc[g][t] = T::mfma16(vop, pr[g], acc[g][t]);
             __builtin_amdgcn_sched_barrier(0);
         }
         fill(i + 1, vslot, false);
