@@ -133,7 +133,8 @@ struct Verify {
     const TreeVerifyJob& j;
     int b, s, n, parts;
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    uint64_t (*scratch)[2];  // LDS, a pair for each wave
+    uint64_t (*scratch)[2];                              // LDS, a pair for each wave
+    uint64_t (*row_sums)[kVerifyThreads / kWave];        // and a number for each part and wave
     bool target_only = false;  // weights are p's
     double next = 0.0;         // the request's u_next
 
@@ -251,48 +252,60 @@ struct Verify {
         if constexpr (WITH == 1) return verify_units_biased(fmax((double)x - (double)verify_value(qv), 0.0));
         return verify_units_biased(verify_left(x, verify_value(qv), taken));
     }
-    // This thread's share of a part's sum; every token of the part is some thread's.
-    template <int WITH>
-    __device__ __forceinline__ uint64_t part_sum_of(const E* pr, const E* qr, double taken, int part) const {
-        const int begin = part * kPart, end = begin + kPart < j.vocab ? begin + kPart : j.vocab;
+    // This thread's share of the sums of N parts; every token of a part is some thread's.
+    template <int WITH, int N>
+    __device__ __forceinline__ void part_sums_of(const E* pr, const E* qr, double taken, int part, uint64_t (&sum)[N]) const {
+        const int begin = part * kPart, end = begin + N * kPart < j.vocab ? begin + N * kPart : j.vocab;
         constexpr int VEC = 16 / (int)sizeof(E);
         typedef E vec __attribute__((ext_vector_type(VEC)));
         typedef vec vec_any __attribute__((aligned(sizeof(E))));
-        uint64_t sum = 0;
-        if (end - begin == kPart) {
-            vec pv[kEach / VEC], qv[kEach / VEC];
 #pragma unroll
-            for (int i = 0; i < kEach / VEC; ++i) {
-                pv[i] = *(const vec_any*)(pr + begin + (i * kVerifyThreads + (int)threadIdx.x) * VEC);
-                if constexpr (WITH != 0) qv[i] = *(const vec_any*)(qr + begin + (i * kVerifyThreads + (int)threadIdx.x) * VEC);
+        for (int k = 0; k < N; ++k) sum[k] = 0;
+        if (end - begin == N * kPart) {
+            vec pv[N][kEach / VEC], qv[N][kEach / VEC];
+#pragma unroll
+            for (int k = 0; k < N; ++k)
+#pragma unroll
+                for (int i = 0; i < kEach / VEC; ++i) {
+                    const int at = begin + k * kPart + (i * kVerifyThreads + (int)threadIdx.x) * VEC;
+                    pv[k][i] = *(const vec_any*)(pr + at);
+                    if constexpr (WITH != 0) qv[k][i] = *(const vec_any*)(qr + at);
+                }
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+#pragma unroll
+                for (int i = 0; i < kEach / VEC; ++i)
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) sum[k] += weight<WITH>((float)pv[k][i][e], WITH ? (float)qv[k][i][e] : 0.f, taken);
+                sum[k] -= kEach * kUnitsBias;
+            }
+            return;
+        }
+        // (the row's end, by single values; what is not there has no weight)
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            E pv[kEach], qv[kEach];
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                const int v = begin + k * kPart + i * kVerifyThreads + (int)threadIdx.x;
+                pv[i] = v < end ? pr[v] : (E)0.f;
+                if constexpr (WITH != 0) qv[i] = v < end ? qr[v] : (E)0.f;
             }
 #pragma unroll
-            for (int i = 0; i < kEach / VEC; ++i)
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) sum += weight<WITH>((float)pv[i][e], WITH ? (float)qv[i][e] : 0.f, taken);
-            return sum - kEach * kUnitsBias;
+            for (int i = 0; i < kEach; ++i) sum[k] += weight<WITH>((float)pv[i], WITH ? (float)qv[i] : 0.f, taken);
+            sum[k] -= kEach * kUnitsBias;
         }
-        // (the row's last part, by single values; what is not there has no weight)
-        E pv[kEach], qv[kEach];
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const int v = begin + i * kVerifyThreads + (int)threadIdx.x;
-            pv[i] = v < end ? pr[v] : (E)0.f;
-            if constexpr (WITH != 0) qv[i] = v < end ? qr[v] : (E)0.f;
-        }
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) sum += weight<WITH>((float)pv[i], WITH ? (float)qv[i] : 0.f, taken);
-        return sum - kEach * kUnitsBias;
     }
-    __device__ __forceinline__ uint64_t part_sum(const VerifyState& st, int part) const {
+    template <int N>
+    __device__ __forceinline__ void part_sums(const VerifyState& st, int part, uint64_t (&sum)[N]) const {
         const E* const pr = row_p(st.node);
         if constexpr (DRAFT) {
             if (with_draft(st)) {
-                if (st.taken == kUnit) return part_sum_of<1>(pr, row_q(st.node), 1.0, part);
-                return part_sum_of<2>(pr, row_q(st.node), (double)st.taken / kUnits, part);
+                if (N == 1 && st.taken == kUnit) return part_sums_of<1>(pr, row_q(st.node), 1.0, part, sum);
+                return part_sums_of<2>(pr, row_q(st.node), (double)st.taken / kUnits, part, sum);
             }
         }
-        return part_sum_of<0>(pr, pr, 0.0, part);
+        return part_sums_of<0>(pr, pr, 0.0, part, sum);
     }
     static __device__ __forceinline__ uint64_t of_lane(uint64_t x, int l) {
         const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, l);
@@ -318,7 +331,9 @@ struct Verify {
     }
     // A part's sum, in every thread.
     __device__ __forceinline__ uint64_t part_total(const VerifyState& st, int part) {
-        uint64_t x = total(part_sum(st, part));
+        uint64_t sum[1];
+        part_sums(st, part, sum);
+        uint64_t x = total(sum[0]);
         if constexpr (!DRAFT) {
             if (!target_only)
                 rejected(st, [&](int child, int v) {
@@ -366,10 +381,28 @@ struct Verify {
     }
     // The sums of all parts, a thread each, by this workgroup alone.
     __device__ __forceinline__ uint64_t all_parts(const VerifyState& st) {
+        constexpr int N = 2;  // parts on their way at once (one: 49 us where one of two requests needs a sum more than there are rounds, so 39)
+        __syncthreads();
+        for (int i = 0; i < parts; i += N) {
+            uint64_t sum[N];
+            part_sums(st, i, sum);
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                const uint64_t x = wave_add(sum[k]);
+                if (lane == 0 && i + k < parts) row_sums[i + k][wave] = x;
+            }
+        }
+        __syncthreads();
         uint64_t mine = 0;
-        for (int i = 0; i < parts; ++i) {
-            const uint64_t x = part_total(st, i);
-            if ((int)threadIdx.x == i) mine = x;
+        if ((int)threadIdx.x < parts) {
+#pragma unroll
+            for (int w = 0; w < kVerifyThreads / kWave; ++w) mine += row_sums[threadIdx.x][w];
+        }
+        if constexpr (!DRAFT) {
+            if (!target_only)
+                rejected(st, [&](int child, int v) {
+                    if (!repeated(st.node, child, v) && v / kPart == (int)threadIdx.x) mine -= verify_units((double)verify_value((float)row_p(st.node)[v]));
+                });
         }
         return mine;
     }
@@ -429,7 +462,7 @@ struct Verify {
 
 template <class E, bool DRAFT>
 FEDRAG_KERNEL __launch_bounds__(kVerifyThreads) void tree_verify_kernel(TreeVerifyJob j, int parts, int round, int last_round) {
-    __shared__ uint64_t scratch[kVerifyThreads / kWave][2];
+    __shared__ uint64_t scratch[kVerifyThreads / kWave][2], row_sums[kMostParts][kVerifyThreads / kWave];
     const int part = (int)blockIdx.x, b = (int)blockIdx.y;
     VerifyState* const states = (VerifyState*)j.workspace;  // [2][batch], then the sums [2][batch][parts]
     uint64_t* const sums = (uint64_t*)(states + 2 * (int64_t)j.batch);
@@ -437,6 +470,7 @@ FEDRAG_KERNEL __launch_bounds__(kVerifyThreads) void tree_verify_kernel(TreeVeri
     const int s = clamped(j.q_start[b], 0, j.n_rows), e = clamped(j.q_start[b + 1], 0, j.n_rows);
     Verify<E, DRAFT> v{j, b, s, e > s ? e - s : 0, parts};
     v.scratch = scratch;
+    v.row_sums = row_sums;
     v.at = -1;
     VerifyState st{kVerifyDone, 0, 0, 1, 0};
     // (what the round may need of the one before, in one trip to memory)
@@ -480,13 +514,13 @@ FEDRAG_KERNEL __launch_bounds__(kVerifyThreads) void tree_verify_kernel(TreeVeri
         return;
     }
     if (st.need == kVerifyDone || part != 0) return;
+    uint64_t mine = v.all_parts(st);
     while (st.need == kVerifyMass) {  // (each time around a child has been tried)
-        uint64_t sum = 0;
-        for (int i = 0; i < parts; ++i) sum += v.part_sum(st, i);
-        v.walk(st, v.total(sum), true);
+        v.walk(st, v.total(mine), true);
+        mine = v.all_parts(st);
     }
     finish_kept();
-    v.draw(st, v.all_parts(st), -1);
+    v.draw(st, mine, -1);
 }
 
 // Rows of up to 128 KiB (32768 tokens in fp32, 65536 in 16 bits): one workgroup to a request, whose threads have the row of p and that of q
