@@ -474,7 +474,7 @@ size_t fedrag_paged_attn_workspace_bytes(const fedrag_shape* shape, int64_t n_ro
  * Nodes for every token and layer (Section 5.3): several drafts in one step share it.
  *
  * Row t of request b, t = q_start[b] .. q_start[b+1]-1, is node i = t - q_start[b]; n = q_start[b+1] - q_start[b] is the number of its
- * nodes.  q_start and what lies behind the last request are as in the paged calls.
+ * nodes.  q_start and what lies behind the last request are as in the paged calls;  n_rows <= INT32_MAX - 255.
  */
 
 /*
@@ -498,7 +498,8 @@ fedrag_status fedrag_tree_map(int32_t batch, int64_t n_rows, int32_t mask_words,
  * sees the first kv_lens[b] - n, and token kv_lens[b] - n + j if bit j of tree_mask[t] is set, 0 <= j < n, j < 64 * mask_words.
  * tree_mask : uint64 [n_rows, mask_words], 8-byte aligned, any bits (an ancestor is not told from another node);
  * a row without any bit sees the tokens of before, and if there are none, it has O = 0, lse = -inf.
- * Everything else as fedrag_paged_attn: strides, rounding, what is not finite, padding rows, max_q_len, the workspace's use.
+ * Everything else as fedrag_paged_attn: strides, rounding, what is not finite, padding rows, max_q_len, the workspace's use, but that
+ * probabilities in bf16 may enter the second product as three terms, with all their bits (requests of up to 32 rows a KV head).
  */
 fedrag_status fedrag_paged_tree_attn(const fedrag_shape* shape, int64_t n_rows, const fedrag_rows* Q,
                                      const fedrag_paged_cache* cache, const int32_t* block_table, int64_t max_pages,
@@ -506,7 +507,8 @@ fedrag_status fedrag_paged_tree_attn(const fedrag_shape* shape, int64_t n_rows, 
                                      int64_t max_q_len, float softmax_scale, float* O, float* lse,
                                      void* workspace, size_t workspace_bytes, void* stream);
 
-/* Bytes of workspace fedrag_paged_tree_attn needs for these sizes, by the rules of fedrag_paged_attn_workspace_bytes. */
+/* Bytes of workspace fedrag_paged_tree_attn needs for these sizes, by the rules of fedrag_paged_attn_workspace_bytes; whatever the
+ * sizes, 73 MiB are enough on a device of 256 compute units. */
 size_t fedrag_paged_tree_attn_workspace_bytes(const fedrag_shape* shape, int64_t n_rows, int64_t max_pages,
                                               int32_t page_tokens, int64_t max_q_len);
 
