@@ -371,30 +371,35 @@ hipError_t launch_paged_keep(const PagedKeep& k, hipStream_t stream) {
 }
 
 // ------------------------------------------------------------------------------------------------ trim
-// One workgroup takes the requests 1024 at a time.  Their places on the stack are prefix sums of the pages that each gives back: entries of
-// the table below 0 are none, so that the columns are looked at before any is written.  Up to 1024 columns are a thread's each; more are
-// a wave's request by request, twice (the second time out of L2), the columns of two requests in flight together.  64 requests of a page or
-// none 3.8 us on the device; 256 that end at once, 130000 pages, 30: what one compute unit reads and writes in that time (loads of
-// 16 bytes a lane, wherever they begin, 34).
+// The requests are taken 1024 at a time.  Their places on the stack are prefix sums of the pages that each gives back: entries of the table
+// below 0 are none, so that the columns are looked at before any is written.  Up to 1024 columns are a thread's each, of the last
+// workgroup; more are a wave's request by request, the columns of two requests in flight together: a workgroup counts what is before its
+// share, and writes its share (the second time out of L2).  Nothing passes between workgroups, and the last one keeps the books.  64 requests
+// of a page or none 4.5 us on the device; 256 that end at once, 130000 pages, 20: the last workgroup's count of all, at some 50 GB/s.
+// (More columns in flight, or 16 bytes a lane: 33 to 42 us by one workgroup, which takes 30.)
 constexpr int kTrimWaves = kMapThreads / kWave;
+constexpr int kTrimMost = 16;  // workgroups
 constexpr int kTrimAhead = 4;  // columns of a request that a lane has in flight
 
 FEDRAG_KERNEL __launch_bounds__(kMapThreads) void paged_trim_kernel(PagedTrimJob j, int shift) {
     __shared__ MapPrefix waves[kTrimWaves];
     __shared__ uint32_t col_end[kMapThreads], found[kMapThreads];
     __shared__ int first_col[kMapThreads];
+    __shared__ int range[kTrimWaves][2];
     __shared__ int flags;
     const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+    const uint32_t wg = blockIdx.x, wgs = gridDim.x;
+    const bool last = wg == wgs - 1;
     const int64_t max_pages = j.max_pages;
     const int count_in = *j.free_count;
     const uint32_t count = count_in < 0 ? 0 : (uint32_t)(count_in < j.n_free ? count_in : j.n_free);
     const uint32_t most = INT_MAX;
     uint32_t top = count;
+    bool full = false;  // there is no room for all
     if (tid == 0) flags = (uint32_t)count_in == count ? 0 : FEDRAG_TRIM_BAD_LENGTH;
     auto below = [&](uint64_t lanes) { return (uint32_t)__builtin_popcountll(lanes & (((uint64_t)1 << lane) - 1)); };
     auto push = [&](uint32_t to, int id) {
         if (to < j.n_free) j.free_pages[to] = id;
-        else atomicOr(&flags, FEDRAG_TRIM_NO_ROOM);
     };
     for (int64_t b0 = 0; b0 < j.batch; b0 += kMapThreads) {
         __syncthreads();
@@ -414,7 +419,7 @@ FEDRAG_KERNEL __launch_bounds__(kMapThreads) void paged_trim_kernel(PagedTrimJob
             const int64_t stay = (len + (1 << shift) - 1) >> shift;
             mine = had > stay ? (uint32_t)(had - stay) : 0;
             first_col[tid] = (int)stay;
-            j.lens_out[b] = (int)len;
+            if (last) j.lens_out[b] = (int)len;
         }
         MapPrefix total;
         const MapPrefix p = map_scan(MapPrefix{mine, 0}, most, waves, &total);
@@ -435,16 +440,34 @@ FEDRAG_KERNEL __launch_bounds__(kMapThreads) void paged_trim_kernel(PagedTrimJob
                 if (w == wave) before = sum;
                 sum += found[w];
             }
-            if (id >= 0) push(top + before + below(pages), id);
+            if (id >= 0 && last) push(top + before + below(pages), id);
+            full = full || top + sum > (uint32_t)j.n_free;
             top = min(top + sum, (uint32_t)j.n_free);
             continue;
         }
+        // This workgroup writes the pages of requests lo .. hi-1, an even share of the columns, and counts those before them, too (and those
+        // behind them, if there are requests after these).
+        auto up_to = [&](uint32_t w) {
+            const uint32_t bound = (uint32_t)((uint64_t)total.rows * w / wgs);
+            return __builtin_popcountll(__builtin_amdgcn_ballot_w64(b < j.batch && (w == wgs || p.rows - mine < bound)));
+        };
+        const int lo_here = up_to(wg), hi_here = up_to(wg + 1);
+        if (lane == 0) {
+            range[wave][0] = lo_here;
+            range[wave][1] = hi_here;
+        }
         col_end[tid] = mine;  // (how many, here)
         __syncthreads();
+        int lo = 0, hi = 0;
+#pragma unroll
+        for (int w = 0; w < kTrimWaves; ++w) {
+            lo += range[w][0];
+            hi += range[w][1];
+        }
         // f(request, a lane's entries of it from column c on, one every 64; -1: none)
-        auto each = [&](auto f) {
-            for (int k0 = wave; k0 < n_req; k0 += 2 * kTrimWaves) {
-                const int k1 = k0 + kTrimWaves < n_req ? k0 + kTrimWaves : k0;
+        auto each = [&](int from, int end, auto f) {
+            for (int k0 = from + wave; k0 < end; k0 += 2 * kTrimWaves) {
+                const int k1 = k0 + kTrimWaves < end ? k0 + kTrimWaves : k0;
                 const uint32_t n0 = col_end[k0], n1 = k1 != k0 ? col_end[k1] : 0;
                 const int32_t* const row0 = j.block_table + (b0 + k0) * max_pages + first_col[k0];
                 const int32_t* const row1 = j.block_table + (b0 + k1) * max_pages + first_col[k1];
@@ -461,7 +484,7 @@ FEDRAG_KERNEL __launch_bounds__(kMapThreads) void paged_trim_kernel(PagedTrimJob
                 }
             }
         };
-        each([&](int k, const int (&id)[kTrimAhead]) {
+        each(0, b0 + kMapThreads < j.batch ? n_req : hi, [&](int k, const int (&id)[kTrimAhead]) {
             uint32_t n = 0;
 #pragma unroll
             for (int u = 0; u < kTrimAhead; ++u) n += (uint32_t)__builtin_popcountll(__builtin_amdgcn_ballot_w64(id[u] >= 0));
@@ -473,7 +496,7 @@ FEDRAG_KERNEL __launch_bounds__(kMapThreads) void paged_trim_kernel(PagedTrimJob
         const MapPrefix q = map_scan(MapPrefix{here, 0}, most, waves, &all);
         found[tid] = top + (q.rows - here);  // where the request's next page goes
         __syncthreads();
-        each([&](int k, const int (&id)[kTrimAhead]) {
+        each(lo, hi, [&](int k, const int (&id)[kTrimAhead]) {
             uint32_t to = found[k];
             wave_lds_fence();  // (all lanes have it)
 #pragma unroll
@@ -485,17 +508,23 @@ FEDRAG_KERNEL __launch_bounds__(kMapThreads) void paged_trim_kernel(PagedTrimJob
             if (lane == 0) found[k] = to;
             wave_lds_fence();
         });
+        full = full || top + all.rows > (uint32_t)j.n_free;
         top = min(top + all.rows, (uint32_t)j.n_free);
     }
     __syncthreads();
-    if (tid == 0) {
+    if (tid == 0 && last) {
         *j.free_left = (int)top;
-        *j.flags = flags;
+        *j.flags = flags | (full ? FEDRAG_TRIM_NO_ROOM : 0);
     }
 }
 
 hipError_t launch_paged_trim(const PagedTrimJob& job, hipStream_t stream) {
-    hipLaunchKernelGGL(paged_trim_kernel, dim3(1), dim3(kMapThreads), 0, stream, job, __builtin_ctz((unsigned)job.page_tokens));
+    // Lengths and a count that are written in place are one workgroup's work, as the others would still read them.  (256 requests of 300 to
+    // 16000 tokens that end at once: 30.5 us by one, 22.8, 21.4, 20.6, 20.4 by 4, 8, 16, 32; of up to 900 17.5 and 12.0.)
+    const bool in_place = job.lens_out == job.kv_lens || job.free_left == job.free_count;
+    const int64_t shares = in_place ? 1 : (int64_t)job.batch * job.max_pages / kMapThreads;  // (of up to so many columns one reads each at once)
+    const int wgs = shares < 1 ? 1 : shares < kTrimMost ? (int)shares : kTrimMost;
+    hipLaunchKernelGGL(paged_trim_kernel, dim3((unsigned)wgs), dim3(kMapThreads), 0, stream, job, __builtin_ctz((unsigned)job.page_tokens));
     return hipGetLastError();
 }
 

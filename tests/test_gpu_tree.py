@@ -503,20 +503,20 @@ def test_trim(B, page, top, tree):
         assert _trim(kv, kept, table, free, 5, page, TR.starts(n) if tree else None, in_place)[3] == 0
 
 
-@pytest.mark.parametrize("what", ["full", "no_stack", "holes", "full_of_holes", "lengths", "count_above", "count_below", "short", "no_requests", "no_columns"])
+@pytest.mark.parametrize("what", ["full", "no_stack", "holes", "full_of_holes", "many", "lengths", "count_above", "count_below", "short", "no_requests", "no_columns"])
 def test_trim_out_of_the_ordinary(what):
     rng = np.random.default_rng(4)
-    B, page = 300, 16
+    B, page = 2500 if what == "many" else 300, 16
     kv, kept = rng.integers(1, 2000, B), rng.integers(0, 60, B)
     kept = np.minimum(kv, kept)
-    table, free, count = rng.integers(0, 10 ** 6, (B, 130)), rng.integers(0, 10 ** 6, 30000), 9
+    table, free, count = rng.integers(0, 10 ** 6, (B, 130)), rng.integers(0, 10 ** 6, 30000 if B == 300 else 150000), 9
     if what == "full":
         free = free[:200]
     if what == "no_stack":
         free, count = free[:0], 0
     if what == "full_of_holes":
         free = free[:7003]
-    if what in ("holes", "full_of_holes"):
+    if what in ("holes", "full_of_holes", "many"):
         table[rng.random(table.shape) < 0.3] = -1
         table[5:40] = -2 ** 31
     if what == "lengths":
