@@ -246,7 +246,7 @@ hipError_t launch_paged_write(const PagedWriteJob& job, hipStream_t stream) {
 // lies above kept[j] >= j), so that the next round's can be on their way by then.  A workgroup has CH 16-byte chunks of one head's rows,
 // K's or V's, of a request in one cache: its rounds follow each other, but its chunks are its own.  Bound for accepted drafts by its chain
 // of trips (lengths, list, table, rows: 16 requests in 32 layers 6.4 us), for long lists by the addresses of a workgroup's loads and
-// stores, a lane's each for 16 bytes: 4096 rows a round of 9 us (20001 of 32768 tokens of 8 heads of 64 in fp16 43 us, 1.9 TB/s; 51 with
+// stores, a lane's each for 16 bytes of a line: 4096 rows a round of 8 us (20001 of 32768 tokens of 8 heads of 64 in fp16 42 us, 1.9 TB/s; 51 with
 // the next round's rows asked for after this one's are written).
 struct PagedKeepJob {
     const int32_t *table, *q_start, *kv_lens, *kept, *n_kept;
@@ -267,72 +267,73 @@ FEDRAG_KERNEL __launch_bounds__(THREADS) void paged_keep_kernel(const PagedKeepJ
     const int b = (int)j.by_h.div(blockIdx.x), h = (int)(blockIdx.x - (uint32_t)b * j.by_h.d);
     const uint32_t layer = j.by_splits.div(blockIdx.y), split = blockIdx.y - layer * j.by_splits.d;
     const auto& cache = j.cache[layer];
-    char* const pages = blockIdx.z ? cache.V : cache.K;
     const int64_t page_bytes = cache.page_bytes;
     const uint32_t n_pages = cache.n_pages;
+    const int row_bytes = j.row_bytes, shift = j.shift;
+    char* const chunk = (blockIdx.z ? cache.V : cache.K) + ((int64_t)h << shift) * row_bytes + ((int)split * CH + threadIdx.x % CH) * 16;
     const int kv = j.kv_lens[b] < 0 ? 0 : j.kv_lens[b];
-    const int64_t n = (int64_t)j.q_start[b + 1] - j.q_start[b], base = kv - n;
-    int64_t count = j.n_kept[b] < n ? j.n_kept[b] : n;
-    count = count < j.max_kept ? count : j.max_kept;
+    const int64_t rows = (int64_t)j.q_start[b + 1] - j.q_start[b];
+    const int n = rows < 0 ? 0 : rows < INT_MAX ? (int)rows : INT_MAX, base = kv - n;
+    int64_t most = j.n_kept[b] < n ? j.n_kept[b] : n;
+    most = most < j.max_kept ? most : j.max_kept;
+    const uint32_t count = most > 0 ? (uint32_t)most : 0;
     const int32_t* const kept = j.kept + b * j.max_kept;
     const int32_t* const table = j.table + b * j.max_pages;
-    const int64_t c = ((int64_t)h << j.shift) * j.row_bytes + ((int)split * CH + threadIdx.x % CH) * 16;
-    const int row_bytes = j.row_bytes;
-    auto page_of = [&](int64_t token) {  // -1: there is no such token, or no column for it
-        return token >= 0 && token < kv && token >> j.shift < j.max_pages ? table[token >> j.shift] : -1;
-    };
-    auto place = [&](int page, int64_t token) {
-        return (uint32_t)page < n_pages ? pages + (int64_t)page * page_bytes + (token & ((1 << j.shift) - 1)) * row_bytes + c : nullptr;
-    };
+    const uint32_t end = j.max_pages << shift < kv ? (uint32_t)(j.max_pages << shift) : (uint32_t)kv;  // tokens that have a column
+    auto page_of = [&](int token) { return (uint32_t)token < end ? table[(uint32_t)token >> shift] : -1; };
+    auto place = [&](int page, int token) { return chunk + ((int64_t)page * page_bytes + (token & ((1 << shift) - 1)) * row_bytes); };
     // Four stages, each with the rows of a round in its arrays: the list, the table, the rows, and the writing.  Reading the rows of a round
     // before those of the round before are written is sound: they lie above all that these are written to.
-    int k[kSteps], from_page[kSteps], to_page[kSteps], moved[kSteps];
-    char* dest[kSteps];
+    int k[kSteps], from_page[kSteps], to_page[kSteps], from[kSteps];
+    char* to[kSteps];
+    bool moves[kSteps];
     u32x4_t row[kSteps];
-    const int step = threadIdx.x / CH;
-    auto list = [&](int64_t j0) {
+    const uint32_t step = threadIdx.x / CH;
+    auto list = [&](uint32_t j0) {
 #pragma unroll
         for (int u = 0; u < kSteps; ++u) k[u] = j0 + u * kRows + step < count ? kept[j0 + u * kRows + step] : -1;
     };
-    auto pages_of = [&](int64_t j0) {
+    auto pages_of = [&](uint32_t j0) {
 #pragma unroll
         for (int u = 0; u < kSteps; ++u) {
-            const int64_t i = j0 + u * kRows + step;
-            const bool moves = k[u] > i && k[u] < n;  // (a row that stays where it is has nothing to do)
-            moved[u] = k[u];
-            from_page[u] = moves ? page_of(base + k[u]) : -1;
-            to_page[u] = moves ? page_of(base + i) : -1;
+            const int i = (int)(j0 + u * kRows + step);
+            const bool is = k[u] > i && k[u] < n;  // (a row that stays where it is has nothing to do)
+            from[u] = base + k[u];
+            from_page[u] = is ? page_of(base + k[u]) : -1;
+            to_page[u] = is ? page_of(base + i) : -1;
         }
     };
-    auto read = [&](int64_t j0) {
+    auto read = [&](uint32_t j0) {
 #pragma unroll
         for (int u = 0; u < kSteps; ++u) {
-            const char* const from = place(from_page[u], base + moved[u]);
-            dest[u] = from ? place(to_page[u], base + j0 + u * kRows + step) : nullptr;
-            if (dest[u]) row[u] = *(const u32x4_t*)from;
+            moves[u] = (uint32_t)from_page[u] < n_pages && (uint32_t)to_page[u] < n_pages;
+            to[u] = place(to_page[u], base + (int)(j0 + u * kRows + step));
+            if (moves[u]) row[u] = *(const u32x4_t*)place(from_page[u], from[u]);
         }
     };
-    constexpr int64_t kRound = kSteps * kRows;
+    constexpr uint32_t kRound = kSteps * kRows;
     list(0);
     pages_of(0);
     if (kRound < count) list(kRound);
     read(0);
     if (kRound < count) pages_of(kRound);
-    for (int64_t j0 = 0; j0 < count; j0 += kRound) {
+    for (uint32_t j0 = 0; j0 < count; j0 += kRound) {  // (count is at most INT_MAX)
         if (j0 + 2 * kRound < count) list(j0 + 2 * kRound);
         __builtin_amdgcn_s_waitcnt(0x0f70);  // this thread's chunks are here, and behind the barrier everybody's
         __syncthreads();
-        char* to[kSteps];
+        char* old_to[kSteps];
+        bool old_moves[kSteps];
         u32x4_t old[kSteps];
 #pragma unroll
         for (int u = 0; u < kSteps; ++u) {
-            to[u] = dest[u];
+            old_to[u] = to[u];
+            old_moves[u] = moves[u];
             old[u] = row[u];
         }
         if (j0 + kRound < count) read(j0 + kRound);
 #pragma unroll
         for (int u = 0; u < kSteps; ++u)
-            if (to[u]) *(u32x4_t*)to[u] = old[u];
+            if (old_moves[u]) *(u32x4_t*)old_to[u] = old[u];
         if (j0 + 2 * kRound < count) pages_of(j0 + 2 * kRound);
     }
 }
