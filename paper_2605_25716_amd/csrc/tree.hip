@@ -525,7 +525,8 @@ FEDRAG_KERNEL __launch_bounds__(kVerifyThreads) void tree_verify_kernel(TreeVeri
 
 // Rows of up to 128 KiB (32768 tokens in fp32, 65536 in 16 bits): one workgroup to a request, whose threads have the row of p and that of q
 // in registers, so that a sum after the first at a node costs no trip to memory, and one launch does.  Bound by that workgroup's 64-bit
-// arithmetic (8 instructions a token and sum) and by its trips: 12.6 us on the device for 8 nodes of 32000 tokens in fp32, 6.5 for 64 tokens.
+// arithmetic (8 instructions a token and sum) and by what it can read (256 KB in some 4 us): 12.6 us on the device for 8 nodes of 32000 tokens in
+// fp32, 6.1 for 64 tokens.
 // Against rounds it is ahead everywhere: 1 request of 32000 tokens 11.7 us (17.4 by rounds), 64 23 (35), 200 27 (60), 1000 of 4 nodes 59
 // (104); 128 of 16000 in bf16 21 (50); 8 of 65001 in fp16 26 (31); without drafts 1000 of 32000 45 (64).
 constexpr int kWholeThreads = 1024;
@@ -541,6 +542,7 @@ FEDRAG_KERNEL __launch_bounds__(kWholeThreads) void tree_verify_whole_kernel(Tre
     typedef E vec __attribute__((ext_vector_type(VEC)));
     typedef vec vec_any __attribute__((aligned(sizeof(E))));
     __shared__ __attribute__((aligned(16))) uint64_t sums[2][kWholeSteps * kWholeWaves][kWave / 16];
+    __shared__ VerifyState walked;
     const int b = (int)blockIdx.x, tid = (int)threadIdx.x, lane = tid % kWave, wave = tid / kWave, vocab = j.vocab;
     const int s = clamped(j.q_start[b], 0, j.n_rows), e = clamped(j.q_start[b + 1], 0, j.n_rows);
     Verify<E, DRAFT> v{j, b, s, e > s ? e - s : 0, 0};
@@ -603,7 +605,16 @@ FEDRAG_KERNEL __launch_bounds__(kWholeThreads) void tree_verify_whole_kernel(Tre
     uint64_t two[2], all = kUnit;
     for (int turn = 0;; turn ^= 1) {
         if (!target_only) {
-            v.walk(st, all, true);
+            if constexpr (DRAFT) {  // by one wave (without drafts' rows all need to know the children that were rejected)
+                if (wave == 0) {
+                    v.walk(st, all, true);
+                    if (lane == 0) walked = st;
+                }
+                __syncthreads();
+                st = walked;
+            } else {
+                v.walk(st, all, true);
+            }
             if (st.need == kVerifyDraw) {
                 for (int64_t i = st.n_kept + tid; i < j.max_kept; i += kWholeThreads) j.kept[b * j.max_kept + i] = 0;
                 if (tid == 0) j.n_kept[b] = st.n_kept;
