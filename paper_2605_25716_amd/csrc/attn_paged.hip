@@ -214,7 +214,12 @@ static PagedPlan paged_plan(int B, int Hq, int Hkv, int dtype, int64_t T, int64_
     const bool alike = 8 * T > 7 * (int64_t)B * most;
     if (tree && (most * G <= 32 || (most * G <= 64 && alike))) {
         const int tile = !many ? 4 : most * G <= 32 ? 5 : 6;
-        p.shares = paged_shares(PagedCut{tile, 8, 1, tile == 6 ? cus : cus + 1, 1, 1, INT32_MAX}, tiles(tile), keys);
+        // A unit of keys is two steps of each wave, or one for 17 to 32 rows where that leaves workgroups for all, few to a tile (32 heads of 128: 6
+        // tokens over 500 12.6 us, 14.2 by two steps; 5 each of 8 heads over 1000, 200, 2000 14.0, 15.8; but 1 of 16 heads over 5000 and 2 over 9000
+        // 30.7, 19.8; 16 rows, 2 over 4000, 14.8, 13.5; 64, 16 over 1000, 17.0, 15.3).
+        const int target = tile == 6 ? cus : cus + 1;
+        const bool short_units = tile == 5 && keys > 256 && keys <= 2048 && tiles(tile) * ((keys + 255) >> 8) <= (int64_t)1 << target >> 1;
+        p.shares = paged_shares(PagedCut{tile, short_units ? 7 : 8, 1, target, 1, 1, INT32_MAX}, tiles(tile), keys);
         return p;
     }
     const int few_rows = tree ? 2 * kPagedDecodeRows : kPagedDecodeRows;  // of a request of few rows, beside others of many

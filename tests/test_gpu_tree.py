@@ -555,6 +555,14 @@ def test_many_short_requests(dt, n, G):
     R.check_attn(O[:, :, rows], lse[:, :, rows], ref, FILL)
 
 
+@pytest.mark.parametrize("dt,d", [("bf16", 128), ("f16", 64)])
+def test_short_units(dt, d):
+    """17 to 32 rows over 257 to 2048 tokens, where keys are cut into shorter units; around those bounds, beside requests of none and of one unit."""
+    for sizes, kv in (([6], [257]), ([6], [2048]), ([6], [2049]), ([8, 5, 0, 7], [129, 128, 300, 1000]), ([8, 8, 8], [8, 384, 900]), ([5, 8], [500, 700]),
+                      ([8], [256])):
+        _attn(_attn_case(sizes, kv, 8, 2, d, 16, dt, seed=sum(kv), columns_more=0), what=(sizes, kv))
+
+
 def test_pages_beyond_4_gib():
     """Attention, and rows moved, in pages whose bytes are numbered beyond 2^32."""
     H, page, d, n = 8, 256, 128, 9000
