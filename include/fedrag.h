@@ -533,7 +533,7 @@ size_t fedrag_paged_tree_attn_workspace_bytes(const fedrag_shape* shape, int64_t
  * u : double [n_rows], u_next : double [batch], in [0, 1), 8-byte aligned (outside: as the nearest);
  * kept : int32 [batch, max_kept], the nodes of the accepted path, beginning with 0, and 0 behind them;  n_kept, next_token : int32
  * [batch];  a request of no rows has n_kept = 0, next_token = -1.  batch : 0 .. 65535;  vocab : 1 .. 2^20;  max_kept : 1 .. INT32_MAX.
- * workspace : fedrag_tree_verify_workspace_bytes(batch, vocab) bytes, 16-byte aligned.  Out of place.
+ * workspace : fedrag_tree_verify_workspace_bytes(batch, vocab, dtype) bytes, 16-byte aligned (NULL if 0).  Out of place.
  */
 fedrag_status fedrag_tree_verify(int32_t batch, int64_t n_rows, int64_t vocab, int32_t dtype, const int32_t* q_start,
                                  const int32_t* parents, const int32_t* tokens, const void* target, int64_t target_stride,
@@ -541,8 +541,8 @@ fedrag_status fedrag_tree_verify(int32_t batch, int64_t n_rows, int64_t vocab, i
                                  int32_t* kept, int32_t* n_kept, int32_t* next_token,
                                  void* workspace, size_t workspace_bytes, void* stream);
 
-/* Bytes of workspace fedrag_tree_verify needs; 0 for sizes it would reject. */
-size_t fedrag_tree_verify_workspace_bytes(int32_t batch, int64_t vocab);
+/* Bytes of workspace fedrag_tree_verify needs: none for rows of 16 bytes to 128 KiB; 0 for arguments it would reject. */
+size_t fedrag_tree_verify_workspace_bytes(int32_t batch, int64_t vocab, int32_t dtype);
 
 /*
  * The rows that stay, moved together: for j = 0 .. n_kept[b]-1

@@ -137,7 +137,7 @@ def load() -> ctypes.CDLL:
         lib.fedrag_paged_tree_attn_workspace_bytes.restype = ctypes.c_size_t
         lib.fedrag_tree_verify.argtypes = [i32, i64, i64, i32, vp, vp, vp, vp, i64, vp, i64, vp, vp, i64, vp, vp, vp, vp,
                                            ctypes.c_size_t, vp]
-        lib.fedrag_tree_verify_workspace_bytes.argtypes = [i32, i64]
+        lib.fedrag_tree_verify_workspace_bytes.argtypes = [i32, i64, i32]
         lib.fedrag_tree_verify_workspace_bytes.restype = ctypes.c_size_t
         lib.fedrag_paged_keep.argtypes = [sp, i32, cp, vp, i64, vp, vp, vp, i64, vp, vp]
         lib.fedrag_paged_trim.argtypes = [i32, i32, i64, vp, vp, vp, vp, vp, i64, vp, vp, vp, vp, vp]
@@ -788,8 +788,15 @@ def fedrag_paged_tree_attn(Q, K_pages, V_pages, block_table, q_start, kv_lens, t
     return O_part, lse
 
 
-def fedrag_tree_verify_workspace_bytes(batch: int, vocab: int) -> int:
-    return int(load().fedrag_tree_verify_workspace_bytes(index(batch), index(vocab)))
+def fedrag_tree_verify_workspace_bytes(batch: int, vocab: int, dtype) -> int:
+    """Bytes for one call of these sizes; none for rows of up to 128 KiB."""
+    code = _DTYPES[dtype] if isinstance(dtype, torch.dtype) else int(dtype)
+    return int(load().fedrag_tree_verify_workspace_bytes(index(batch), index(vocab), code))
+
+
+@functools.lru_cache(maxsize=256)
+def _verify_need(*sizes) -> int:  # (the same on every device)
+    return fedrag_tree_verify_workspace_bytes(*sizes)
 
 
 def _vocab_rows(name, X, dtype, dev, n_rows, vocab):
@@ -823,13 +830,17 @@ def fedrag_tree_verify(target, tokens, parents, q_start, u, u_next, draft=None, 
     target_at, target_stride = _vocab_rows("target", target, target.dtype, dev, n_rows, vocab)
     draft_at, draft_stride = (None, 0) if draft is None else _vocab_rows("draft", draft, target.dtype, dev, n_rows, vocab)
     if workspace is None:
-        workspace = torch.empty(max(fedrag_tree_verify_workspace_bytes(B, vocab), 16), dtype=torch.uint8, device=target.device)
+        ws, ws_bytes = None, _verify_need(B, vocab, target.dtype)
+        if ws_bytes:
+            workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=target.device)
+            ws = workspace.data_ptr()
+    else:
+        ws, ws_bytes = _values("workspace", workspace, workspace.dtype, dev, 0), workspace.numel() * workspace.element_size()
     st = load().fedrag_tree_verify(
         B, n_rows, vocab, _DTYPES[target.dtype], _values("q_start", q_start, i32, dev, B + 1), _values("parents", parents, i32, dev, n_rows),
         _values("tokens", tokens, i32, dev, n_rows), target_at, target_stride, draft_at, draft_stride, _values("u", u, f64, dev, n_rows),
         _values("u_next", u_next, f64, dev, B), columns, _exactly("kept", kept, i32, dev, (B, columns)),
-        _values("n_kept", n_kept, i32, dev, B), _values("next_token", next_token, i32, dev, B),
-        _values("workspace", workspace, workspace.dtype, dev, 0), workspace.numel() * workspace.element_size(),
+        _values("n_kept", n_kept, i32, dev, B), _values("next_token", next_token, i32, dev, B), ws, ws_bytes,
         torch._C._cuda_getCurrentRawStream(dev))
     if st != OK:
         raise FedragError(st, "fedrag_tree_verify")

@@ -990,8 +990,9 @@ fedrag_status fedrag_tree_map(int32_t batch, int64_t n_rows, int32_t mask_words,
     return dev(launch_tree_map(batch, n_rows, mask_words, q_start, kv_lens, parents, tree_mask, positions, flags, (hipStream_t)stream));
 }
 
-size_t fedrag_tree_verify_workspace_bytes(int32_t batch, int64_t vocab) {
-    return verify_sizes_ok(batch, vocab) ? tree_verify_workspace(batch, (int)vocab) : 0;
+size_t fedrag_tree_verify_workspace_bytes(int32_t batch, int64_t vocab, int32_t dtype) {
+    if (!verify_sizes_ok(batch, vocab) || (dtype != FEDRAG_F32 && dtype != FEDRAG_BF16 && dtype != FEDRAG_F16)) return 0;
+    return tree_verify_workspace(batch, (int)vocab, dtype);
 }
 
 fedrag_status fedrag_tree_verify(int32_t batch, int64_t n_rows, int64_t vocab, int32_t dtype, const int32_t* q_start,
@@ -1023,8 +1024,8 @@ fedrag_status fedrag_tree_verify(int32_t batch, int64_t n_rows, int64_t vocab, i
     if ((words & 3u) || ((reinterpret_cast<uintptr_t>(u) | reinterpret_cast<uintptr_t>(u_next)) & 7u) || (values & (uintptr_t)(e - 1)) ||
         !aligned16(workspace))
         return FEDRAG_ERR_ALIAS;
-    const size_t need = tree_verify_workspace(batch, (int)vocab);
-    if (!workspace || workspace_bytes < need) return FEDRAG_ERR_WORKSPACE;
+    const size_t need = tree_verify_workspace(batch, (int)vocab, dtype);
+    if (need > 0 && (!workspace || workspace_bytes < need)) return FEDRAG_ERR_WORKSPACE;
     const size_t nb = (size_t)batch, nr = (size_t)n_rows;
     const Range in[] = {{q_start, nb * 4 + 4}, {parents, nr * 4}, {tokens, nr * 4}, {target, (size_t)target_bytes}, {draft, (size_t)draft_bytes},
                         {u, nr * 8}, {u_next, nb * 8}},

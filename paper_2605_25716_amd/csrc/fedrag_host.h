@@ -295,7 +295,7 @@ struct TreeVerifyJob {
     int32_t *kept, *n_kept, *next_token;
     void* workspace;
 };
-size_t tree_verify_workspace(int batch, int vocab);
+size_t tree_verify_workspace(int batch, int vocab, int dtype);
 hipError_t launch_tree_verify(const TreeVerifyJob& job, hipStream_t stream);
 
 // Accepted rows to the front of a request's rows (fedrag_paged_keep).

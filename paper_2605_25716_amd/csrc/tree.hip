@@ -736,13 +736,19 @@ FEDRAG_KERNEL __launch_bounds__(kWholeThreads) void tree_verify_whole_kernel(Tre
 }
 
 static int verify_parts(int vocab) { return (vocab + kPart - 1) / kPart; }
-size_t tree_verify_workspace(int batch, int vocab) {
+// Rows that one workgroup has in registers, none shorter than a load of a lane.
+static bool verify_whole(int vocab, int dtype) {
+    const size_t bytes = (size_t)vocab * (dtype == FEDRAG_F32 ? 4 : 2);
+    return bytes >= 16 && bytes <= kWholeBytes;
+}
+size_t tree_verify_workspace(int batch, int vocab, int dtype) {
+    if (verify_whole(vocab, dtype)) return 0;
     return 2 * (size_t)batch * (sizeof(VerifyState) + (size_t)verify_parts(vocab) * sizeof(uint64_t));
 }
 
 template <class E>
 static hipError_t launch_tree_verify_t(const TreeVerifyJob& job, hipStream_t stream) {
-    if (job.vocab >= 16 / (int)sizeof(E) && (size_t)job.vocab * sizeof(E) <= kWholeBytes) {
+    if (verify_whole(job.vocab, job.dtype)) {
         hipLaunchKernelGGL((job.draft ? tree_verify_whole_kernel<E, true> : tree_verify_whole_kernel<E, false>), dim3((unsigned)job.batch),
                            dim3(kWholeThreads), 0, stream, job);
         return hipGetLastError();

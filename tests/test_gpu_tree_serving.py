@@ -244,17 +244,18 @@ def test_calls_at_once():
             assert all(torch.equal(i, j) for i, j in zip(x, y))
 
 
-def test_recorded_verification_replays():
-    """Rounds over a workspace that holds anything, replayed with new inputs in place."""
+@pytest.mark.parametrize("V", [5000, 40000])
+def test_recorded_verification_replays(V):
+    """One launch, and rounds over a workspace that holds anything, replayed with new inputs in place."""
     rng = np.random.default_rng(1)
     sizes = [9, 30, 4]
-    start, T, V = TR.starts(sizes), sum(sizes), 5000
+    start, T = TR.starts(sizes), sum(sizes)
     up = TR.trees(rng, sizes)
     g = torch.Generator().manual_seed(1)
     draw = lambda: [torch.softmax(2 * torch.randn((T, V), generator=g), -1) for _ in range(2)]  # noqa: E731
     p, q = (x.to(DEV) for x in draw())
     tokens, u, un = i32([0] * T), torch.zeros(T, dtype=torch.float64, device=DEV), torch.zeros(3, dtype=torch.float64, device=DEV)
-    ws = torch.full((fb.fedrag_tree_verify_workspace_bytes(3, V),), 255, dtype=torch.uint8, device=DEV)
+    ws = torch.full((fb.fedrag_tree_verify_workspace_bytes(3, V, torch.float32),), 255, dtype=torch.uint8, device=DEV)
     args = (p, tokens, i32(up), i32(start), u, un)
     fb.fedrag_tree_verify(*args, draft=q, max_kept=7, workspace=ws)
     graph = torch.cuda.CUDAGraph()

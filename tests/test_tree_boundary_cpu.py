@@ -98,7 +98,7 @@ def test_attn_workspace(lib):
         assert lib.fedrag_paged_tree_attn_workspace_bytes(*bad) == 0
 
 
-VERIFY = dict(batch=2, n_rows=10, vocab=500, dtype=fb.F32, q_start=A, parents=2 * A, tokens=3 * A, target=4 * A, ts=500, draft=5 * A, ds=500, u=6 * A,
+VERIFY = dict(batch=2, n_rows=10, vocab=70000, dtype=fb.F32, q_start=A, parents=2 * A, tokens=3 * A, target=4 * A, ts=70000, draft=5 * A, ds=70000, u=6 * A,
               u_next=7 * A, most=4, kept=8 * A, n_kept=9 * A, next=10 * A, ws=11 * A, ws_bytes=1 << 20)
 
 
@@ -112,11 +112,11 @@ def verify_call(lib, **kw):
 def test_verify_refusals(lib):
     for k in ("q_start", "parents", "tokens", "target", "u", "u_next", "kept", "n_kept", "next"):
         assert verify_call(lib, **{k: None}) == fb.ERR_NULL, k
-    for k, v in (("batch", -1), ("batch", 65536), ("n_rows", -1), ("n_rows", 2 ** 31 - 1), ("vocab", 0), ("vocab", (1 << 20) + 1), ("ts", 499),
-                 ("ds", 499), ("most", 0), ("most", 1 << 31), ("ts", 1 << 61), ("ds", 1 << 61)):
+    for k, v in (("batch", -1), ("batch", 65536), ("n_rows", -1), ("n_rows", 2 ** 31 - 1), ("vocab", 0), ("vocab", (1 << 20) + 1), ("ts", 69999),
+                 ("ds", 69999), ("most", 0), ("most", 1 << 31), ("ts", 1 << 61), ("ds", 1 << 61)):
         assert verify_call(lib, **{k: v}) == fb.ERR_SHAPE, (k, v)
     assert verify_call(lib, dtype=3) == fb.ERR_UNSUPPORTED
-    need = lib.fedrag_tree_verify_workspace_bytes(2, 500)
+    need = lib.fedrag_tree_verify_workspace_bytes(2, 70000, fb.F32)
     assert need > 0 and verify_call(lib, ws=None) == fb.ERR_WORKSPACE and verify_call(lib, ws_bytes=need - 1) == fb.ERR_WORKSPACE
     for k in ("q_start", "parents", "tokens", "target", "draft", "kept", "n_kept", "next"):
         assert verify_call(lib, **{k: VERIFY[k] + 2}) == fb.ERR_ALIAS, k
@@ -128,7 +128,10 @@ def test_verify_refusals(lib):
             if o != other:
                 assert verify_call(lib, **{o: VERIFY[other]}) == fb.ERR_ALIAS, (o, other)
     assert verify_call(lib, batch=0, q_start=None, u_next=None, kept=None, n_kept=None, next=None) == fb.OK
-    for bad in ((-1, 500), (2, 0), (65536, 500), (2, (1 << 20) + 1)):
+    for dtype, most in ((fb.F32, 32768), (fb.BF16, 65536), (fb.F16, 65536)):  # what one workgroup has in its registers
+        for vocab, some in ((1, True), (3 if dtype == fb.F32 else 7, True), (8, False), (500, False), (most, False), (most + 1, True)):
+            assert (lib.fedrag_tree_verify_workspace_bytes(2, vocab, dtype) > 0) == some, (dtype, vocab)
+    for bad in ((-1, 70000, fb.F32), (2, 0, fb.F32), (65536, 70000, fb.F32), (2, (1 << 20) + 1, fb.F32), (2, 70000, 3)):
         assert lib.fedrag_tree_verify_workspace_bytes(*bad) == 0
 
 
