@@ -14,9 +14,9 @@
 //   the transposing LDS read.  An operand of K or V is read once for all of a wave's rows.
 // Probabilities enter the second product as two storage-type terms in fp16 (22 significant bits) and three in bf16 (24; of two workgroups a
 // tile two, 16: there the third would cost 3 to 10 %, 64 rows of 64 columns 162 -> 177 us, up to 32 rows 0 to 1.5 %; outputs of drafts behind
-// short requests are 2e-7 to 4e-7 off with it, 6e-7 to 1e-6 without).  They are relative to the largest score so far, whose own probability
-// is a power of two and exact; outputs are rescaled only where it moves.  (Leaving it until it is 2^8 off takes 1 % off the time and doubles
-// the error of rows whose weight sits on few tokens.)
+// short requests are 2e-7 to 4e-7 off with it, 6e-7 to 1e-6 without).  They are relative to the largest score so far: in a masked
+// tile its own probability is a power of two and exact, elsewhere off by what its rounding took; outputs are rescaled only where it moves.
+// (Leaving it until it is 2^8 off takes 1 % off the time and doubles the error of rows whose weight sits on few tokens.)
 // Only the key tiles that hold drafted tokens are masked, by bits of the rows' words.
 #pragma once
 #include "attn_paged.h"
@@ -238,9 +238,15 @@ __device__ __forceinline__ void tree_body(const PagedArgs& a, uint32_t wg, Slots
                     for (int t = 0; t < DCH; ++t) acc[g][t] *= alpha;
                 }
                 float x[8];
-                if constexpr (masked) {  // a key alone has a power of two
+                if constexpr (masked) {
+                    // A key alone has a power of two: the product is rounded as the maximum's was.  (Contracted to one operation, the probability
+                    // is 2^(what that rounding took off): in two bf16 terms a lone key's V came back 7e-6 off at scores of 3 * 10^5, in fp16 2.4e-7.)
+#pragma clang fp contract(off)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] = s[g][e / 4][e % 4] * scale_log2 - m_run[g];
+                    for (int e = 0; e < 8; ++e) {
+                        const float product = s[g][e / 4][e % 4] * scale_log2;
+                        x[e] = product - m_run[g];
+                    }
                 } else {  // one rounding of the exponent's argument
 #pragma unroll
                     for (int e = 0; e < 8; ++e) x[e] = __builtin_fmaf(s[g][e / 4][e % 4], scale_log2, -m_run[g]);
