@@ -193,16 +193,11 @@ fedrag_status paged_attn(const fedrag_shape* shape, int64_t n_rows, const fedrag
                          cache->page_tokens, max_q_len, tree, &need))
         return FEDRAG_ERR_SHAPE;
     if (need > 0 && (!workspace || workspace_bytes < need)) return FEDRAG_ERR_WORKSPACE;
-    const struct { const void* p; size_t n; } in[] = {{Q->data, qb}, {p.pages.K, extent}, {p.pages.V, extent}, {block_table, (size_t)table},
-                                                      {q_start, ((size_t)shape->batch + 1) * 4}, {kv_lens, (size_t)shape->batch * 4},
-                                                      {tree_mask, (size_t)n_rows * (size_t)mask_words * 8}},
-        out[] = {{O, (size_t)n * 4}, {lse, (size_t)rows * 4}, {workspace, need}};
-    for (const auto& o : out) {
-        for (const auto& i : in)
-            if (overlaps(o.p, o.n, i.p, i.n)) return FEDRAG_ERR_ALIAS;
-        for (const auto& other : out)
-            if (&other != &o && overlaps(o.p, o.n, other.p, other.n)) return FEDRAG_ERR_ALIAS;
-    }
+    const Range in[] = {{Q->data, qb}, {p.pages.K, extent}, {p.pages.V, extent}, {block_table, (size_t)table},
+                        {q_start, ((size_t)shape->batch + 1) * 4}, {kv_lens, (size_t)shape->batch * 4},
+                        {tree_mask, (size_t)n_rows * (size_t)mask_words * 8}},
+                out[] = {{O, (size_t)n * 4}, {lse, (size_t)rows * 4}, {workspace, need}};
+    if (any_overlap(in, out)) return FEDRAG_ERR_ALIAS;
     const int64_t e = (int64_t)elem_size(shape->dtype);
     p.B = shape->batch;
     p.Hq = shape->n_q_heads;
