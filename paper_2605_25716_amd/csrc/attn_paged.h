@@ -272,8 +272,8 @@ __device__ __forceinline__ PagedPiece paged_piece(Args& a, uint32_t index) {
 }
 
 // ---- shares
-// A share is ceil(units of all / target) units, or `least`.  A tile of few units (at most `least`, or an eighth of a share) is not
-// cut: it belongs as a whole to the share in which it begins.  Partials: workgroup w's of a tile that another began in slot 2 w, of one that it begins and does
+// A share is ceil(units of all / target) units, or `least`.  A tile counts its units of keys and, for some kernels, `extra` ones for what it costs
+// beside them.  One of few units of keys (at most `least`, or an eighth of a share) is not cut: it belongs as a whole to the share in which it begins.  Partials: workgroup w's of a tile that another began in slot 2 w, of one that it begins and does
 // not end in slot 2 w + 1.
 struct PagedSpan {
     PagedRequest req;

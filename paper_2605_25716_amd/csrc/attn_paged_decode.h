@@ -14,6 +14,7 @@
 //   which are also its contraction slice of O^T (d x 16) += V^T (d x 32) . P^T (32 x 16), whose V^T operands come through
 //   the transposing LDS read.
 // Probabilities enter the second product as two storage-type terms (about 16 significant bits): outputs are fp32.
+// (attn_tree.h has the same way of the keys, walk along a share and fold for rows with masks: a mend here concerns it, too.)
 #pragma once
 #include "attn_paged.h"
 

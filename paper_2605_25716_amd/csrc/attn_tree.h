@@ -18,6 +18,8 @@
 // tile its own probability is a power of two and exact, elsewhere off by what its rounding took; outputs are rescaled only where it moves.
 // (Leaving it until it is 2^8 off takes 1 % off the time and doubles the error of rows whose weight sits on few tokens.)
 // Only the key tiles that hold drafted tokens are masked, by bits of the rows' words.
+// The way of the keys (pages, descriptors, LDS, its swizzles), the walk along a share and the fold of the waves are attn_paged_decode.h's, written
+// again for several groups of rows: what is mended in the one has to be looked at in the other.
 #pragma once
 #include "attn_paged.h"
 
