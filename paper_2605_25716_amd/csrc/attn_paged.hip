@@ -216,7 +216,9 @@ static PagedPlan paged_plan(int B, int Hq, int Hkv, int dtype, int64_t T, int64_
         const int tile = !many ? 4 : most * G <= 32 ? 5 : 6;
         // A unit of keys is two steps of each wave, or one for 17 to 32 rows where that leaves workgroups for all, few to a tile (32 heads of 128: 6
         // tokens over 500 12.6 us, 14.2 by two steps; 5 each of 8 heads over 1000, 200, 2000 14.0, 15.8; but 1 of 16 heads over 5000 and 2 over 9000
-        // 30.7, 19.8; 16 rows, 2 over 4000, 14.8, 13.5; 64, 16 over 1000, 17.0, 15.3).
+        // 30.7, 19.8; 16 rows, 2 over 4000, 14.8, 13.5; 64, 16 over 1000, 17.0, 15.3).  It goes by the tokens that the table has columns for, as lengths are
+        // not known here: the same requests under a table for 32768 go by two steps (recorded and replayed: 6 over 500 15.5 us for 13.4, the
+        // three of 5 19.2 for 18.6).
         const int target = tile == 6 ? cus : cus + 1;
         const bool short_units = tile == 5 && keys > 256 && keys <= 2048 && tiles(tile) * ((keys + 255) >> 8) <= (int64_t)1 << target >> 1;
         p.shares = paged_shares(PagedCut{tile, short_units ? 7 : 8, 1, target, 1, 1, INT32_MAX}, tiles(tile), keys);

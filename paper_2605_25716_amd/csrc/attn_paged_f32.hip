@@ -12,6 +12,8 @@
 // Bound by the matrix pipe (64 NQ instructions of 32 cycles per 16 KiB of K, V at 128 columns): 1024 rows of 32 heads over 4096 keys
 // 571 to 604 us, 105 TFLOP/s, where a library product of fp32 reaches 150 (every step of 16 keys rescales all outputs, a multiplication
 // for every two matrix instructions at 128 columns); single tokens by HBM (64 over 1000 keys 93 us, 5.6 TB/s).
+// Rows with masks of their own: 32 requests of 1000 to 32768 tokens, 8 KV heads of 128, 2.46 GB: 16 rows a KV head 433 us (5.7 TB/s), 64 rows 832 (94
+// TFLOP/s; each of two tiles reads the keys, 5.9 TB/s if both did so from HBM: which of the two bounds it was not told apart).
 #include "attn_paged.h"
 
 namespace fedrag {

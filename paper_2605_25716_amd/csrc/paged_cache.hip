@@ -376,8 +376,9 @@ hipError_t launch_paged_keep(const PagedKeep& k, hipStream_t stream) {
 // below 0 are none, so that the columns are looked at before any is written.  Up to 1024 columns are a thread's each, of the last
 // workgroup; more are a wave's request by request, the columns of two requests in flight together: a workgroup counts what is before its
 // share, and writes its share (the second time out of L2).  Nothing passes between workgroups, and the last one keeps the books.  64 requests
-// of a page or none 4.5 us on the device; 256 that end at once, 130000 pages, 20: the last workgroup's count of all, at some 50 GB/s.
-// (More columns in flight, or 16 bytes a lane: 33 to 42 us by one workgroup, which takes 30.)
+// of a page or none 4.6 us on the device, 3.9 in place; 256 that end at once, 63541 pages, 20.2, and in place, by one workgroup, 30.4: the last workgroup
+// looks at the whole table by itself, 254 KB, and is bound by its trips, two requests' columns a wave at a time.
+// (More columns in flight, or 16 bytes a lane: 33 to 42 us by one workgroup.)
 constexpr int kTrimWaves = kMapThreads / kWave;
 constexpr int kTrimMost = 16;  // workgroups
 constexpr int kTrimAhead = 4;  // columns of a request that a lane has in flight

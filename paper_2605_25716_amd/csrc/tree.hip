@@ -96,8 +96,8 @@ hipError_t launch_tree_map(int batch, int64_t n_rows, int words, const int32_t* 
 // the request's walk by itself, from the state and the sums of the round before, until a sum over the vocabulary is needed, and adds up
 // its part of it.  The state is the same in all of a request's workgroups, and the first one writes it down.  No workgroup waits for
 // another.  What the last round finds unfinished, the request's first workgroup finishes alone.  Bound by reading the rows while all requests
-// are at it (64 requests of 16 nodes and 128000 tokens in fp32: 13 and 14 us for the first two rounds, 131 MB at most each), later by a round's
-// chain of a launch, state, nodes, part and sums, 6 to 8 us.
+// are at it (64 requests of 16 nodes and 128000 tokens in fp32, under the profiler: 15.4 and 11.2 us for the first two rounds, 66 MB at most each), later by a
+// round's chain of a launch, state, nodes, part and sums, 7 to 9 us.  Without drafts' rows it is one sum, and 11.9 and 8.8 us.
 constexpr int kVerifyThreads = 256;                  // (512: 28.5 us for 20.6 where 64 requests of 128000 tokens only draw)
 constexpr int kPart = 4096;                          // tokens of a workgroup
 constexpr int kEach = kPart / kVerifyThreads;        // and of a thread
@@ -525,9 +525,9 @@ FEDRAG_KERNEL __launch_bounds__(kVerifyThreads) void tree_verify_kernel(TreeVeri
 
 // Rows of up to 128 KiB (32768 tokens in fp32, 65536 in 16 bits): one workgroup to a request, whose threads have the row of p and that of q
 // in registers, so that a sum after the first at a node costs no trip to memory, and one launch does.  Bound by that workgroup's 64-bit
-// arithmetic (8 instructions a token and sum) and by what it can read (256 KB in some 4 us): 12.6 us on the device for 8 nodes of 32000 tokens in
-// fp32, 6.1 for 64 tokens.
-// Against rounds it is ahead everywhere: 1 request of 32000 tokens 11.7 us (17.4 by rounds), 64 23 (35), 200 27 (60), 1000 of 4 nodes 59
+// arithmetic (8 instructions a token and sum) and by what it can read (256 KB in some 4 us): 13.3 us on the device for 8 nodes of 32000 tokens in
+// fp32, 6.0 for 64 tokens, both under the profiler.
+// Against rounds it is ahead everywhere (calls, without it): 1 request of 32000 tokens 11.7 us (17.4 by rounds), 64 23 (35), 200 27 (60), 1000 of 4 nodes 59
 // (104); 128 of 16000 in bf16 21 (50); 8 of 65001 in fp16 26 (31); without drafts 1000 of 32000 45 (64).
 constexpr int kWholeThreads = 1024;
 constexpr int kWholeWaves = kWholeThreads / kWave;
